@@ -65,7 +65,9 @@ typedef enum {
   PIC_ERR_UNSUPPORTED = -6   /* valid request this build has no kernel for */
 } pic_status;
 
-enum { PIC_F32 = 0, PIC_BF16 = 1 };     /* pic_store_desc.dtype */
+/* pic_store_desc.dtype. PIC_FP4: chunk caches are held in 4 bits (17 bytes per
+ * 32 elements); see below. */
+enum { PIC_F32 = 0, PIC_BF16 = 1, PIC_FP4 = 2 };
 enum { PIC_GQA = 0, PIC_MLA = 1 };      /* pic_store_desc.kind  */
 
 /* Shape of a store's chunk caches. d_k and d_v must be multiples of 8.
@@ -80,6 +82,21 @@ enum { PIC_GQA = 0, PIC_MLA = 1 };      /* pic_store_desc.kind  */
  * Each chunk occupies its length rounded up to whole pages in every layer,
  * in one run of consecutive pages when a free run is long enough, else in
  * several (removal leaves holes; no copy ever moves a chunk). */
+/* 4-bit stores (dtype PIC_FP4; GQA only, d_k = d_v of 64 or 128, else
+ * UNSUPPORTED). Everything that goes in or out is bf16: k and v of pic_store_put
+ * and pic_store_write_rows, q, k_self, v_self and out of the link calls, and
+ * the values that pic_debug_gather returns. What a put rounds: a row (one
+ * token of one head) is cut into blocks of 32 elements; a block keeps the
+ * numbers 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign, times 2^e, where e is the
+ * smallest exponent in -126 .. 125 with max|x| < 7 * 2^e (125 where there is
+ * none). Elements are rounded to the nearest such number, ties to the one
+ * with the even index in that list; what lies above 6 * 2^e, infinities too,
+ * becomes 6 * 2^e. A block with a NaN reads as NaN throughout. A row's numbers depend
+ * on that row alone. The request's own KV is not rounded. Store calls, link
+ * calls, plans and export work as for the other dtypes. A NaN in the cached
+ * or own V, or an infinity in the own V, may reach every row of the requests
+ * that link it, also rows that a limit or the causal mask keeps from it; a
+ * query row with a NaN or an infinity gives an output row of NaN or zeros. */
 typedef struct pic_store_desc {
   int32_t kind;
   int32_t dtype;
@@ -368,6 +385,69 @@ pic_status pic_mla_absorb_q(int32_t n_tokens, int32_t n_heads, const void *q, co
                             void *q_out, void *stream);
 pic_status pic_mla_up_v(int32_t n_tokens, int32_t n_heads, const void *o_lat, const void *w_uv,
                         void *out, void *stream);
+
+/* Rotary positions: pairs of a head's elements are turned by an angle that
+ * grows with the token's position, for the queries and keys of a layer before
+ * they are put or linked (chunk caches are computed from position zero, Sec. 1),
+ * and, transposed, for the gradient of that.
+ *   y_a = c x_a - s x_b,  y_b = s x_a + c x_b
+ *   c = magnitude cos(pos f_i),  s = magnitude sin(pos f_i);  transposed: -s
+ * With i = 0 .. rot_dim/2 - 1, pair i is (rot_at + i, rot_at + rot_dim/2 + i)
+ * for PIC_ROPE_HALF, (rot_at + 2i, rot_at + 2i + 1) for PIC_ROPE_INTERLEAVED; the
+ * head's other elements are copied. Frequencies, g_i = theta^(-2i / rot_dim):
+ *   PIC_ROPE_PLAIN   f_i = g_i
+ *   PIC_ROPE_LINEAR  f_i = g_i / factor
+ *   PIC_ROPE_BANDED  f_i = g_i (w + (1 - w) / factor), w = (original_len g_i / 2pi -
+ *                    band_low) / (band_high - band_low) held to 0..1: pairs that
+ *                    turn often within the original length are kept, slow ones
+ *                    stretched (the rule of the Llama-3.1 backbone)
+ *   PIC_ROPE_YARN    the same with w falling over the pair's index, 1 - w = (i - lo) /
+ *                    max(hi - lo, 0.001) held to 0..1, with at(n) = rot_dim
+ *                    ln(original_len / (2pi n)) / (2 ln theta), lo = max(floor(at(
+ *                    turns_fast)), 0), hi = min(ceil(at(turns_slow)), rot_dim - 1)
+ *                    (YaRN, used by the DeepSeek-V2-Lite backbone)
+ * Angles are formed and reduced in 64 bits, products in fp32, and each output is
+ * rounded once.
+ * pic_rope_create: host only. dtype PIC_F32 or PIC_BF16; rot_dim even, 2..256;
+ *   head_dim at most 768; magnitude 1 unless the scaling calls for another
+ *   one. Fields that the scaling does not name are not read. Errors: INVALID,
+ *   UNSUPPORTED, OOM.
+ * pic_rope_apply: n_tensors (1..4) tensors of the same tokens in one launch.
+ *   positions device int32 [n_tokens], any value.
+ *   x, out device [n_tokens][n_heads][head_dim] of the handle's dtype, n_heads
+ *   1..1024, token t at t * stride elements (0: dense, else at least n_heads *
+ *   head_dim: slices of a fused projection). out may be x itself (same stride;
+ *   the elements outside the rotated part are then not touched); buffers must not
+ *   overlap otherwise. Allocates nothing: may be captured. One handle may be
+ *   used by several threads at once. Errors: INVALID, HIP. */
+enum { PIC_ROPE_HALF = 0, PIC_ROPE_INTERLEAVED = 1 };   /* pic_rope_desc.layout */
+enum { PIC_ROPE_PLAIN = 0, PIC_ROPE_LINEAR = 1, PIC_ROPE_BANDED = 2, PIC_ROPE_YARN = 3 };
+typedef struct pic_rope_desc {
+  int32_t dtype;
+  int32_t layout;
+  int32_t head_dim;
+  int32_t rot_at;
+  int32_t rot_dim;
+  int32_t scaling;           /* PIC_ROPE_PLAIN .. PIC_ROPE_YARN */
+  double theta;
+  double factor;
+  double original_len;
+  double band_low, band_high;
+  double turns_fast, turns_slow;
+  double magnitude;
+} pic_rope_desc;
+typedef struct pic_rope_tensor {
+  const void *x;
+  void *out;
+  int64_t x_stride, out_stride;
+  int32_t n_heads;
+} pic_rope_tensor;
+typedef struct pic_rope pic_rope;
+pic_status pic_rope_create(const pic_rope_desc *desc, pic_rope **out);
+pic_status pic_rope_destroy(pic_rope *rope);
+pic_status pic_rope_apply(const pic_rope *rope, int32_t n_tokens, const int32_t *positions,
+                          const pic_rope_tensor *tensors, int32_t n_tensors, int32_t transposed,
+                          void *stream);
 
 /* Kernel timing for measurement. pic_prof_begin() clears and enables
  * recording of HIP events around every launch of the main attention kernel;

@@ -25,6 +25,9 @@ SOURCES = [
     "kernels_stream.hip",
     "kernels_peaks.hip",
     "kernels_mla_proj.hip",
+    "kernels_fp4_store.hip",
+    "kernels_fp4_decode.hip",
+    "kernels_rope.hip",
     "static_scratch.hip",
 ]
 

@@ -1,0 +1,408 @@
+// Link attention over a 4-bit chunk cache on gfx950, one wave per piece of
+// work: 16 rows (query token x query head) of one kv head over a piece of a
+// request's keys.
+//
+// The tiles of the cache hold their codes in the order of the matrix
+// operands (fp4.hpp), so a wave streams them from HBM into registers, 1 KB per
+// load, widens them there (a conversion that takes the block's scale: one
+// instruction per two elements) and multiplies:
+//   S^T[64 keys][16 rows] = K . Q^T       4 key blocks x D/32 steps of
+//                                         v_mfma_f32_16x16x32_bf16
+//   O^T[D][16 rows]      += V^T . P^T     D/16 channel blocks x 2 steps
+// After the first product lane (n, g) holds the scores of row n for the keys
+// 16 b + 4 g + i, which are the keys that its operand of the second one
+// needs: no exchange between lanes. Value codes lie key by key with their channels
+// side by side (a row has its own scales); conversions give pairs of
+// channels, and one byte permute per pair of keys turns them into pairs of keys.
+// Channel block cb, index m is channel D/16 * m + cb, so that a lane ends with
+// D/16 neighbouring channels.
+//
+// The own KV is bf16 and read in place, 32 keys at a time, its key rows as they
+// are and its value rows through the same permutes.
+//
+// Softmax: log2 domain, exact running max per tile, sums of the probabilities
+// in fp32 before they are rounded to bf16 for the matrix product (half a step,
+// 2^-9 of each; keys and values are exact in bf16).
+#include "fp4.hpp"
+
+namespace pic {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(1))) const u32x4 *global_u32x4;
+
+constexpr int kRows = 16;
+constexpr int kWaves = 4;
+
+__device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
+__device__ __forceinline__ uint32_t word(uint4 u, int i) {
+  return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
+}
+
+// Reduction over the 4 lane groups (l, l^16, l^32, l^48) of a row.
+__device__ __forceinline__ float row_max(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ uint4 load_nt(const char *p) {
+  const u32x4 w = __builtin_nontemporal_load((global_u32x4)p);
+  return make_uint4(w.x, w.y, w.z, w.w);
+}
+
+// A 64-key tile of the cache as loaded.
+template <int D>
+struct CacheTile {
+  static constexpr int kKeyBlocks = 4;
+  uint4 k[D / 32], v[D / 32];
+  uint32_t ks;      // K scales of key blocks 0..3 (this lane's block of 32)
+  uint4 vs;         // V scales of keys 16 b + 4 g + i (this lane's channels)
+
+  __device__ __forceinline__ void load(const char *tile, int lane) {
+    typedef Fp4Tile<D> T;
+    const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      k[j] = load_nt(tile + j * 1024 + lane * 16);
+      v[j] = load_nt(tile + T::kV + j * 1024 + lane * 16);
+    }
+    const int kc = D == 128 ? g : g >> 1;
+    const int vc = m * (D / 16) / 32;
+    ks = *(const uint32_t *)(tile + T::kKs + (kc * 16 + m) * 4);
+    vs = *(const uint4 *)(tile + T::kVs + (g * T::kBlocks + vc) * 16);
+  }
+  // Operand of key block b, step s: elements D/4 * g + 8 s ..+7 of key 16 b + m.
+  __device__ __forceinline__ bf16x8 key(int b, int s) const {
+    const float sc = fp4_scale((ks >> (8 * b)) & 255u);
+    const uint32_t c = D == 128 ? word(k[b % (D / 32)], s)
+                                : word(k[b / 2 % (D / 32)], 2 * (b & 1) + s);
+    return as_bf16x8(fp4_decode8(c, sc));
+  }
+  // Channels 2 c, 2 c + 1 of this lane's, key 16 b + 4 g + i.
+  template <int kC>
+  __device__ __forceinline__ uint32_t value(int b, int i) const {
+    const float sc = fp4_scale((word(vs, b) >> (8 * i)) & 255u);
+    if constexpr (D == 128) {
+      return fp4_pair<kC>(word(v[b % (D / 32)], i), sc);
+    } else {
+      const uint32_t w = word(v[b / 2 % (D / 32)], 2 * (b & 1) + (i >> 1));
+      return (i & 1) ? fp4_pair<2 + (kC & 1)>(w, sc) : fp4_pair<kC & 1>(w, sc);
+    }
+  }
+};
+
+// 32 own keys, read in place. k, v: this kv head's first own row; stride: bytes per
+// token. Keys past the last own one reread it (their scores are masked), with
+// zeros for values: 0 times an infinity would be a NaN.
+template <int D>
+struct OwnTile {
+  static constexpr int kKeyBlocks = 2;
+  uint4 k[2][D / 32];
+  uint32_t v[2][4][D / 32];
+
+  __device__ __forceinline__ void load(const char *kr, const char *vr, int64_t stride, int j0,
+                                       int last, int lane) {
+    const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const char *row = kr + min(j0 + 16 * b + m, last) * stride + g * (D / 2);
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) k[b][s] = *(const uint4 *)(row + 16 * s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = j0 + 16 * b + 4 * g + i;
+        const char *vp = vr + min(key, last) * stride + m * (D / 8);
+        const uint32_t keep = key <= last ? ~0u : 0u;
+#pragma unroll
+        for (int c = 0; c < D / 32; c += 2) {
+          const uint2 w = *(const uint2 *)(vp + 4 * c);
+          v[b][i][c] = w.x & keep;
+          v[b][i][c + 1] = w.y & keep;
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ bf16x8 key(int b, int s) const { return as_bf16x8(k[b][s]); }
+  template <int kC>
+  __device__ __forceinline__ uint32_t value(int b, int i) const {
+    return v[b][i][kC];
+  }
+};
+
+template <int D>
+struct State {
+  f32x4 o[D / 16];  // channel block cb: channels D/16 * (4 g + i) + cb of row n
+  float m, l;       // running max (log2 domain, per row) and this lane's part of the sum
+};
+
+template <int D, int kC, class Tile>
+__device__ __forceinline__ void value_pair(const Tile &x, int t, bf16x8 pf, State<D> &st) {
+  uint4 lo, hi;
+  uint32_t d[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    d[i] = x.template value<kC>(2 * t, i);
+    d[4 + i] = x.template value<kC>(2 * t + 1, i);
+  }
+  lo = make_uint4(__builtin_amdgcn_perm(d[1], d[0], 0x05040100u),
+                  __builtin_amdgcn_perm(d[3], d[2], 0x05040100u),
+                  __builtin_amdgcn_perm(d[5], d[4], 0x05040100u),
+                  __builtin_amdgcn_perm(d[7], d[6], 0x05040100u));
+  hi = make_uint4(__builtin_amdgcn_perm(d[1], d[0], 0x07060302u),
+                  __builtin_amdgcn_perm(d[3], d[2], 0x07060302u),
+                  __builtin_amdgcn_perm(d[5], d[4], 0x07060302u),
+                  __builtin_amdgcn_perm(d[7], d[6], 0x07060302u));
+  st.o[2 * kC] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(lo), pf, st.o[2 * kC], 0, 0, 0);
+  st.o[2 * kC + 1] =
+      __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(hi), pf, st.o[2 * kC + 1], 0, 0, 0);
+}
+
+// kl: last visible key of the tile for this lane's row (relative to the tile),
+// used where masked.
+template <int D, class Tile>
+__device__ __forceinline__ void compute_tile(const Tile &x, const bf16x8 (&qf)[D / 32],
+                                             State<D> &st, int lane, bool masked, int kl,
+                                             float sc) {
+  constexpr int kB = Tile::kKeyBlocks;
+  f32x4 s[kB];
+#pragma unroll
+  for (int b = 0; b < kB; ++b) {
+    s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+      s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.key(b, j), qf[j], s[b], 0, 0, 0);
+  }
+  if (masked) {
+    const int k0 = kl - 4 * (lane >> 4);
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (16 * b + i > k0) s[b][i] = -INFINITY;
+  }
+  float tmax = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < kB; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, s[b][i]);
+  tmax = row_max(tmax);
+  const float mnew = fmaxf(st.m, tmax * sc);
+  if (mnew > st.m) {             // per lane: rescale this row's state
+    const float alpha = __builtin_amdgcn_exp2f(st.m - mnew);   // 0 when st.m = -inf
+    st.l *= alpha;
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) st.o[b] *= alpha;
+    st.m = mnew;
+  }
+  const float neg_m = st.m == -INFINITY ? 0.f : -st.m;
+#pragma unroll
+  for (int t = 0; t < kB / 2; ++t) {
+    bf16x8 pf;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * t][i], sc, neg_m));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * t + 1][i], sc, neg_m));
+      st.l += p0 + p1;
+      pf[i] = (__bf16)p0;
+      pf[4 + i] = (__bf16)p1;
+    }
+    value_pair<D, 0>(x, t, pf, st);
+    value_pair<D, 1>(x, t, pf, st);
+    if constexpr (D == 128) {
+      value_pair<D, 2>(x, t, pf, st);
+      value_pair<D, 3>(x, t, pf, st);
+    }
+  }
+}
+
+// Walk over the tiles of a request's documents.
+struct Cursor {
+  const_links links;       // the request's links, from the item's first on
+  int li;
+  const char *base;        // the link's first tile
+  int len, tok0, tile0, end;
+};
+__device__ __forceinline__ void cursor_next(Cursor &c) {
+  ++c.li;
+  c.base = (const char *)c.links[c.li].k;
+  c.len = c.links[c.li].len;
+  c.tok0 = c.links[c.li].tok0;
+  c.tile0 = c.links[c.li].tile0;
+  c.end = c.tile0 + (c.len + kTile - 1) / kTile;
+}
+struct TileInfo {
+  const char *p;
+  int nvalid, tok;
+};
+
+// kLim: rows see different numbers of linked rows.
+template <int D, bool kLim>
+__global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t u = (int64_t)blockIdx.x * kWaves + wave;
+  const int64_t units = (int64_t)p.n_items * p.n_kv_heads;
+  const int rb = (int)(u / units);
+  if (rb >= p.nrb) return;
+  const int kvh = (int)(u % p.n_kv_heads);
+  const WorkItem it = load_item(p.items, (int)(u % units / p.n_kv_heads));
+  const ReqEntry R = item_request(it);
+  const int group = p.group;
+  const int nrows = R.lq * group, row0 = rb * kRows;
+  if (row0 >= nrows) return;
+
+  // this lane's row
+  const int n = lane & 15, g = lane >> 4;
+  const int row = row0 + n;
+  const bool rvalid = row < nrows;
+  const int qi = rvalid ? row / group : 0;
+  const int qh = kvh * group + (rvalid ? row % group : 0);
+  const int own_last = rvalid ? qi + R.ls - R.lq : -1;      // last visible own key
+  const int64_t orow = (int64_t)(R.q0 + qi) * p.n_q_heads + qh;
+  int dl = kNoLimit, dmin = kNoLimit;
+  if (kLim) {
+    if (rvalid) dl = p.doc_lim[R.q0 + qi];
+    dmin = dl;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) dmin = min(dmin, __shfl_xor(dmin, o));
+    dmin = __builtin_amdgcn_readfirstlane(dmin);
+  }
+
+  Cursor c;
+  c.links = (const_links)p.links + it.link;
+  c.li = 0;
+  c.base = (const char *)it.k;
+  c.len = it.len;
+  c.tok0 = it.tok0;
+  c.tile0 = it.tile0;
+  c.end = it.tile0 + (it.len + kTile - 1) / kTile;
+  auto info = [&](int t) {       // t only grows
+    while (t >= c.end) cursor_next(c);
+    const int tt = t - c.tile0;
+    return TileInfo{c.base + ((int64_t)tt * p.n_kv_heads + kvh) * Fp4Tile<D>::kBytes,
+                    min(kTile, c.len - tt * kTile), c.tok0 + tt * kTile};
+  };
+  const int t_begin = it.t_begin, doc_end = min(it.t_end, R.doc_tiles);
+  CacheTile<D> ta, tb;
+  TileInfo ia{}, ib{};
+  if (t_begin < doc_end) {
+    ia = info(t_begin);
+    ta.load(ia.p, lane);
+  }
+  bf16x8 qf[D / 32];
+  {
+    const uint4 *qrow = (const uint4 *)((const uint16_t *)p.q + orow * D + g * (D / 4));
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (rvalid) v = qrow[s];
+      qf[s] = as_bf16x8(v);
+    }
+  }
+  State<D> st;
+#pragma unroll
+  for (int b = 0; b < D / 16; ++b) st.o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  st.m = -INFINITY;
+  st.l = 0.f;
+  const float sc = p.scale_log2;
+  auto doc_tile = [&](const CacheTile<D> &x, const TileInfo &i) {
+    const bool masked = i.nvalid < kTile || (kLim && i.tok + kTile > dmin);
+    compute_tile<D>(x, qf, st, lane, masked, (kLim ? min(i.nvalid, dl - i.tok) : i.nvalid) - 1, sc);
+  };
+  // The load past the last tile reads the last one again, which keeps the
+  // loop free of branches around loads (the compiler waits for every load in
+  // flight where such paths meet).
+  for (int t = t_begin; t < doc_end; t += 2) {
+    ib = info(min(t + 1, doc_end - 1));
+    tb.load(ib.p, lane);
+    doc_tile(ta, ia);
+    if (t + 1 >= doc_end) break;
+    ia = info(min(t + 2, doc_end - 1));
+    ta.load(ia.p, lane);
+    doc_tile(tb, ib);
+  }
+  // Own tiles up to the one that holds the block's last visible key.
+  const int last_qi = (min(row0 + kRows, nrows) - 1) / group;
+  const int t_end = min(it.t_end, visible_tiles(R, last_qi));
+  const int own0 = max(t_begin, R.doc_tiles);
+  if (own0 < t_end) {
+    int s0 = it.tok0;             // the own link's: its first own row
+    if (it.tile0 < R.doc_tiles) {
+      while (c.tile0 < R.doc_tiles) cursor_next(c);
+      s0 = c.tok0;
+    }
+    const int64_t at = ((int64_t)s0 * p.n_kv_heads + kvh) * D * 2;
+    const int64_t stride = (int64_t)p.n_kv_heads * D * 2;
+    const int k_end = min(R.ls, (t_end - R.doc_tiles) * kTile);
+    for (int j0 = (own0 - R.doc_tiles) * kTile; j0 < k_end; j0 += 32) {
+      OwnTile<D> x;
+      x.load((const char *)p.k_self + at, (const char *)p.v_self + at, stride, j0, R.ls - 1, lane);
+      compute_tile<D>(x, qf, st, lane, true, min(own_last, R.ls - 1) - j0, sc);
+    }
+  }
+
+  const float ltot = row_sum(st.l);
+  if (!rvalid) return;
+  if (it.part < 0) {
+    const float inv = ltot > 0.f ? 1.f / ltot : 0.f;
+    uint16_t *out = (uint16_t *)p.out + orow * D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __bf16 v[D / 16];
+#pragma unroll
+      for (int b = 0; b < D / 16; ++b) v[b] = (__bf16)(st.o[b][i] * inv);
+      if constexpr (D == 128)
+        *(uint4 *)(out + 8 * (4 * g + i)) = __builtin_bit_cast(uint4, v);
+      else
+        *(uint2 *)(out + 4 * (4 * g + i)) = __builtin_bit_cast(uint2, v);
+    }
+    if (p.lse && g == 0) p.lse[orow] = ltot == 0.f ? -INFINITY : log_sum(st.m, ltot);
+  } else {
+    const int64_t prow = it.part + (orow - (int64_t)R.q0 * p.n_q_heads);
+    float *po = p.part_o + prow * D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int b = 0; b < D / 16; b += 4)
+        *(float4 *)(po + (D / 16) * (4 * g + i) + b) =
+            make_float4(st.o[b][i], st.o[b + 1][i], st.o[b + 2][i], st.o[b + 3][i]);
+    if (g == 0) {
+      p.part_m[prow] = partial_max(st.m, ltot);
+      p.part_l[prow] = ltot;
+    }
+  }
+}
+
+}  // namespace
+
+int fp4_rows_per_block() { return kRows; }
+
+hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **name) {
+  *name = "link_fp4_kernel";
+  const int64_t units = (int64_t)p.n_items * p.n_kv_heads * p.nrb;
+  const dim3 grid((unsigned)((units + kWaves - 1) / kWaves)), block(64 * kWaves);
+  if (p.d_k == 128) {
+    if (p.doc_lim)
+      hipLaunchKernelGGL((link_fp4_kernel<128, true>), grid, block, 0, st, p);
+    else
+      hipLaunchKernelGGL((link_fp4_kernel<128, false>), grid, block, 0, st, p);
+  } else {
+    if (p.doc_lim)
+      hipLaunchKernelGGL((link_fp4_kernel<64, true>), grid, block, 0, st, p);
+    else
+      hipLaunchKernelGGL((link_fp4_kernel<64, false>), grid, block, 0, st, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace pic

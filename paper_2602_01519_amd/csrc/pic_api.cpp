@@ -18,6 +18,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "fp4.hpp"
 #include "pic_internal.hpp"
 
 namespace pic {
@@ -166,6 +167,7 @@ struct pic_store {
   int64_t live_plans = 0;
   int64_t k_tok_elems = 0;       // K elements per padded token (all heads)
   int64_t v_tok_elems = 0;       // V elements per padded token (GQA)
+  int64_t page_bytes = 0;        // bytes of a 64-token page in one layer
   std::unordered_map<uint64_t, Slot> map;
   Stage ring[kRing];
   int next = 0;
@@ -292,13 +294,40 @@ bool alloc_pages(pic_store *s, int64_t pages, std::vector<Run> &out) {
   return true;
 }
 
+bool is_fp4(const pic_store_desc &d) { return d.dtype == PIC_FP4; }
+
+// Type of q, own KV and out.
+int io_dtype(const pic_store_desc &d) { return is_fp4(d) ? PIC_BF16 : d.dtype; }
+
+// Bytes of a 64-token page of one layer.
+int64_t page_bytes(const pic_store_desc &d, int64_t k_tok_elems, int64_t v_tok_elems, int esz) {
+  return is_fp4(d) ? fp4_page_bytes(d.n_kv_heads, d.d_k) : kTile * (k_tok_elems + v_tok_elems) * esz;
+}
+
+// Moves a link's first token `skip` tokens (whole pages) on within its run.
+void skip_tokens(const pic_store *s, LinkEntry &E, int64_t skip) {
+  const pic_store_desc &d = s->desc;
+  if (is_fp4(d)) {
+    E.k = E.v = (const char *)E.k + skip / kTile * s->page_bytes;
+    return;
+  }
+  // rows of K, panels of V^T (the head stride stays the run's)
+  E.k = (const char *)E.k + skip * d.d_k * s->esz;
+  E.v = d.kind == PIC_MLA ? E.k : (const char *)E.v + skip * d.d_v * s->esz;
+}
+
 // Link-table entry of one run of a chunk in `layer`.
 LinkEntry run_entry(const pic_store *s, const Run &r, int32_t layer) {
-  const int64_t slot_tok_bytes = (s->k_tok_elems + s->v_tok_elems) * s->esz;
   const int32_t lp = r.pages * kTile;
   const int64_t skip_tok = (int64_t)r.skip * kTile;
-  const char *block = s->pool + (int64_t)layer * s->layer_bytes + r.page0 * kTile * slot_tok_bytes;
+  const char *block = s->pool + (int64_t)layer * s->layer_bytes + r.page0 * s->page_bytes;
   LinkEntry E{};
+  if (is_fp4(s->desc)) {
+    E.k = E.v = block + r.skip * s->page_bytes;
+    E.len = r.ntok;
+    E.lp = lp;
+    return E;
+  }
   // K rows and V^T panels of the view start skip_tok tokens into the block
   // (skip_tok is a multiple of the 32-token panel: skip_tok * d_v elements)
   E.k = block + skip_tok * s->desc.d_k * s->esz;
@@ -460,11 +489,9 @@ pic_status plan_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, f
       for (const Run &run : sl.runs) {
         if (run.tok0 + run.ntok <= start) continue;
         LinkEntry E = run_entry(s, run, layer);
-        // skip the run's pages before `start`: rows of K, panels of V^T
-        // (the head stride stays the run's)
+        // skip the run's pages before `start`
         const int32_t skip = std::max(0, start - run.tok0);
-        E.k = (const char *)E.k + (int64_t)skip * d.d_k * s->esz;
-        E.v = d.kind == PIC_MLA ? E.k : (const char *)E.v + (int64_t)skip * d.d_v * s->esz;
+        skip_tokens(s, E, skip);
         E.len -= skip;
         E.tile0 = (int32_t)tiles;
         E.tok0 = (int32_t)toks;
@@ -507,9 +534,13 @@ pic_status plan_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, f
       E.lp = (int32_t)round_up(R.ls, kTile);
       E.tile0 = (int32_t)tiles;
       E.tok0 = (int32_t)toks;
-      P.own.emplace_back((int32_t)P.links.size(), P.own_bytes);
-      P.own_bytes += round_up((int64_t)E.lp * slot_tok_bytes, 256);
-      P.max_own_lp = std::max(P.max_own_lp, E.lp);
+      if (is_fp4(d)) {
+        E.tok0 = R.s0;          // its kernels read the own rows in place
+      } else {
+        P.own.emplace_back((int32_t)P.links.size(), P.own_bytes);
+        P.own_bytes += round_up((int64_t)E.lp * slot_tok_bytes, 256);
+        P.max_own_lp = std::max(P.max_own_lp, E.lp);
+      }
       P.links.push_back(E);
       tiles += E.lp / kTile;
     }
@@ -575,7 +606,7 @@ void prof_stop(hipStream_t st, std::pair<hipEvent_t, hipEvent_t> *ev, const char
 }
 
 enum class Mode { Prefill, Decode };
-enum class Kern { Valu, Mfma128, Decode128, Mla, Stream };
+enum class Kern { Valu, Mfma128, Decode128, Mla, Stream, Fp4 };
 
 // Everything about a call that does not depend on its tensors: the resolved
 // tables, the kernel, the split count and the workspace layout
@@ -933,6 +964,11 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     c.slots = 8 * (int64_t)cus;
     c.over = 2;
     c.min_piece = 1;
+  } else if (kern == Kern::Fp4) {
+    us = 5.0;
+    c.slots = 8 * (int64_t)cus;
+    c.over = 2;
+    c.min_piece = 1;
   } else {
     // Cycles of a wave's 32-key tile. fp32: D / 16 x 16 matrix instructions of
     // 32 cycles per 16 rows. bf16: 22 per row. Measured, 8 requests x 512 tokens
@@ -1070,6 +1106,7 @@ size_t noalloc_charge(const pic_store *s, const Setup &C, int32_t num_splits) {
   }
   const size_t part = splits > 1 ? (size_t)P.total_q * C.lp.n_q_heads * splits * (d.d_v + 2) * 4 : 0;
   if ((C.kern == Kern::Valu || C.kern == Kern::Stream) && small_tables(P)) return part;
+  // (the 4-bit kernels read the own KV in place: P.own_bytes is 0)
   return round_up(sizeof(LinkEntry) * P.links.size(), 256) +
          round_up(sizeof(ReqEntry) * P.reqs.size(), 256) +
          round_up(sizeof(int32_t) * P.reqs.size(), 256) +
@@ -1086,6 +1123,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   if (rc != PIC_OK) return rc;
   const pic_store_desc &d = s->desc;
   const bool mla = d.kind == PIC_MLA;
+  const bool fp4 = is_fp4(d);
   LinkParams &lp = C.lp;
   lp.batch = req->batch;
   lp.n_q_heads = n_q_heads;
@@ -1121,6 +1159,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   // per-row masks of the flash kernel
   if (kern == Kern::Decode128 && !P.doc_lim.empty()) kern = Kern::Mfma128;
   if (d.dtype == PIC_BF16 && mla && d.d_k == 576 && d.d_v == 512) kern = Kern::Mla;
+  if (fp4) kern = Kern::Fp4;
   // A small generic call of a shape the lean kernel is built for (tables as
   // a kernel argument, at most kLeanTiles tiles in all) runs it; other fp32
   // and narrow bf16 GQA calls stream their keys through the matrix cores.
@@ -1147,6 +1186,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
                              : kern == Kern::Stream ? ss.rows * 4 / ss.kpar
                              : kern == Kern::Valu  ? valu_rows_per_block()
                              : kern == Kern::Mla   ? mla_rows_per_block()
+                             : kern == Kern::Fp4   ? fp4_rows_per_block()
                                                    : decode_d128_max_rows();
   C.rows_per_block = rows_per_block;
   lp.nrb = std::max(1, (P.max_rows + rows_per_block - 1) / rows_per_block);
@@ -1275,12 +1315,14 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
     e = launch_link_mfma_d128(lp, st, &name);
   else if (C.kern == Kern::Stream)
     e = launch_link_stream(lp, d.dtype, C.stream_rows, st, &name);
+  else if (C.kern == Kern::Fp4)
+    e = launch_link_fp4(lp, st, &name);
   else
     e = launch_link_valu(lp, d.dtype, mla, st, &name);
   prof_stop(st, &ev, name);
   if (e != hipSuccess) return hip_fail(e, name);
   if (C.splits > 1) {
-    e = launch_combine(lp, d.dtype, lp.max_rows * d.n_kv_heads, st);
+    e = launch_combine(lp, io_dtype(d), lp.max_rows * d.n_kv_heads, st);
     if (e != hipSuccess) return hip_fail(e, "combine_kernel");
   }
   return PIC_OK;
@@ -1432,7 +1474,8 @@ pic_status pic_store_create(const pic_store_desc *desc, pic_store **out) {
   *out = nullptr;
   const pic_store_desc &d = *desc;
   if (d.kind != PIC_GQA && d.kind != PIC_MLA) return fail(PIC_ERR_INVALID, "unknown kind %d", d.kind);
-  if (d.dtype != PIC_F32 && d.dtype != PIC_BF16) return fail(PIC_ERR_INVALID, "unknown dtype %d", d.dtype);
+  if (d.dtype != PIC_F32 && d.dtype != PIC_BF16 && d.dtype != PIC_FP4)
+    return fail(PIC_ERR_INVALID, "unknown dtype %d", d.dtype);
   if (d.n_layers < 0 || d.n_layers > 256) return fail(PIC_ERR_INVALID, "n_layers must be 0..256");
   if (d.n_kv_heads <= 0 || d.d_k <= 0 || d.d_v <= 0 || d.capacity_tokens <= 0)
     return fail(PIC_ERR_INVALID, "n_kv_heads, d_k, d_v and capacity_tokens must be positive");
@@ -1441,6 +1484,8 @@ pic_status pic_store_create(const pic_store_desc *desc, pic_store **out) {
   if (d.d_k % 8 || d.d_v % 8) return fail(PIC_ERR_UNSUPPORTED, "d_k and d_v must be multiples of 8");
   if (d.d_k > 1024 || d.d_v > 1024 || d.n_kv_heads > 256)
     return fail(PIC_ERR_UNSUPPORTED, "head count or width too large");
+  if (is_fp4(d) && (d.kind != PIC_GQA || !fp4_width(d.d_k, d.d_v)))
+    return fail(PIC_ERR_UNSUPPORTED, "4-bit stores hold GQA caches with d_k = d_v of 64 or 128");
   pic_store *s = new (std::nothrow) pic_store();
   if (!s) return fail(PIC_ERR_OOM, "host allocation failed");
   s->desc = d;
@@ -1449,7 +1494,8 @@ pic_status pic_store_create(const pic_store_desc *desc, pic_store **out) {
   s->k_tok_elems = (int64_t)d.n_kv_heads * d.d_k;
   s->v_tok_elems = d.kind == PIC_GQA ? (int64_t)d.n_kv_heads * d.d_v : 0;
   s->n_layers = d.n_layers > 1 ? d.n_layers : 1;
-  s->layer_bytes = s->capacity * (s->k_tok_elems + s->v_tok_elems) * s->esz;
+  s->page_bytes = page_bytes(d, s->k_tok_elems, s->v_tok_elems, s->esz);
+  s->layer_bytes = s->capacity / kTile * s->page_bytes;
   s->free_runs.emplace(0, s->capacity / kTile);
   hipError_t e = hipGetDevice(&s->device);
   if (e == hipSuccess) s->shape = device_shape();
@@ -1533,6 +1579,14 @@ pic_status pic_store_put(pic_store *s, uint64_t chunk_id, int64_t n_tokens, cons
   hipError_t e = hipSuccess;
   for (const Run &r : runs) {
     const LinkEntry E = run_entry(s, r, 0);
+    if (is_fp4(d)) {
+      const int64_t at = (int64_t)r.tok0 * s->k_tok_elems;
+      const Fp4Put fp{(const uint16_t *)k + at, (const uint16_t *)v + at, (char *)E.k,
+                      n_tokens * s->k_tok_elems, s->layer_bytes, r.ntok, d.n_kv_heads};
+      e = launch_fp4_put(fp, d.d_k, s->n_layers, st);
+      if (e != hipSuccess) break;
+      continue;
+    }
     PutParams pp{};
     pp.src_k = (const char *)k + (int64_t)r.tok0 * s->k_tok_elems * s->esz;
     pp.src_v = gqa ? (const char *)v + (int64_t)r.tok0 * s->v_tok_elems * s->esz : nullptr;
@@ -1639,7 +1693,8 @@ pic_status pic_store_derive(pic_store *s, uint64_t new_id, uint64_t base_id, int
       pc.page[i] = PageCopy{(const char *)S.k, gqa ? (const char *)S.v : nullptr, (char *)D.k,
                             gqa ? (char *)D.v : nullptr, S.lp, D.lp};
     }
-    e = launch_copy_pages(pc, (int32_t)n, s->n_layers, st);
+    e = is_fp4(d) ? launch_fp4_copy_pages(pc, (int32_t)n, s->n_layers, st)
+                  : launch_copy_pages(pc, (int32_t)n, s->n_layers, st);
   }
   if (e != hipSuccess) {
     for (const Run &r : fresh) free_run(s, r.page0, r.pages);
@@ -1696,11 +1751,13 @@ pic_status pic_store_write_rows(pic_store *s, uint64_t chunk_id, int32_t layer, 
   int32_t n_views = 0, first = 0;    // views listed, first row not yet written
   auto flush = [&](int32_t end) {
     const int64_t done = first;
-    const hipError_t e = launch_write_rows(
-        views, n_views, rows + first, end - first,
-        (const char *)k + done * s->k_tok_elems * s->esz,
-        gqa ? (const char *)v + done * s->v_tok_elems * s->esz : nullptr, d.n_kv_heads, d.d_k,
-        d.d_v, s->esz, (hipStream_t)stream);
+    const char *kr = (const char *)k + done * s->k_tok_elems * s->esz;
+    const char *vr = gqa ? (const char *)v + done * s->v_tok_elems * s->esz : nullptr;
+    const hipError_t e =
+        is_fp4(d) ? launch_fp4_write_rows(views, n_views, rows + first, end - first, kr, vr,
+                                          d.n_kv_heads, d.d_k, (hipStream_t)stream)
+                  : launch_write_rows(views, n_views, rows + first, end - first, kr, vr,
+                                      d.n_kv_heads, d.d_k, d.d_v, s->esz, (hipStream_t)stream);
     first = end;
     n_views = 0;
     return e;
@@ -1851,7 +1908,8 @@ pic_status pic_store_import(const void *buf, size_t buf_bytes, pic_store **out) 
   if (h.magic != kExportMagic) return fail(PIC_ERR_INVALID, "not an exported store");
   if (h.bytes > buf_bytes || h.n_chunks < 0 || h.n_layers < 1 || h.n_layers > 256 ||
       (h.esz != 2 && h.esz != 4) || h.capacity <= 0 || h.capacity % kTile ||
-      h.layer_bytes != h.capacity * (h.k_tok_elems + h.v_tok_elems) * h.esz ||
+      (is_fp4(h.desc) && (h.desc.kind != PIC_GQA || !fp4_width(h.desc.d_k, h.desc.d_v) || h.esz != 2)) ||
+      h.layer_bytes != h.capacity / kTile * page_bytes(h.desc, h.k_tok_elems, h.v_tok_elems, h.esz) ||
       h.layer_bytes * h.n_layers > kMaxExportBytes)
     return fail(PIC_ERR_INVALID, "inconsistent exported store header");
   const int64_t pages = h.capacity / kTile;
@@ -1865,6 +1923,7 @@ pic_status pic_store_import(const void *buf, size_t buf_bytes, pic_store **out) 
   s->v_tok_elems = h.v_tok_elems;
   s->n_layers = h.n_layers;
   s->layer_bytes = h.layer_bytes;
+  s->page_bytes = h.layer_bytes / (h.capacity / kTile);
   const char *in = (const char *)buf + sizeof h, *end = (const char *)buf + h.bytes;
   for (int64_t c = 0; c < h.n_chunks; ++c) {
     ExportChunk ch;
@@ -2043,7 +2102,7 @@ pic_status pic_link_plan_create(pic_store *s, const pic_link_req *req, int32_t n
     for (int32_t l = 0; l < s->n_layers; ++l)
       for (size_t i = 0; i < nl; ++i) {
         LinkEntry E = P.links[i];
-        if (!own_link[i]) {
+        if (!own_link[i] && E.k) {
           E.k = (const char *)E.k + (int64_t)l * s->layer_bytes;
           E.v = (const char *)E.v + (int64_t)l * s->layer_bytes;
         }
@@ -2083,7 +2142,7 @@ pic_status pic_link_plan_create(pic_store *s, const pic_link_req *req, int32_t n
     for (int32_t l = 0; l < s->n_layers; ++l) {
       std::vector<LinkEntry> at(links);
       for (size_t i = 0; i < nl; ++i)
-        if (!own[i]) {
+        if (!own[i] && at[i].k) {   // (own KV read in place has no address here)
           at[i].k = (const char *)at[i].k + (int64_t)l * s->layer_bytes;
           at[i].v = (const char *)at[i].v + (int64_t)l * s->layer_bytes;
         }
@@ -2184,8 +2243,12 @@ pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_
   HIP_TRY(launch_table_copy(stage->host_dev, stage->dev, (int64_t)(sizeof(LinkEntry) * n), st),
           "table_copy_kernel");
   const pic_store_desc &d = s->desc;
-  hipError_t e = launch_gather((const LinkEntry *)stage->dev, n, toks, d.n_kv_heads,
-                               d.d_k, d.d_v, !gqa, s->esz, k_out, v_out, st);
+  int64_t tiles = 0;
+  for (const LinkEntry &E : links) tiles += (E.len + kTile - 1) / kTile;
+  hipError_t e = is_fp4(d) ? launch_fp4_gather((const LinkEntry *)stage->dev, n, (int32_t)tiles,
+                                               d.n_kv_heads, d.d_k, k_out, v_out, st)
+                           : launch_gather((const LinkEntry *)stage->dev, n, toks, d.n_kv_heads,
+                                           d.d_k, d.d_v, !gqa, s->esz, k_out, v_out, st);
   if (e != hipSuccess) return hip_fail(e, "gather_kernel");
   HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");
   stage->pending = true;
@@ -2278,6 +2341,122 @@ pic_status pic_mla_up_v(int32_t n_tokens, int32_t n_heads, const void *o_lat, co
   hipError_t e = launch_mla_up_v(o_lat, w_uv, out, n_tokens, n_heads, device_shape(),
                                  (hipStream_t)stream);
   if (e != hipSuccess) return hip_fail(e, "proj_kernel (up)");
+  return PIC_OK;
+}
+
+// Rotary positions: the description and the angle per position of each pair.
+struct pic_rope {
+  pic_rope_desc desc{};
+  double rev[kRopeMost / 2] = {};   // revolutions per position
+};
+
+pic_status pic_rope_create(const pic_rope_desc *desc, pic_rope **out) {
+  if (!desc || !out) return fail(PIC_ERR_INVALID, "desc/out is NULL");
+  *out = nullptr;
+  const pic_rope_desc &d = *desc;
+  if (d.dtype != PIC_F32 && d.dtype != PIC_BF16) return fail(PIC_ERR_INVALID, "unknown dtype %d", d.dtype);
+  if (d.layout != PIC_ROPE_HALF && d.layout != PIC_ROPE_INTERLEAVED)
+    return fail(PIC_ERR_INVALID, "unknown layout %d", d.layout);
+  if (d.rot_dim < 2 || d.rot_dim % 2 || d.rot_at < 0 || d.head_dim < 2 ||
+      d.rot_at > d.head_dim - d.rot_dim)
+    return fail(PIC_ERR_INVALID, "rot_dim must be even, at least 2, and the rotated part inside the head");
+  if (d.rot_dim > kRopeMost || d.head_dim > 768)
+    return fail(PIC_ERR_UNSUPPORTED, "rot_dim is at most %d and head_dim at most 768", kRopeMost);
+  const auto positive = [](double x) { return std::isfinite(x) && x > 0; };
+  if (!positive(d.theta)) return fail(PIC_ERR_INVALID, "theta must be positive and finite");
+  if (!positive(d.magnitude)) return fail(PIC_ERR_INVALID, "magnitude must be positive and finite");
+  if (d.scaling < PIC_ROPE_PLAIN || d.scaling > PIC_ROPE_YARN)
+    return fail(PIC_ERR_INVALID, "unknown scaling %d", d.scaling);
+  if (d.scaling != PIC_ROPE_PLAIN && !positive(d.factor))
+    return fail(PIC_ERR_INVALID, "factor must be positive and finite");
+  if (d.scaling == PIC_ROPE_BANDED && !(positive(d.original_len) && positive(d.band_low) &&
+                                        positive(d.band_high) && d.band_low < d.band_high))
+    return fail(PIC_ERR_INVALID, "banded scaling needs original_len and 0 < band_low < band_high");
+  if (d.scaling == PIC_ROPE_YARN &&
+      !(positive(d.original_len) && positive(d.turns_slow) && positive(d.turns_fast) &&
+        d.turns_slow < d.turns_fast && d.theta > 1))
+    return fail(PIC_ERR_INVALID,
+                "yarn scaling needs original_len, 0 < turns_slow < turns_fast and theta above 1");
+  pic_rope *r = new (std::nothrow) pic_rope();
+  if (!r) return fail(PIC_ERR_OOM, "host allocation failed");
+  r->desc = d;
+  const double pi2 = 6.283185307179586476925286766559;
+  const int half = d.rot_dim / 2;
+  // yarn: pair index that turns `turns` times in the original length
+  const auto at = [&](double turns) {
+    return half * std::log(d.original_len / (turns * pi2)) / std::log(d.theta);
+  };
+  double lo = 0, hi = 0;
+  if (d.scaling == PIC_ROPE_YARN) {
+    lo = std::max(std::floor(at(d.turns_fast)), 0.0);
+    hi = std::min(std::ceil(at(d.turns_slow)), d.rot_dim - 1.0);
+  }
+  for (int i = 0; i < half; ++i) {
+    const double f = std::pow(d.theta, -(double)i / half);
+    double keep = 1;               // share of the unscaled frequency
+    if (d.scaling == PIC_ROPE_LINEAR)
+      keep = 0;
+    else if (d.scaling == PIC_ROPE_BANDED)
+      keep = (d.original_len * f / pi2 - d.band_low) / (d.band_high - d.band_low);
+    else if (d.scaling == PIC_ROPE_YARN)
+      keep = 1 - (i - lo) / std::max(hi - lo, 0.001);
+    keep = std::min(1.0, std::max(0.0, keep));
+    r->rev[i] = (d.scaling == PIC_ROPE_PLAIN ? f : f * (keep + (1 - keep) / d.factor)) / pi2;
+  }
+  *out = r;
+  return PIC_OK;
+}
+
+pic_status pic_rope_destroy(pic_rope *rope) {
+  delete rope;
+  return PIC_OK;
+}
+
+pic_status pic_rope_apply(const pic_rope *rope, int32_t n_tokens, const int32_t *positions,
+                          const pic_rope_tensor *tensors, int32_t n_tensors, int32_t transposed,
+                          void *stream) {
+  if (!rope) return fail(PIC_ERR_INVALID, "rope is NULL");
+  if (n_tokens < 0) return fail(PIC_ERR_INVALID, "n_tokens must be >= 0");
+  if (n_tensors < 1 || n_tensors > kRopeTensors || !tensors)
+    return fail(PIC_ERR_INVALID, "1 to %d tensors", kRopeTensors);
+  const pic_rope_desc &d = rope->desc;
+  const int esz = d.dtype == PIC_F32 ? 4 : 2;
+  RopeParams p{};
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const pic_rope_tensor &t = tensors[i];
+    if (t.n_heads < 1 || t.n_heads > 1024)
+      return fail(PIC_ERR_INVALID, "tensor %d: n_heads must be 1..1024", i);
+    const int64_t row = (int64_t)t.n_heads * d.head_dim;
+    RopeTensor &o = p.t[i];
+    o.x = t.x;
+    o.out = t.out;
+    o.x_stride = t.x_stride ? t.x_stride : row;
+    o.out_stride = t.out_stride ? t.out_stride : row;
+    o.heads = t.n_heads;
+    if (o.x_stride < row || o.out_stride < row)
+      return fail(PIC_ERR_INVALID, "tensor %d: a token stride is below %lld elements", i, (long long)row);
+    if (n_tokens == 0) continue;
+    if (!t.x || !t.out) return fail(PIC_ERR_INVALID, "tensor %d: x/out is NULL", i);
+    if ((uintptr_t)t.x % esz || (uintptr_t)t.out % esz)
+      return fail(PIC_ERR_INVALID, "tensor %d is not aligned to its elements", i);
+    if (t.x == t.out && o.x_stride != o.out_stride)
+      return fail(PIC_ERR_INVALID, "tensor %d: in place with two strides", i);
+    p.heads += t.n_heads;
+  }
+  if (n_tokens == 0) return PIC_OK;
+  if (!positions) return fail(PIC_ERR_INVALID, "positions is NULL");
+  std::copy(rope->rev, rope->rev + d.rot_dim / 2, p.rev);
+  p.positions = positions;
+  p.n_tensors = n_tensors;
+  p.n_tokens = n_tokens;
+  p.width = d.head_dim;
+  p.rot_at = d.rot_at;
+  p.rot = d.rot_dim;
+  p.magnitude = (float)d.magnitude;
+  p.sine = (float)(transposed ? -d.magnitude : d.magnitude);
+  const hipError_t e = launch_rope(p, d.dtype, d.layout == PIC_ROPE_HALF, device_shape(),
+                                   (hipStream_t)stream);
+  if (e != hipSuccess) return hip_fail(e, "rope_kernel");
   return PIC_OK;
 }
 

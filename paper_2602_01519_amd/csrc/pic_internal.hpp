@@ -359,6 +359,26 @@ hipError_t launch_write_rows(const RowView *views, int32_t n_views, const int32_
                              const void *src_k, const void *src_v, int32_t heads, int32_t d_k,
                              int32_t d_v, int32_t esz, hipStream_t st);
 
+// The 4-bit store (see fp4.hpp): a run of pages is [page][head][tile], its
+// LinkEntry's k the first page (v and lp unused). One run of a put chunk:
+struct Fp4Put {
+  const uint16_t *k, *v;      // the run's first token, layer 0 (bf16, token-major)
+  char *dst;                  // the run's first page in layer 0
+  int64_t src_layer;          // elements from layer to layer
+  int64_t layer_bytes;
+  int32_t n_tokens, heads;
+};
+hipError_t launch_fp4_put(const Fp4Put &p, int32_t d, int32_t n_layers, hipStream_t st);
+// c: src_k / dst_k of each page, layer_bytes, heads and d_k
+hipError_t launch_fp4_copy_pages(const PageCopies &c, int32_t n, int32_t n_layers, hipStream_t st);
+// views' k: their first page; limits as for launch_write_rows
+hipError_t launch_fp4_write_rows(const RowView *views, int32_t n_views, const int32_t *rows,
+                                 int32_t n, const void *k, const void *v, int32_t heads, int32_t d,
+                                 hipStream_t st);
+// tiles: tiles of all links
+hipError_t launch_fp4_gather(const LinkEntry *links, int32_t n_links, int32_t tiles, int32_t heads,
+                             int32_t d, void *k, void *v, hipStream_t st);
+
 // Copies bytes (a multiple of 16) from a host-mapped buffer to the device.
 hipError_t launch_table_copy(const void *src, void *dst, int64_t bytes, hipStream_t st);
 
@@ -367,6 +387,27 @@ hipError_t launch_mla_absorb_q(const void *q, const void *w_uk_t, void *q_out, i
                                int32_t n_heads, const DevShape &ds, hipStream_t st);
 hipError_t launch_mla_up_v(const void *o_lat, const void *w_uv, void *out, int32_t n_tokens,
                            int32_t n_heads, const DevShape &ds, hipStream_t st);
+// Rotary positions of several tensors (see pic.h). The last block is set by
+// launch_rope.
+constexpr int kRopeTensors = 4, kRopeMost = 256;   // tensors of a call, elements rotated
+struct RopeTensor {
+  const void *x;
+  void *out;
+  int64_t x_stride, out_stride;   // elements from token to token
+  int32_t heads;
+};
+struct RopeParams {
+  double rev[kRopeMost / 2];      // revolutions per position of each pair
+  RopeTensor t[kRopeTensors];
+  const int32_t *positions;
+  int32_t n_tensors, n_tokens, heads;   // heads: of all tensors
+  int32_t width, rot_at, rot;
+  float magnitude, sine;          // factor of cos; of sin (its sign with it)
+  int32_t rot_chunks, lanes, slots, tokens, heads_per_block;
+  float inv_lanes, inv_half;
+};
+hipError_t launch_rope(RopeParams p, int dtype, bool half, const DevShape &ds, hipStream_t st);
+
 // The call's prologue: lays out the own KV of every request (token-major
 // k_self / v_self) like a chunk slot at its own link (the request's last
 // link), zero-padded to lp, in `work` (when max_own_lp > 0) and copies copy_bytes of tables from
@@ -412,6 +453,11 @@ struct StreamShape {
 StreamShape stream_shape(int dtype, int d, int max_rows, bool small);
 hipError_t launch_link_stream(const LinkParams &p, int dtype, int rows, hipStream_t st,
                               const char **name);
+
+// Link attention over a 4-bit store, d_k = d_v in {64, 128}: one wave per 16 rows
+// and piece.
+hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **name);
+int fp4_rows_per_block();
 
 // bf16 MLA (absorbed) link attention: one 576-wide latent kv head, values
 // are the first 512 entries of each latent row.

@@ -23,9 +23,11 @@ _HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__)
 _lib = None
 
 OK, ERR_INVALID, ERR_NOT_FOUND, ERR_EXISTS, ERR_OOM, ERR_HIP, ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5, -6
-F32, BF16 = 0, 1
+F32, BF16, FP4 = 0, 1, 2
 GQA, MLA = 0, 1
 PREFILL, DECODE = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDED, ROPE_YARN = 0, 1, 2, 3
 
 
 class PicError(RuntimeError):
@@ -53,6 +55,20 @@ class LinkReq(ctypes.Structure):
                 ("chunk_offsets", ctypes.c_void_p), ("chunk_ids", ctypes.c_void_p),
                 ("q_offsets", ctypes.c_void_p), ("self_offsets", ctypes.c_void_p),
                 ("chunk_starts", ctypes.c_void_p), ("q_doc_limits", ctypes.c_void_p)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rot_at", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("band_low", ctypes.c_double),
+                ("band_high", ctypes.c_double), ("turns_fast", ctypes.c_double),
+                ("turns_slow", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class RopeTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("x_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("n_heads", ctypes.c_int32)]
 
 
 def lib_path() -> str:
@@ -88,6 +104,9 @@ def lib():
             "pic_link_plan_destroy": [vp],
             "pic_mla_absorb_q": [i32, i32, vp, vp, vp, vp],
             "pic_mla_up_v": [i32, i32, vp, vp, vp, vp],
+            "pic_rope_create": [vp, vp],
+            "pic_rope_destroy": [vp],
+            "pic_rope_apply": [vp, i32, vp, vp, i32, i32, vp],
             "pic_prof_begin": [],
             "pic_prof_begin_sampled": [i32],
             "pic_prof_end": [vp, vp, vp, i32],
@@ -371,6 +390,48 @@ def mla_absorb_q(n_tokens: int, n_heads: int, q, w_uk_t, q_out, stream: Optional
 def mla_up_v(n_tokens: int, n_heads: int, o_lat, w_uv, out, stream: Optional[int] = None):
     """pic_mla_up_v: out = W_UV o_lat per head (bf16)."""
     _check(lib().pic_mla_up_v(int(n_tokens), int(n_heads), _ptr(o_lat), _ptr(w_uv), _ptr(out), stream))
+
+
+class Rope:
+    """pic_rope_*: rotary positions of one kind of heads (frequencies formed once, on the host)."""
+
+    def __init__(self, dtype: int, layout: int, head_dim: int, rot_at: int, rot_dim: int,
+                 theta: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+                 original_len: float = 0.0, band_low: float = 0.0, band_high: float = 0.0,
+                 turns_fast: float = 0.0, turns_slow: float = 0.0, magnitude: float = 1.0):
+        desc = RopeDesc(dtype, layout, head_dim, rot_at, rot_dim, scaling, theta, factor,
+                        original_len, band_low, band_high, turns_fast, turns_slow, magnitude)
+        h = ctypes.c_void_p()
+        _check(lib().pic_rope_create(ctypes.byref(desc), ctypes.byref(h)))
+        self.handle = h
+
+    def apply(self, n_tokens: int, positions, tensors, transposed: bool = False,
+              stream: Optional[int] = None):
+        """pic_rope_apply: tensors is a list of (x, out, n_heads, x_stride, out_stride), strides in
+        elements from token to token (0: dense)."""
+        if not self.handle:
+            raise PicError(ERR_INVALID, "the handle is closed")
+        arr = (RopeTensor * max(1, len(tensors)))(
+            *[RopeTensor(_ptr(x), _ptr(y), int(xs), int(ys), int(h)) for x, y, h, xs, ys in tensors])
+        _check(lib().pic_rope_apply(self.handle, int(n_tokens), _ptr(positions), arr, len(tensors),
+                                    int(bool(transposed)), stream))
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(lib().pic_rope_destroy(self.handle))
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def peak_mfma_bf16(iters: int = 4096, stream: Optional[int] = None) -> float:

@@ -1,0 +1,206 @@
+"""Rotary positions against their formulas in 64 bits.
+
+Tolerances: cos and sin are fp32 of an angle of at most half a turn that is off by at most
+2^-23 (its rounding to fp32 and the product's), plus 2 units of their own: 2^-22 each; two
+products and a sum in fp32 add 2^-23 of their size: |out - ref| <= mag (|x_a| + |x_b|) (2^-22 +
+2^-23), and for bf16 2^-8 |ref| more."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_01519_amd import pic
+
+pytestmark = pytest.mark.gpu
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def frequencies(rot, theta, scaling=pic.ROPE_PLAIN, factor=1.0, original_len=0.0, band_low=0.0,
+                band_high=0.0, turns_fast=0.0, turns_slow=0.0, **_):
+    f = np.array([theta ** (-2.0 * i / rot) for i in range(rot // 2)])
+    if scaling == pic.ROPE_LINEAR:
+        return f / factor
+    if scaling == pic.ROPE_BANDED:
+        w = np.clip((original_len * f / (2 * math.pi) - band_low) / (band_high - band_low), 0, 1)
+        return f * w + f * (1 - w) / factor
+    if scaling == pic.ROPE_YARN:
+        at = lambda n: rot * math.log(original_len / (2 * math.pi * n)) / (2 * math.log(theta))  # noqa: E731
+        lo, hi = max(math.floor(at(turns_fast)), 0), min(math.ceil(at(turns_slow)), rot - 1)
+        ramp = np.clip((np.arange(rot // 2) - lo) / max(hi - lo, 0.001), 0, 1)
+        return f * (1 - ramp) + f * ramp / factor
+    return f
+
+
+def turned(x, pos, f, mag, half, at, rot, transposed):
+    """(rotated x, what its tolerance scales with) in 64 bits."""
+    turns = pos.astype(np.float64)[:, None] * f / (2 * math.pi)
+    a = 2 * math.pi * (turns - np.rint(turns))
+    c, s = mag * np.cos(a)[:, None], mag * np.sin(a)[:, None] * (-1 if transposed else 1)
+    y, size = x.copy(), np.zeros(x.shape)
+    lo, hi = (slice(at, at + rot // 2), slice(at + rot // 2, at + rot)) if half else \
+        (slice(at, at + rot, 2), slice(at + 1, at + rot, 2))
+    y[..., lo] = c * x[..., lo] - s * x[..., hi]
+    y[..., hi] = s * x[..., lo] + c * x[..., hi]
+    size[..., lo] = size[..., hi] = mag * (np.abs(x[..., lo]) + np.abs(x[..., hi]))
+    return y, size
+
+
+def to_dev(x, dtype):
+    return torch.from_numpy(x).to(torch.float32 if dtype == pic.F32 else torch.bfloat16).cuda()
+
+
+def check(got, ref, size, dtype):
+    tol = (2.0 ** -22 + 2.0 ** -23) * size + (2.0 ** -8 * np.abs(ref) if dtype == pic.BF16 else 0)
+    over = np.abs(got.double().cpu().numpy() - ref) - tol
+    assert (over <= 0).all(), f"off its bound by {over.max()}"
+
+
+YARN = dict(scaling=pic.ROPE_YARN, factor=40.0, original_len=4096, turns_fast=32, turns_slow=1,
+            magnitude=1.3689)
+BANDED = dict(scaling=pic.ROPE_BANDED, factor=8.0, original_len=8192, band_low=1, band_high=4,
+              theta=500000.0)
+
+
+@pytest.mark.parametrize("dtype", [pic.F32, pic.BF16])
+@pytest.mark.parametrize("layout", [pic.ROPE_HALF, pic.ROPE_INTERLEAVED])
+@pytest.mark.parametrize("width,at,rot,kw", [
+    (128, 0, 128, {}), (192, 128, 64, YARN), (64, 0, 64, BANDED), (2, 0, 2, {}), (7, 1, 6, {}),
+    (90, 31, 50, dict(scaling=pic.ROPE_LINEAR, factor=3.0)), (768, 500, 256, BANDED), (33, 0, 22, YARN),
+    (768, 767 - 2, 2, {})])
+def test_shapes_and_scalings(dtype, layout, width, at, rot, kw):
+    rng = np.random.default_rng(width + rot)
+    kw = {"theta": 10000.0, **kw}
+    n, heads = 13, (3, 2)
+    pos = np.concatenate([[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 131072], rng.integers(0, 200000, n - 6)]).astype(np.int32)
+    xs = [to_dev(rng.standard_normal((n, h, width)), dtype) for h in heads]
+    outs = [torch.full_like(x, 7.0) for x in xs]
+    f = frequencies(rot, **kw)
+    with pic.Rope(dtype, layout, width, at, rot, **kw) as rope:
+        for transposed in (False, True):
+            rope.apply(n, torch.from_numpy(pos).cuda(),
+                       [(x, y, h, 0, 0) for x, y, h in zip(xs, outs, heads)], transposed, stream())
+            torch.cuda.synchronize()
+            for x, y in zip(xs, outs):
+                ref, size = turned(x.double().cpu().numpy(), pos, f, kw.get("magnitude", 1.0),
+                                   layout == pic.ROPE_HALF, at, rot, transposed)
+                check(y, ref, size, dtype)
+                part = np.ones(width, bool)
+                part[at:at + rot] = False
+                assert torch.equal(y[..., part], x[..., part])
+
+
+@pytest.mark.parametrize("dtype", [pic.F32, pic.BF16])
+@pytest.mark.parametrize("n,hq,hk", [(1, 1, 1), (1, 32, 8), (64, 32, 8), (300, 5, 3), (5000, 4, 1), (9001, 2, 2)])
+def test_fused_rows_in_place_and_not(dtype, n, hq, hk):
+    """Queries and keys as slices of one projection's rows, whose other parts stay as they are."""
+    rng = np.random.default_rng(n)
+    width, rot = 64, 48
+    x = to_dev(rng.standard_normal((n, hq + 2 * hk, width)), dtype)
+    row = (hq + 2 * hk) * width
+    pos = torch.randint(0, 100000, (n,), dtype=torch.int32, device="cuda")
+    f = frequencies(rot, 10000.0)
+    q, k = x[:, :hq], x[:, hq:hq + hk]
+    q_out = torch.empty((n, hq, width), dtype=x.dtype, device="cuda")
+    k_out = torch.full((n, hk + 1, width), 3.0, dtype=x.dtype, device="cuda")
+    with pic.Rope(dtype, pic.ROPE_HALF, width, 8, rot) as rope:
+        before = x.clone()
+        rope.apply(n, pos, [(q, q_out, hq, row, 0), (k, k_out, hk, row, (hk + 1) * width)], stream=stream())
+        torch.cuda.synchronize()
+        assert torch.equal(x, before) and bool((k_out[:, hk] == 3.0).all())
+        for a, b in ((q, q_out), (k, k_out[:, :hk])):
+            ref, size = turned(a.double().cpu().numpy(), pos.cpu().numpy(), f, 1.0, True, 8, rot, False)
+            check(b, ref, size, dtype)
+        # in place: the same bits, the rest untouched
+        rope.apply(n, pos, [(q, q, hq, row, row), (k, k, hk, row, row)], stream=stream())
+        torch.cuda.synchronize()
+        assert torch.equal(q, q_out) and torch.equal(k, k_out[:, :hk])
+        assert torch.equal(x[:, hq + hk:], before[:, hq + hk:])
+
+
+@pytest.mark.parametrize("layout", [pic.ROPE_HALF, pic.ROPE_INTERLEAVED])
+def test_transposed_is_the_gradient(layout):
+    """Against differences: the map is linear, so a difference quotient of <w, y> is exact but
+    for rounding. y is off by at most 1.5 * 2^-22 (|x_a| + |x_b|), each way."""
+    rng = np.random.default_rng(3)
+    n, h, width, rot = 5, 2, 24, 16
+    x, w = rng.standard_normal((n, h, width)), rng.standard_normal((n, h, width))
+    pos = torch.tensor([0, 3, 77, 4096, 100001], dtype=torch.int32, device="cuda")
+    with pic.Rope(pic.F32, layout, width, 4, rot, **{**YARN, "theta": 10000.0}) as rope:
+        def run(t, transposed):
+            t = to_dev(t, pic.F32)
+            out = torch.empty_like(t)
+            rope.apply(n, pos, [(t, out, h, 0, 0)], transposed, stream())
+            torch.cuda.synchronize()
+            return out.double().cpu().numpy()
+
+        grad = run(w, True)
+        base = run(x, False)
+        for e in range(width):
+            up = x.copy()
+            up[..., e] += 1.0
+            diff = ((run(up, False) - base) * w).sum(-1)
+            x32 = np.abs(up).max() + np.abs(x).max()
+            tol = width * np.abs(w).max() * 1.3689 * 4 * x32 * 2.0 ** -21
+            assert np.abs(diff - grad[..., e]).max() <= tol
+
+
+def test_captured_and_other_stream():
+    n, h = 100, 6
+    x = torch.randn(n, h, 128, device="cuda").bfloat16()
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    want, out = torch.empty_like(x), torch.empty_like(x)
+    with pic.Rope(pic.BF16, pic.ROPE_HALF, 128, 0, 128) as rope:
+        rope.apply(n, pos, [(x, want, h, 0, 0)], stream=stream())
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        rope.apply(n, pos, [(x, out, h, 0, 0)], stream=side.cuda_stream)
+        side.synchronize()
+        assert torch.equal(out, want)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            rope.apply(n, pos, [(x, out, h, 0, 0)], stream=stream())
+        for k in range(3):
+            out.fill_(k)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+
+
+def test_positions_then_4_bit_cache_then_link():
+    """The operators as they are used together: a document's keys turned at positions from zero
+    and put into a 4-bit store, a question's queries and keys turned at theirs, linked."""
+    import fp4_model as M
+    rng = np.random.default_rng(11)
+    hq, hkv, d, n, lq = 8, 2, 128, 150, 6
+    draw = lambda *s: M.bf16(rng.standard_normal(s))  # noqa: E731
+    k, v, q, ko, vo = draw(n, hkv, d), draw(n, hkv, d), draw(lq, hq, d), draw(lq, hkv, d), draw(lq, hkv, d)
+    t = {x: to_dev(y, pic.BF16) for x, y in dict(k=k, v=v, q=q, ko=ko, vo=vo).items()}
+    pos = np.arange(n + lq, dtype=np.int32)
+    dp = torch.from_numpy(pos).cuda()
+    with pic.Rope(pic.BF16, pic.ROPE_HALF, d, 0, d, **BANDED) as rope, \
+            pic.Store(pic.GQA, pic.FP4, hkv, d, d, 256) as store:
+        rope.apply(n, dp, [(t["k"], t["k"], hkv, 0, 0)], stream=stream())
+        store.put(1, n, t["k"], t["v"], stream())
+        rope.apply(lq, dp[n:], [(t["q"], t["q"], hq, 0, 0), (t["ko"], t["ko"], hkv, 0, 0)], stream=stream())
+        out = torch.empty((lq, hq, d), dtype=torch.bfloat16, device="cuda")
+        lse = torch.empty((lq, hq), device="cuda")
+        scale = float(np.float32(d ** -0.5))
+        pic.link_attn(store, [0, 1], [1], [0, lq], [0, lq], hq, t["q"], t["ko"], t["vo"], scale, out, lse,
+                      stream=stream())
+        torch.cuda.synchronize()
+    f = frequencies(d, **BANDED)
+    # the turned bf16 numbers as the GPU rounded them: within their bound, then exact inputs
+    got = {x: t[x].double().cpu().numpy() for x in ("k", "q", "ko")}
+    for x, p in (("k", pos[:n]), ("q", pos[n:]), ("ko", pos[n:])):
+        ref, size = turned(dict(k=k, q=q, ko=ko)[x], p, f, 1.0, True, 0, d, False)
+        check(t[x], ref, size, pic.BF16)
+    seen = np.ones((lq, n + lq), bool)
+    seen[:, n:] = np.tril(seen[:, n:])
+    ro, rl, to, tl = M.attend(got["q"], np.concatenate([M.stored(got["k"]), got["ko"]]),
+                              np.concatenate([M.stored(v), vo]), scale, seen)
+    assert (np.abs(out.double().cpu().numpy() - ro) <= to).all()
+    assert (np.abs(lse.double().cpu().numpy() - rl) <= tl).all()
