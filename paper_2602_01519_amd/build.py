@@ -27,6 +27,7 @@ SOURCES = [
     "kernels_mla_proj.hip",
     "kernels_fp4_store.hip",
     "kernels_fp4_decode.hip",
+    "kernels_fp4_prefill.hip",
     "kernels_rope.hip",
     "static_scratch.hip",
 ]

@@ -1,0 +1,533 @@
+// Link attention over a 4-bit chunk cache on gfx950 for calls with many rows
+// per kv head, head dims 64 and 128.
+//
+// Workgroup: 8 waves x 32 rows = 256 rows (query token x query head) of one
+// (request, kv head) over a piece of its keys, in 64-key tiles. Per tile and wave
+//   S^T[64 keys][32 rows] = K . Q^T      2 x D/16 v_mfma_f32_32x32x16_bf16
+//   O^T[D][32 rows]      += V^T . P^T    4 x D/32 of them
+// A tile is widened once per workgroup: waves 0-3 take its keys, waves 4-7 its
+// values, 1 / 8 D bytes per lane, into registers while the tile before is
+// computed, then through the scaled conversion into LDS as bf16 (K rows, V
+// transposed; 32 KB for D = 128, two buffers). Widening in every wave instead would read an
+// eighth of the LDS bytes and convert eight times as often: 128 conversions and 64
+// permutes per wave and tile beside some 130 vector instructions of the
+// softmax. The own KV is bf16 and takes the same way without the conversion,
+// straight from k_self / v_self.
+//
+// The order of the keys within a tile is free: the scores that lane (n, g) holds
+// after the first product, keys 8 a + 4 g + c, are made the 8 neighbouring
+// positions of its operand of the second one by where V's keys are written.
+//
+// Softmax: log2 domain, against the running max as it stands; a tile is redone
+// against the new one when a lane's probabilities sum to more than 2^20 (the first
+// tile of a row always is). Sums are fp32 of the probabilities before they are rounded to
+// bf16 for the product.
+#include "fp4.hpp"
+
+namespace pic {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kWaves = 8;
+constexpr int kRowsPerWave = 32;
+constexpr int kRows = kWaves * kRowsPerWave;
+constexpr float kJumpSum = 1048576.0f;
+constexpr int kQkAhead = 5;    // K-fragment read lead, in QK steps
+constexpr int kPvAhead = 8;    // V-fragment read lead, in PV MFMAs
+
+__device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float half_swap_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_swap_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// LDS tiles in 16-byte chunks, XOR-swizzled within a row so that the fragment
+// reads (16 lanes: 16 rows of K, or of V^T, at one chunk) meet no bank twice.
+//   K   [key][D/8 chunks]: D = 128: c ^ (bits 2 and 3 of key & 15 swapped);
+//       D = 64, two rows to 256 bytes: c ^ ((key >> 1) & 7)
+//   V^T [channel][8 chunks of 8 key positions]: c ^ ((x ^ x >> 3) & 7), x = channel & 31
+template <int D>
+__device__ __forceinline__ int k_slot(int key, int c) {
+  if constexpr (D == 128)
+    return key * 16 + (c ^ ((key & 3) | ((key & 8) >> 1) | ((key & 4) << 1)));
+  else
+    return key * 8 + (c ^ ((key >> 1) & 7));
+}
+__device__ __forceinline__ int v_slot(int ch, int c) {
+  const int x = ch & 31;
+  return ch * 8 + (c ^ ((x ^ (x >> 3)) & 7));
+}
+
+// A key tile: workgroup-uniform facts.
+struct TileRef {
+  const char *p;     // the tile in the cache (kv head applied)
+  int nvalid;        // valid keys
+  int j0;            // own tiles: first own key
+  int tok;           // document tiles: first row within the request's linked rows
+  int own;
+};
+
+template <int D>
+struct Ctx {
+  ReqEntry R;
+  int kvh, heads, wave, lane, n, g;
+  const_links links;
+  int li;
+  const char *base;
+  int len, tok0, tile0, end;
+  const char *ks, *vs;     // k_self / v_self, kv head applied, token 0 of the batch
+  int64_t stride;          // ... bytes per token
+
+  __device__ __forceinline__ void next_link() {
+    ++li;
+    base = (const char *)links[li].k;
+    len = links[li].len;
+    tok0 = links[li].tok0;
+    tile0 = links[li].tile0;
+    end = tile0 + (len + kTile - 1) / kTile;
+  }
+  // Tile t of the request (t only grows across calls). The own link's tok0 is its
+  // first row in k_self.
+  __device__ __forceinline__ TileRef tile(int t) {
+    while (t >= end) next_link();
+    const int tt = t - tile0;
+    TileRef r;
+    r.own = t >= R.doc_tiles;
+    r.nvalid = min(kTile, len - tt * kTile);
+    r.j0 = tt * kTile;
+    r.tok = tok0 + (r.own ? 0 : tt * kTile);
+    r.p = base + ((int64_t)tt * heads + kvh) * Fp4Tile<D>::kBytes;
+    return r;
+  }
+};
+
+// This lane's share of a cache tile, as loaded: waves 0-3 the key 16 b + m (D/4
+// elements from D/4 * g on), waves 4-7 the keys 16 b + 4 g ..+3 (D/16 channels from
+// D/16 * m on).
+template <int D>
+struct Share {
+  uint32_t x[D / 32];
+  uint32_t scale;
+};
+
+// Keys: wave b, lane (g, m). Values: lane (m', 4 b + g), m = 4 wave + m', so that
+// sixteen lanes write one whole row of V^T.
+struct Place {
+  bool value;
+  int b, g, m;
+};
+template <int D>
+__device__ __forceinline__ Place place(const Ctx<D> &c, int lane) {
+  const int w = c.wave & 3, lo = lane & 15, hi = lane >> 4;
+  const bool value = c.wave >= 4;
+  return Place{value, value ? lo >> 2 : w, value ? lo & 3 : hi, value ? 4 * w + hi : lo};
+}
+
+template <int D>
+__device__ __forceinline__ void fetch(const Ctx<D> &c, const TileRef &r, Share<D> &s) {
+  typedef Fp4Tile<D> T;
+  if (r.own) return;            // loaded where it is written (see widen)
+  const Place l = place(c, c.lane);
+  const char *p = r.p + (l.value ? T::kV : 0);
+  if constexpr (D == 128) {
+    const uint4 u = *(const uint4 *)(p + (l.b * 64 + l.g * 16 + l.m) * 16);
+    s.x[0] = u.x, s.x[1] = u.y, s.x[2] = u.z, s.x[3] = u.w;
+  } else {
+    const uint2 u = *(const uint2 *)(p + ((l.b >> 1) * 64 + l.g * 16 + l.m) * 16 + (l.b & 1) * 8);
+    s.x[0] = u.x, s.x[1] = u.y;
+  }
+  if (l.value)
+    s.scale = *(const uint32_t *)(r.p + T::v_scale(16 * l.b + 4 * l.g, l.m * (D / 16) / 32));
+  else
+    s.scale = *(const uint8_t *)(r.p + T::k_scale(16 * l.b + l.m, l.g * (D / 4) / 32));
+}
+
+// Pairs of channels (2 kC, 2 kC + 1) of four keys into V^T as four keys of each.
+template <int D, int kC>
+__device__ __forceinline__ void put_pair(const Place &l, uint4 *vt, const uint32_t (&d)[4]) {
+  const int ch = l.m * (D / 16) + 2 * kC, chunk = 2 * l.b + (l.g & 1), half = l.g >> 1;
+  ((uint2 *)vt)[v_slot(ch, chunk) * 2 + half] =
+      make_uint2(__builtin_amdgcn_perm(d[1], d[0], 0x05040100u),
+                 __builtin_amdgcn_perm(d[3], d[2], 0x05040100u));
+  ((uint2 *)vt)[v_slot(ch + 1, chunk) * 2 + half] =
+      make_uint2(__builtin_amdgcn_perm(d[1], d[0], 0x07060302u),
+                 __builtin_amdgcn_perm(d[3], d[2], 0x07060302u));
+}
+
+template <int D, int kC>
+__device__ __forceinline__ void widen_pair(const Place &l, const Share<D> &s, const float (&sc)[4],
+                                           uint4 *vt) {
+  uint32_t d[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (D == 128)
+      d[i] = fp4_pair<kC>(s.x[i], sc[i]);
+    else
+      d[i] = (i & 1) ? fp4_pair<2 + (kC & 1)>(s.x[i >> 1], sc[i]) : fp4_pair<kC & 1>(s.x[i >> 1], sc[i]);
+  }
+  put_pair<D, kC>(l, vt, d);
+}
+
+// An own tile, from k_self / v_self straight to LDS. (Loaded a tile ahead as the
+// cache's tiles are, it would hold 16 registers over the whole tile, more than
+// there are; a request has few own tiles.) Keys past the last own one: the last
+// key again, and zeros for values (their probability is 0, and 0 times an
+// infinity would be a NaN).
+template <int D>
+__device__ __forceinline__ void stage_own(const Ctx<D> &c, const TileRef &r, uint4 *kt, uint4 *vt) {
+  // (the lane made opaque: addresses formed from it here stay here and take no
+  // register in the loop over the tiles)
+  int lane = c.lane;
+  asm volatile("" : "+v"(lane));
+  const Place l = place(c, lane);
+  const char *kv = (l.value ? c.vs : c.ks) + ((int64_t)r.tok + r.j0) * c.stride;
+  if (!l.value) {
+    const int key = 16 * l.b + l.m;
+    const char *p = kv + min(key, r.nvalid - 1) * c.stride + l.g * (D / 2);
+    uint4 x[D / 32];
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) x[j] = *(const uint4 *)(p + 16 * j);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) kt[k_slot<D>(key, l.g * (D / 32) + j)] = x[j];
+    return;
+  }
+  uint32_t x[D / 32][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int key = 16 * l.b + 4 * l.g + i;
+    const char *p = kv + min(key, r.nvalid - 1) * c.stride + l.m * (D / 8);
+    const uint32_t keep = key < r.nvalid ? ~0u : 0u;
+#pragma unroll
+    for (int j = 0; j < D / 32; j += 2) {
+      const uint2 u = *(const uint2 *)(p + 4 * j);
+      x[j][i] = u.x & keep;
+      x[j + 1][i] = u.y & keep;
+    }
+  }
+  put_pair<D, 0>(l, vt, x[0]);
+  put_pair<D, 1>(l, vt, x[1]);
+  if constexpr (D == 128) {
+    put_pair<D, 2>(l, vt, x[2]);
+    put_pair<D, 3>(l, vt, x[3]);
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void widen(const Ctx<D> &c, const TileRef &r, const Share<D> &s, uint4 *kt,
+                                      uint4 *vt) {
+  if (r.own) {
+    stage_own(c, r, kt, vt);
+    return;
+  }
+  const Place l = place(c, c.lane);
+  if (!l.value) {
+    const float sc = fp4_scale(s.scale);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+      kt[k_slot<D>(16 * l.b + l.m, l.g * (D / 32) + j)] = fp4_decode8(s.x[j], sc);
+    return;
+  }
+  float sc[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sc[i] = fp4_scale((s.scale >> (8 * i)) & 255u);
+  widen_pair<D, 0>(l, s, sc, vt);
+  widen_pair<D, 1>(l, s, sc, vt);
+  if constexpr (D == 128) {
+    widen_pair<D, 2>(l, s, sc, vt);
+    widen_pair<D, 3>(l, s, sc, vt);
+  }
+}
+
+template <int D>
+struct Acc {
+  f32x16 o[D / 32];
+  float m, l;      // running max in use (log2 domain); this lane half's part of the sum
+};
+
+// Per-row limit on the visible linked rows, and its minimum over the wave.
+struct DocLim {
+  int dl, wmin;
+};
+
+template <int D, bool kLim>
+__device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, const uint4 *vt,
+                                             const bf16x8 (&qf)[D / 16], Acc<D> &a, const TileRef &r,
+                                             int own_last, const DocLim &dlm, float sc) {
+  f32x16 s0, s1;
+#pragma unroll
+  for (int x = 0; x < 16; ++x) {
+    s0[x] = 0.f;
+    s1[x] = 0.f;
+  }
+  constexpr int kSteps = D / 16, kAhead = kQkAhead < kSteps ? kQkAhead : kSteps;
+  bf16x8 ka[kSteps], kb[kSteps];
+#pragma unroll
+  for (int st = 0; st < kAhead; ++st) {
+    ka[st] = as_bf16x8(kt[k_slot<D>(c.n, st * 2 + c.g)]);
+    kb[st] = as_bf16x8(kt[k_slot<D>(32 + c.n, st * 2 + c.g)]);
+  }
+#pragma unroll
+  for (int st = 0; st < kSteps; ++st) {
+    if (st + kAhead < kSteps) {
+      ka[st + kAhead] = as_bf16x8(kt[k_slot<D>(c.n, (st + kAhead) * 2 + c.g)]);
+      kb[st + kAhead] = as_bf16x8(kt[k_slot<D>(32 + c.n, (st + kAhead) * 2 + c.g)]);
+    }
+    s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[st], qf[st], s0, 0, 0, 0);
+    s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[st], qf[st], s1, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // s0[x] / s1[x]: key 8 (x >> 2) + 4 g + (x & 3) (+ 32)
+  if (r.own || r.nvalid < kTile || (kLim && r.tok + kTile > dlm.wmin)) {
+    const int kl = (r.own   ? min(own_last - r.j0, r.nvalid - 1)
+                    : kLim ? min(dlm.dl - r.tok, r.nvalid) - 1
+                           : r.nvalid - 1) -
+                   c.g * 4;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const int key = 8 * (x >> 2) + (x & 3);
+      if (key > kl) s0[x] = -INFINITY;
+      if (key + 32 > kl) s1[x] = -INFINITY;
+    }
+  }
+  bf16x8 pf[4];
+  auto probs = [&]() {
+    const float neg_m = a.m == -INFINITY ? 0.f : -a.m;
+    float t0 = 0.f, t1 = 0.f;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[x], sc, neg_m));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s1[x], sc, neg_m));
+      t0 += p0;
+      t1 += p1;
+      pf[x >> 3][x & 7] = (__bf16)p0;
+      pf[2 + (x >> 3)][x & 7] = (__bf16)p1;
+    }
+    return t0 + t1;
+  };
+  float ts = probs();
+  if (__builtin_expect(__any(!(ts <= kJumpSum) || (a.m == -INFINITY && ts > 0.f)), 0)) {
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) tmax = fmaxf(fmaxf(tmax, s0[x]), s1[x]);
+    tmax = half_swap_max(tmax);
+    const float mnew = fmaxf(a.m, tmax * sc);
+    const float alpha = mnew == a.m ? 1.f : __builtin_amdgcn_exp2f(a.m - mnew);
+    a.m = mnew;
+    a.l *= alpha;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) a.o[d][x] *= alpha;
+    ts = probs();
+  }
+  a.l += ts;
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      const bf16x8 vf = as_bf16x8(vt[v_slot(d * 32 + c.n, ks * 2 + c.g)]);
+      a.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ks], a.o[d], 0, 0, 0);
+    }
+  // V reads run kPvAhead MFMAs ahead
+  constexpr int kPv = D / 8, kVAhead = kPvAhead < kPv ? kPvAhead : kPv;
+  __builtin_amdgcn_sched_group_barrier(0x100, kVAhead, 0);
+#pragma unroll
+  for (int i = 0; i < kPv; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (i + kVAhead < kPv) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+}
+
+// The tile after the last one of the item that holds a linked row below the
+// farthest limit of query tokens tok_lo .. tok_hi, at most t_end.
+__device__ __forceinline__ int limit_end(const LinkParams &p, const WorkItem &it, int tok_lo,
+                                         int tok_hi, int lane, int t_end) {
+  int far = 0;
+  for (int t = tok_lo + lane; t <= tok_hi; t += 64) far = max(far, p.doc_lim[t]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) far = max(far, __shfl_xor(far, o));
+  far = uni(far);
+  const const_links links = (const_links)p.links + it.link;
+  int li = 0, tok0 = it.tok0, len = it.len, tile0 = it.tile0;
+  while (far > tok0 + len && tile0 + (len + kTile - 1) / kTile < t_end) {
+    ++li;
+    tok0 = links[li].tok0;
+    len = links[li].len;
+    tile0 = links[li].tile0;
+  }
+  return min(t_end, tile0 + (max(0, min(far - tok0, len)) + kTile - 1) / kTile);
+}
+
+template <int D, bool kLim>
+__global__ __launch_bounds__(kWaves * 64, 2) void link_fp4_prefill_kernel(LinkParams p) {
+  __shared__ uint4 sk0[kTile * D / 8], sk1[kTile * D / 8], sv0[kTile * D / 8], sv1[kTile * D / 8];
+  Ctx<D> c;
+  c.lane = threadIdx.x & 63;
+  c.wave = uni(threadIdx.x >> 6);
+  c.n = c.lane & 31;
+  c.g = c.lane >> 5;
+  const int units = p.n_items * p.n_kv_heads;
+  const UnitBlock ub = unit_of_block(blockIdx.x, p.nrb, p.n_xcd, p.spread, units);
+  const int rb = ub.rb;
+  if (ub.u >= units) return;
+  const WorkItem it = load_item(p.items, ub.u / p.n_kv_heads);
+  c.heads = p.n_kv_heads;
+  c.kvh = ub.u % p.n_kv_heads;
+  c.R = item_request(it);
+  const ReqEntry &R = c.R;
+  const int group = p.group;
+  const int nrows = R.lq * group;
+  const int row0 = rb * kRows;
+  if (row0 >= nrows) return;
+  const int vis = visible_tiles(R, min(nrows - 1, row0 + kRows - 1) / group);
+  const int t_begin = it.t_begin;
+  int t_end = min(it.t_end, vis);
+  if (kLim && R.ls == 0 && t_begin < t_end)
+    t_end = limit_end(p, it, R.q0 + row0 / group, R.q0 + min(nrows - 1, row0 + kRows - 1) / group,
+                      c.lane, t_end);
+
+  // this lane's row; a wave without rows only widens its share of every tile
+  const bool active = row0 + c.wave * kRowsPerWave < nrows;
+  const int row = row0 + c.wave * kRowsPerWave + c.n;
+  const bool rvalid = row < nrows;
+  const int qi = rvalid ? row / group : 0;
+  const int qh = c.kvh * group + (rvalid ? row % group : 0);
+  const int own_last = rvalid ? qi + R.ls - R.lq : -1;
+  const int64_t orow = (int64_t)(R.q0 + qi) * p.n_q_heads + qh;
+  DocLim dlm{kNoLimit, kNoLimit};
+  if (kLim) {
+    if (rvalid) dlm.dl = p.doc_lim[R.q0 + qi];
+    int w = dlm.dl;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) w = min(w, __shfl_xor(w, o));
+    dlm.wmin = uni(w);
+  }
+  c.links = (const_links)p.links + it.link;
+  c.li = 0;
+  c.base = (const char *)it.k;
+  c.len = it.len;
+  c.tok0 = it.tok0;
+  c.tile0 = it.tile0;
+  c.end = it.tile0 + (it.len + kTile - 1) / kTile;
+  c.stride = (int64_t)p.n_kv_heads * D * 2;
+  c.ks = (const char *)p.k_self + c.kvh * D * 2;
+  c.vs = (const char *)p.v_self + c.kvh * D * 2;
+
+  TileRef ref0{}, ref1{};
+  Share<D> sh{};
+  if (t_begin < t_end) {
+    ref0 = c.tile(t_begin);
+    fetch(c, ref0, sh);
+  }
+  bf16x8 qf[D / 16];
+  {
+    const uint4 *qrow = (const uint4 *)((const uint16_t *)p.q + orow * D);
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (rvalid) v = qrow[s * 2 + c.g];
+      qf[s] = as_bf16x8(v);
+    }
+  }
+  Acc<D> a;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) a.o[d][x] = 0.f;
+  a.m = -INFINITY;
+  a.l = 0.f;
+  const float sc = p.scale_log2;
+
+  if (t_begin < t_end) {
+    widen(c, ref0, sh, sk0, sv0);
+    __syncthreads();
+  }
+  // Tile t is computed from one buffer pair while tile t + 1 is loaded into
+  // registers and then widened into the other (past the last tile: the last one
+  // again, into the buffers nobody reads); unrolled by two so that every access
+  // names its buffers.
+  for (int t = t_begin; t < t_end; t += 2) {
+    ref1 = t + 1 < t_end ? c.tile(t + 1) : ref0;
+    fetch(c, ref1, sh);
+    if (active) compute_tile<D, kLim>(c, sk0, sv0, qf, a, ref0, own_last, dlm, sc);
+    widen(c, ref1, sh, sk1, sv1);
+    __syncthreads();
+    if (t + 1 >= t_end) break;
+    ref0 = t + 2 < t_end ? c.tile(t + 2) : ref1;
+    fetch(c, ref0, sh);
+    if (active) compute_tile<D, kLim>(c, sk1, sv1, qf, a, ref1, own_last, dlm, sc);
+    widen(c, ref0, sh, sk0, sv0);
+    __syncthreads();
+  }
+
+  // ---- epilogue: O^T[dv][row], dv = 32 d + 8 (x >> 2) + 4 g + (x & 3)
+  const float ltot = half_swap_sum(a.l);
+  const int nvalid = min(kRowsPerWave, nrows - (row0 + c.wave * kRowsPerWave));
+  if (nvalid <= 0) return;
+  const float inv = ltot > 0.f ? 1.f / ltot : 0.f;
+  const int64_t prow = it.part + (orow - (int64_t)R.q0 * p.n_q_heads);
+  if constexpr (D == 128) {
+    typedef __attribute__((address_space(3))) void *lds_ptr;
+    const int bi = c.wave & 3;
+    const lds_ptr buf = bi == 0 ? (lds_ptr)sk0 : bi == 1 ? (lds_ptr)sk1 : bi == 2 ? (lds_ptr)sv0 : (lds_ptr)sv1;
+    const lds_units sb =
+        (lds_units)(uintptr_t)((uint32_t)(uintptr_t)buf + (c.wave >> 2) * kStoreBytes);
+    if (it.part < 0)
+      store_block_bf16(a.o[0], a.o[1], a.o[2], a.o[3], inv, sb, c.lane, nvalid, (int)orow,
+                       (uint16_t *)p.out, D);
+    else if (!p.skip_empty || __any(!(ltot == 0.f)))
+      store_block_f32(a.o[0], a.o[1], a.o[2], a.o[3], sb, c.lane, nvalid, (int)prow, p.part_o, D);
+  } else if (rvalid) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int dv = 32 * d + 8 * j + 4 * c.g;
+        if (it.part < 0) {
+          bf16x4v v;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = (__bf16)(a.o[d][4 * j + x] * inv);
+          *(uint2 *)((uint16_t *)p.out + orow * D + dv) = __builtin_bit_cast(uint2, v);
+        } else {
+          *(float4 *)(p.part_o + prow * D + dv) =
+              make_float4(a.o[d][4 * j], a.o[d][4 * j + 1], a.o[d][4 * j + 2], a.o[d][4 * j + 3]);
+        }
+      }
+  }
+  if (!rvalid || c.g != 0) return;
+  if (it.part < 0) {
+    if (p.lse) p.lse[orow] = ltot == 0.f ? -INFINITY : log_sum(a.m, ltot);
+  } else {
+    p.part_m[prow] = partial_max(a.m, ltot);
+    p.part_l[prow] = ltot;
+  }
+}
+
+template <int D>
+hipError_t launch(const LinkParams &p, hipStream_t st) {
+  const int64_t units = (int64_t)p.n_items * p.n_kv_heads;
+  const dim3 grid((unsigned)unit_blocks(units, p.nrb, p.n_xcd, p.spread)), block(kWaves * 64);
+  if (p.doc_lim)
+    hipLaunchKernelGGL((link_fp4_prefill_kernel<D, true>), grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL((link_fp4_prefill_kernel<D, false>), grid, block, 0, st, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int fp4_prefill_rows_per_block() { return kRows; }
+
+hipError_t launch_link_fp4_prefill(const LinkParams &p, hipStream_t st, const char **name) {
+  *name = "link_fp4_prefill_kernel";
+  return p.d_k == 128 ? launch<128>(p, st) : launch<64>(p, st);
+}
+
+}  // namespace pic

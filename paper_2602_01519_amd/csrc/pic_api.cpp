@@ -606,7 +606,7 @@ void prof_stop(hipStream_t st, std::pair<hipEvent_t, hipEvent_t> *ev, const char
 }
 
 enum class Mode { Prefill, Decode };
-enum class Kern { Valu, Mfma128, Decode128, Mla, Stream, Fp4 };
+enum class Kern { Valu, Mfma128, Decode128, Mla, Stream, Fp4, Fp4Prefill };
 
 // Everything about a call that does not depend on its tensors: the resolved
 // tables, the kernel, the split count and the workspace layout
@@ -933,6 +933,9 @@ bool small_tables(const Plan &P) {
 // gains; fp32 gains or loses with how its split count falls.
 constexpr int kStreamSmallRows = 128;
 
+// Most rows per kv head that the one-wave kernel takes.
+constexpr int kFp4FewRows = 64;
+
 // Costs of a kernel's pieces in its tiles (see choose_splits). Tile times on
 // a full GPU: d128 1.75 us per workgroup (64 keys), MLA 2.0 us (64 keys),
 // decode 5 us per wave (32 keys, eight waves per CU on the HBM stream),
@@ -964,6 +967,11 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     c.slots = 8 * (int64_t)cus;
     c.over = 2;
     c.min_piece = 1;
+  } else if (kern == Kern::Fp4Prefill) {
+    us = d.d_k == 128 ? 1.9 : 1.2;
+    c.slots = cus;
+    c.over = 3;
+    c.min_piece = 4;
   } else if (kern == Kern::Fp4) {
     us = 5.0;
     c.slots = 8 * (int64_t)cus;
@@ -1044,7 +1052,8 @@ void apply_splits(pic_store *s, int32_t n_q_heads, int rows_per_block, Setup &C)
   // last row blocks start first, the empty ones fill in at the end (dispatched
   // among the others, they delayed the start of some: S = 4 pieces 54 us, 3
   // pieces 43 us).
-  if (C.kern == Kern::Mfma128 && lp.skip_empty && lp.nrb > 1) lp.spread = 2;
+  if ((C.kern == Kern::Mfma128 || C.kern == Kern::Fp4Prefill) && !P.doc_lim.empty() && lp.nrb > 1)
+    lp.spread = 2;
   C.part_rows = 0;
   C.comb.clear();
   if (C.splits > 1) {
@@ -1058,7 +1067,7 @@ void apply_splits(pic_store *s, int32_t n_q_heads, int rows_per_block, Setup &C)
     std::stable_sort(P.order.begin(), P.order.end(), [&](int32_t a, int32_t b) {
       return (int64_t)P.reqs[a].tiles * C.req_splits[b] > (int64_t)P.reqs[b].tiles * C.req_splits[a];
     });
-  } else if (C.kern == Kern::Mfma128 && !lp.spread) {
+  } else if ((C.kern == Kern::Mfma128 || C.kern == Kern::Fp4Prefill) && !lp.spread) {
     balance_order_d128(s, P, lp, rows_per_block,
                        s->shape.cus / s->shape.xcds * mfma_d128_blocks_per_cu());
   }
@@ -1094,6 +1103,7 @@ size_t noalloc_charge(const pic_store *s, const Setup &C, int32_t num_splits) {
   const Plan &P = C.P;
   const pic_store_desc &d = s->desc;
   const int block = C.kern == Kern::Mfma128 ? mfma_d128_rows_per_block()
+                    : C.kern == Kern::Fp4Prefill ? fp4_prefill_rows_per_block()
                     : C.kern == Kern::Mla   ? mla_rows_per_block()
                                             : 16;
   int64_t splits = num_splits;
@@ -1159,7 +1169,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   // per-row masks of the flash kernel
   if (kern == Kern::Decode128 && !P.doc_lim.empty()) kern = Kern::Mfma128;
   if (d.dtype == PIC_BF16 && mla && d.d_k == 576 && d.d_v == 512) kern = Kern::Mla;
-  if (fp4) kern = Kern::Fp4;
+  if (fp4) kern = P.max_rows <= kFp4FewRows ? Kern::Fp4 : Kern::Fp4Prefill;
   // A small generic call of a shape the lean kernel is built for (tables as
   // a kernel argument, at most kLeanTiles tiles in all) runs it; other fp32
   // and narrow bf16 GQA calls stream their keys through the matrix cores.
@@ -1187,6 +1197,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
                              : kern == Kern::Valu  ? valu_rows_per_block()
                              : kern == Kern::Mla   ? mla_rows_per_block()
                              : kern == Kern::Fp4   ? fp4_rows_per_block()
+                             : kern == Kern::Fp4Prefill ? fp4_prefill_rows_per_block()
                                                    : decode_d128_max_rows();
   C.rows_per_block = rows_per_block;
   lp.nrb = std::max(1, (P.max_rows + rows_per_block - 1) / rows_per_block);
@@ -1210,12 +1221,15 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
       uneven_rows |= blocks[r] != d.n_kv_heads * lp.nrb;
       // d128 row blocks end at the farthest limit of their rows: count the
       // part of the tiles they walk
-      if (kern == Kern::Mfma128 && !P.doc_lim.empty() && R.ls == 0 && R.nlinks > 0) {
+      if ((kern == Kern::Mfma128 || kern == Kern::Fp4Prefill) && !P.doc_lim.empty() && R.ls == 0 &&
+          R.nlinks > 0) {
         const LinkEntry &last = P.links[R.link0 + R.nlinks - 1];
         share[r] = limit_share(P, R, lp.group, rows_per_block, last.tok0 + last.len);
       }
     }
-    lp.skip_empty = kern == Kern::Mfma128 && !P.doc_lim.empty();
+    // (the combine of 64-wide rows reads every partial)
+    lp.skip_empty = (kern == Kern::Mfma128 || (kern == Kern::Fp4Prefill && d.d_v == 128)) &&
+                    !P.doc_lim.empty();
     const bool given = mode == Mode::Decode && num_splits > 0;
     if (given)
       C.req_splits.assign(B, num_splits);
@@ -1317,6 +1331,8 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
     e = launch_link_stream(lp, d.dtype, C.stream_rows, st, &name);
   else if (C.kern == Kern::Fp4)
     e = launch_link_fp4(lp, st, &name);
+  else if (C.kern == Kern::Fp4Prefill)
+    e = launch_link_fp4_prefill(lp, st, &name);
   else
     e = launch_link_valu(lp, d.dtype, mla, st, &name);
   prof_stop(st, &ev, name);

@@ -455,9 +455,11 @@ hipError_t launch_link_stream(const LinkParams &p, int dtype, int rows, hipStrea
                               const char **name);
 
 // Link attention over a 4-bit store, d_k = d_v in {64, 128}: one wave per 16 rows
-// and piece.
+// and piece, or 256 rows per workgroup.
 hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **name);
 int fp4_rows_per_block();
+hipError_t launch_link_fp4_prefill(const LinkParams &p, hipStream_t st, const char **name);
+int fp4_prefill_rows_per_block();
 
 // bf16 MLA (absorbed) link attention: one 576-wide latent kv head, values
 // are the first 512 entries of each latent row.
