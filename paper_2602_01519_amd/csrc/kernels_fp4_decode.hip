@@ -33,7 +33,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(1))) const u32x4 *global_u32x4;
 
-constexpr int kRows = 16;
 constexpr int kWaves = 4;
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
@@ -139,88 +138,107 @@ struct OwnTile {
   }
 };
 
-template <int D>
+// NB: blocks of 16 rows that a wave takes.
+template <int D, int NB>
 struct State {
-  f32x4 o[D / 16];  // channel block cb: channels D/16 * (4 g + i) + cb of row n
-  float m, l;       // running max (log2 domain, per row) and this lane's part of the sum
+  f32x4 o[NB][D / 16];   // channel block cb: channels D/16 * (4 g + i) + cb of row n
+  float m[NB], l[NB];    // running max (log2 domain, per row) and this lane's part of the sum
 };
 
-template <int D, int kC, class Tile>
-__device__ __forceinline__ void value_pair(const Tile &x, int t, bf16x8 pf, State<D> &st) {
-  uint4 lo, hi;
+template <int D, int NB, int kC, class Tile>
+__device__ __forceinline__ void value_pair(const Tile &x, int t, const bf16x8 (&pf)[NB],
+                                           State<D, NB> &st) {
   uint32_t d[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     d[i] = x.template value<kC>(2 * t, i);
     d[4 + i] = x.template value<kC>(2 * t + 1, i);
   }
-  lo = make_uint4(__builtin_amdgcn_perm(d[1], d[0], 0x05040100u),
-                  __builtin_amdgcn_perm(d[3], d[2], 0x05040100u),
-                  __builtin_amdgcn_perm(d[5], d[4], 0x05040100u),
-                  __builtin_amdgcn_perm(d[7], d[6], 0x05040100u));
-  hi = make_uint4(__builtin_amdgcn_perm(d[1], d[0], 0x07060302u),
-                  __builtin_amdgcn_perm(d[3], d[2], 0x07060302u),
-                  __builtin_amdgcn_perm(d[5], d[4], 0x07060302u),
-                  __builtin_amdgcn_perm(d[7], d[6], 0x07060302u));
-  st.o[2 * kC] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(lo), pf, st.o[2 * kC], 0, 0, 0);
-  st.o[2 * kC + 1] =
-      __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(hi), pf, st.o[2 * kC + 1], 0, 0, 0);
+  const uint4 lo = make_uint4(__builtin_amdgcn_perm(d[1], d[0], 0x05040100u),
+                              __builtin_amdgcn_perm(d[3], d[2], 0x05040100u),
+                              __builtin_amdgcn_perm(d[5], d[4], 0x05040100u),
+                              __builtin_amdgcn_perm(d[7], d[6], 0x05040100u));
+  const uint4 hi = make_uint4(__builtin_amdgcn_perm(d[1], d[0], 0x07060302u),
+                              __builtin_amdgcn_perm(d[3], d[2], 0x07060302u),
+                              __builtin_amdgcn_perm(d[5], d[4], 0x07060302u),
+                              __builtin_amdgcn_perm(d[7], d[6], 0x07060302u));
+#pragma unroll
+  for (int r = 0; r < NB; ++r) {
+    st.o[r][2 * kC] =
+        __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(lo), pf[r], st.o[r][2 * kC], 0, 0, 0);
+    st.o[r][2 * kC + 1] =
+        __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(hi), pf[r], st.o[r][2 * kC + 1], 0, 0, 0);
+  }
 }
 
-// kl: last visible key of the tile for this lane's row (relative to the tile),
+// kl: last visible key of the tile for this lane's rows (relative to the tile),
 // used where masked.
-template <int D, class Tile>
-__device__ __forceinline__ void compute_tile(const Tile &x, const bf16x8 (&qf)[D / 32],
-                                             State<D> &st, int lane, bool masked, int kl,
-                                             float sc) {
+template <int D, int NB, class Tile>
+__device__ __forceinline__ void compute_tile(const Tile &x, const bf16x8 (&qf)[NB][D / 32],
+                                             State<D, NB> &st, int lane, bool masked,
+                                             const int (&kl)[NB], float sc) {
   constexpr int kB = Tile::kKeyBlocks;
-  f32x4 s[kB];
+  f32x4 s[NB][kB];
 #pragma unroll
   for (int b = 0; b < kB; ++b) {
-    s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-      s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.key(b, j), qf[j], s[b], 0, 0, 0);
+    for (int r = 0; r < NB; ++r) s[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      const bf16x8 k = x.key(b, j);
+#pragma unroll
+      for (int r = 0; r < NB; ++r)
+        s[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[r][j], s[r][b], 0, 0, 0);
+    }
   }
   if (masked) {
-    const int k0 = kl - 4 * (lane >> 4);
+#pragma unroll
+    for (int r = 0; r < NB; ++r) {
+      const int k0 = kl[r] - 4 * (lane >> 4);
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * b + i > k0) s[r][b][i] = -INFINITY;
+    }
+  }
+  float neg_m[NB];
+#pragma unroll
+  for (int r = 0; r < NB; ++r) {
+    float tmax = -INFINITY;
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (16 * b + i > k0) s[b][i] = -INFINITY;
+      for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, s[r][b][i]);
+    tmax = row_max(tmax);
+    const float mnew = fmaxf(st.m[r], tmax * sc);
+    if (mnew > st.m[r]) {        // per lane: rescale this row's state
+      const float alpha = __builtin_amdgcn_exp2f(st.m[r] - mnew);   // 0 when m = -inf
+      st.l[r] *= alpha;
+#pragma unroll
+      for (int b = 0; b < D / 16; ++b) st.o[r][b] *= alpha;
+      st.m[r] = mnew;
+    }
+    neg_m[r] = st.m[r] == -INFINITY ? 0.f : -st.m[r];
   }
-  float tmax = -INFINITY;
-#pragma unroll
-  for (int b = 0; b < kB; ++b)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, s[b][i]);
-  tmax = row_max(tmax);
-  const float mnew = fmaxf(st.m, tmax * sc);
-  if (mnew > st.m) {             // per lane: rescale this row's state
-    const float alpha = __builtin_amdgcn_exp2f(st.m - mnew);   // 0 when st.m = -inf
-    st.l *= alpha;
-#pragma unroll
-    for (int b = 0; b < D / 16; ++b) st.o[b] *= alpha;
-    st.m = mnew;
-  }
-  const float neg_m = st.m == -INFINITY ? 0.f : -st.m;
 #pragma unroll
   for (int t = 0; t < kB / 2; ++t) {
-    bf16x8 pf;
+    bf16x8 pf[NB];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * t][i], sc, neg_m));
-      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * t + 1][i], sc, neg_m));
-      st.l += p0 + p1;
-      pf[i] = (__bf16)p0;
-      pf[4 + i] = (__bf16)p1;
-    }
-    value_pair<D, 0>(x, t, pf, st);
-    value_pair<D, 1>(x, t, pf, st);
+    for (int r = 0; r < NB; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][2 * t][i], sc, neg_m[r]));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][2 * t + 1][i], sc, neg_m[r]));
+        st.l[r] += p0 + p1;
+        pf[r][i] = (__bf16)p0;
+        pf[r][4 + i] = (__bf16)p1;
+      }
+    value_pair<D, NB, 0>(x, t, pf, st);
+    value_pair<D, NB, 1>(x, t, pf, st);
     if constexpr (D == 128) {
-      value_pair<D, 2>(x, t, pf, st);
-      value_pair<D, 3>(x, t, pf, st);
+      value_pair<D, NB, 2>(x, t, pf, st);
+      value_pair<D, NB, 3>(x, t, pf, st);
     }
   }
 }
@@ -246,33 +264,42 @@ struct TileInfo {
 };
 
 // kLim: rows see different numbers of linked rows.
-template <int D, bool kLim>
+template <int D, bool kLim, int NB>
 __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t u = (int64_t)blockIdx.x * kWaves + wave;
-  const int64_t units = (int64_t)p.n_items * p.n_kv_heads;
-  const int rb = (int)(u / units);
-  if (rb >= p.nrb) return;
-  const int kvh = (int)(u % p.n_kv_heads);
-  const WorkItem it = load_item(p.items, (int)(u % units / p.n_kv_heads));
+  // Row blocks of a unit (item, kv head) are neighbours: they read the same tiles at
+  // about the same time, mostly from one workgroup. (Workgroups of as many waves as a
+  // unit has row blocks leave SIMDs idle: two of two waves each share two of the
+  // four; 16 requests of 64 rows, 51 -> 40 us.)
+  const int w = blockIdx.x * kWaves + wave, u = w / p.nrb, rb = w % p.nrb;
+  if (u >= p.n_items * p.n_kv_heads) return;
+  const int kvh = u % p.n_kv_heads;
+  const WorkItem it = load_item(p.items, u / p.n_kv_heads);
   const ReqEntry R = item_request(it);
   const int group = p.group;
-  const int nrows = R.lq * group, row0 = rb * kRows;
+  const int nrows = R.lq * group, row0 = rb * (16 * NB);
   if (row0 >= nrows) return;
 
-  // this lane's row
+  // this lane's rows
   const int n = lane & 15, g = lane >> 4;
-  const int row = row0 + n;
-  const bool rvalid = row < nrows;
-  const int qi = rvalid ? row / group : 0;
-  const int qh = kvh * group + (rvalid ? row % group : 0);
-  const int own_last = rvalid ? qi + R.ls - R.lq : -1;      // last visible own key
-  const int64_t orow = (int64_t)(R.q0 + qi) * p.n_q_heads + qh;
-  int dl = kNoLimit, dmin = kNoLimit;
+  bool rvalid[NB];
+  int own_last[NB], dl[NB], dmin = kNoLimit;                // own_last: last visible own key
+  int64_t orow[NB];
+#pragma unroll
+  for (int r = 0; r < NB; ++r) {
+    const int row = row0 + 16 * r + n;
+    rvalid[r] = row < nrows;
+    const int qi = rvalid[r] ? row / group : 0;
+    own_last[r] = rvalid[r] ? qi + R.ls - R.lq : -1;
+    orow[r] = (int64_t)(R.q0 + qi) * p.n_q_heads + kvh * group + (rvalid[r] ? row % group : 0);
+    dl[r] = kNoLimit;
+    if (kLim) {
+      if (rvalid[r]) dl[r] = p.doc_lim[R.q0 + qi];
+      dmin = min(dmin, dl[r]);
+    }
+  }
   if (kLim) {
-    if (rvalid) dl = p.doc_lim[R.q0 + qi];
-    dmin = dl;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) dmin = min(dmin, __shfl_xor(dmin, o));
     dmin = __builtin_amdgcn_readfirstlane(dmin);
@@ -299,25 +326,29 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     ia = info(t_begin);
     ta.load(ia.p, lane);
   }
-  bf16x8 qf[D / 32];
-  {
-    const uint4 *qrow = (const uint4 *)((const uint16_t *)p.q + orow * D + g * (D / 4));
+  bf16x8 qf[NB][D / 32];
+  State<D, NB> st;
+#pragma unroll
+  for (int r = 0; r < NB; ++r) {
+    const uint4 *qrow = (const uint4 *)((const uint16_t *)p.q + orow[r] * D + g * (D / 4));
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
       uint4 v = make_uint4(0, 0, 0, 0);
-      if (rvalid) v = qrow[s];
-      qf[s] = as_bf16x8(v);
+      if (rvalid[r]) v = qrow[s];
+      qf[r][s] = as_bf16x8(v);
     }
-  }
-  State<D> st;
 #pragma unroll
-  for (int b = 0; b < D / 16; ++b) st.o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  st.m = -INFINITY;
-  st.l = 0.f;
+    for (int b = 0; b < D / 16; ++b) st.o[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st.m[r] = -INFINITY;
+    st.l[r] = 0.f;
+  }
   const float sc = p.scale_log2;
   auto doc_tile = [&](const CacheTile<D> &x, const TileInfo &i) {
     const bool masked = i.nvalid < kTile || (kLim && i.tok + kTile > dmin);
-    compute_tile<D>(x, qf, st, lane, masked, (kLim ? min(i.nvalid, dl - i.tok) : i.nvalid) - 1, sc);
+    int kl[NB];
+#pragma unroll
+    for (int r = 0; r < NB; ++r) kl[r] = (kLim ? min(i.nvalid, dl[r] - i.tok) : i.nvalid) - 1;
+    compute_tile<D, NB>(x, qf, st, lane, masked, kl, sc);
   };
   // The load past the last tile reads the last one again, which keeps the
   // loop free of branches around loads (the compiler waits for every load in
@@ -332,7 +363,7 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     doc_tile(tb, ib);
   }
   // Own tiles up to the one that holds the block's last visible key.
-  const int last_qi = (min(row0 + kRows, nrows) - 1) / group;
+  const int last_qi = (min(row0 + 16 * NB, nrows) - 1) / group;
   const int t_end = min(it.t_end, visible_tiles(R, last_qi));
   const int own0 = max(t_begin, R.doc_tiles);
   if (own0 < t_end) {
@@ -347,61 +378,69 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     for (int j0 = (own0 - R.doc_tiles) * kTile; j0 < k_end; j0 += 32) {
       OwnTile<D> x;
       x.load((const char *)p.k_self + at, (const char *)p.v_self + at, stride, j0, R.ls - 1, lane);
-      compute_tile<D>(x, qf, st, lane, true, min(own_last, R.ls - 1) - j0, sc);
+      int kl[NB];
+#pragma unroll
+      for (int r = 0; r < NB; ++r) kl[r] = min(own_last[r], R.ls - 1) - j0;
+      compute_tile<D, NB>(x, qf, st, lane, true, kl, sc);
     }
   }
 
-  const float ltot = row_sum(st.l);
-  if (!rvalid) return;
-  if (it.part < 0) {
-    const float inv = ltot > 0.f ? 1.f / ltot : 0.f;
-    uint16_t *out = (uint16_t *)p.out + orow * D;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      __bf16 v[D / 16];
+  for (int r = 0; r < NB; ++r) {
+    const float ltot = row_sum(st.l[r]);
+    if (!rvalid[r]) continue;
+    if (it.part < 0) {
+      const float inv = ltot > 0.f ? 1.f / ltot : 0.f;
+      uint16_t *out = (uint16_t *)p.out + orow[r] * D;
 #pragma unroll
-      for (int b = 0; b < D / 16; ++b) v[b] = (__bf16)(st.o[b][i] * inv);
-      if constexpr (D == 128)
-        *(uint4 *)(out + 8 * (4 * g + i)) = __builtin_bit_cast(uint4, v);
-      else
-        *(uint2 *)(out + 4 * (4 * g + i)) = __builtin_bit_cast(uint2, v);
-    }
-    if (p.lse && g == 0) p.lse[orow] = ltot == 0.f ? -INFINITY : log_sum(st.m, ltot);
-  } else {
-    const int64_t prow = it.part + (orow - (int64_t)R.q0 * p.n_q_heads);
-    float *po = p.part_o + prow * D;
+      for (int i = 0; i < 4; ++i) {
+        __bf16 v[D / 16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int b = 0; b < D / 16; ++b) v[b] = (__bf16)(st.o[r][b][i] * inv);
+        if constexpr (D == 128)
+          *(uint4 *)(out + 8 * (4 * g + i)) = __builtin_bit_cast(uint4, v);
+        else
+          *(uint2 *)(out + 4 * (4 * g + i)) = __builtin_bit_cast(uint2, v);
+      }
+      if (p.lse && g == 0) p.lse[orow[r]] = ltot == 0.f ? -INFINITY : log_sum(st.m[r], ltot);
+    } else {
+      const int64_t prow = it.part + (orow[r] - (int64_t)R.q0 * p.n_q_heads);
+      float *po = p.part_o + prow * D;
 #pragma unroll
-      for (int b = 0; b < D / 16; b += 4)
-        *(float4 *)(po + (D / 16) * (4 * g + i) + b) =
-            make_float4(st.o[b][i], st.o[b + 1][i], st.o[b + 2][i], st.o[b + 3][i]);
-    if (g == 0) {
-      p.part_m[prow] = partial_max(st.m, ltot);
-      p.part_l[prow] = ltot;
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int b = 0; b < D / 16; b += 4)
+          *(float4 *)(po + (D / 16) * (4 * g + i) + b) =
+              make_float4(st.o[r][b][i], st.o[r][b + 1][i], st.o[r][b + 2][i], st.o[r][b + 3][i]);
+      if (g == 0) {
+        p.part_m[prow] = partial_max(st.m[r], ltot);
+        p.part_l[prow] = ltot;
+      }
     }
   }
 }
 
+template <int D, int NB>
+void launch(const LinkParams &p, dim3 grid, dim3 block, hipStream_t st) {
+  if (p.doc_lim)
+    hipLaunchKernelGGL((link_fp4_kernel<D, true, NB>), grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL((link_fp4_kernel<D, false, NB>), grid, block, 0, st, p);
+}
+
 }  // namespace
 
-int fp4_rows_per_block() { return kRows; }
+int fp4_rows_per_block(int max_rows) { return max_rows <= 16 ? 16 : 32; }
 
 hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **name) {
   *name = "link_fp4_kernel";
   const int64_t units = (int64_t)p.n_items * p.n_kv_heads * p.nrb;
   const dim3 grid((unsigned)((units + kWaves - 1) / kWaves)), block(64 * kWaves);
-  if (p.d_k == 128) {
-    if (p.doc_lim)
-      hipLaunchKernelGGL((link_fp4_kernel<128, true>), grid, block, 0, st, p);
-    else
-      hipLaunchKernelGGL((link_fp4_kernel<128, false>), grid, block, 0, st, p);
-  } else {
-    if (p.doc_lim)
-      hipLaunchKernelGGL((link_fp4_kernel<64, true>), grid, block, 0, st, p);
-    else
-      hipLaunchKernelGGL((link_fp4_kernel<64, false>), grid, block, 0, st, p);
-  }
+  const bool two = fp4_rows_per_block(p.max_rows) == 32;
+  if (p.d_k == 128)
+    two ? launch<128, 2>(p, grid, block, st) : launch<128, 1>(p, grid, block, st);
+  else
+    two ? launch<64, 2>(p, grid, block, st) : launch<64, 1>(p, grid, block, st);
   return hipGetLastError();
 }
 

@@ -291,9 +291,13 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
                    c.g * 4;
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
+      // (opaque: the compiler otherwise chains the comparisons through some
+      // sixty scalar registers, and spills those of the loop)
+      int k = kl;
+      asm volatile("" : "+v"(k));
       const int key = 8 * (x >> 2) + (x & 3);
-      if (key > kl) s0[x] = -INFINITY;
-      if (key + 32 > kl) s1[x] = -INFINITY;
+      if (key > k) s0[x] = -INFINITY;
+      if (key + 32 > k) s1[x] = -INFINITY;
     }
   }
   bf16x8 pf[4];
@@ -449,6 +453,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void link_fp4_prefill_kernel(LinkPa
     widen(c, ref0, sh, sk0, sv0);
     __syncthreads();
   }
+  // The queries have landed: without this use the loop's first products wait for
+  // every load in flight, the next tile's among them.
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) asm volatile("" : "+v"(qf[s]));
   // Tile t is computed from one buffer pair while tile t + 1 is loaded into
   // registers and then widened into the other (past the last tile: the last one
   // again, into the buffers nobody reads); unrolled by two so that every access

@@ -973,8 +973,8 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     c.over = 3;
     c.min_piece = 4;
   } else if (kern == Kern::Fp4) {
-    us = 5.0;
-    c.slots = 8 * (int64_t)cus;
+    us = 1.4;
+    c.slots = (d.d_k == 128 ? 4 : 8) * (int64_t)cus;
     c.over = 2;
     c.min_piece = 1;
   } else {
@@ -1196,7 +1196,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
                              : kern == Kern::Stream ? ss.rows * 4 / ss.kpar
                              : kern == Kern::Valu  ? valu_rows_per_block()
                              : kern == Kern::Mla   ? mla_rows_per_block()
-                             : kern == Kern::Fp4   ? fp4_rows_per_block()
+                             : kern == Kern::Fp4   ? fp4_rows_per_block(P.max_rows)
                              : kern == Kern::Fp4Prefill ? fp4_prefill_rows_per_block()
                                                    : decode_d128_max_rows();
   C.rows_per_block = rows_per_block;
