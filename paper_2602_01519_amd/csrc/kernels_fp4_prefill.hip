@@ -124,7 +124,10 @@ struct Place {
   int b, g, m;
 };
 template <int D>
-__device__ __forceinline__ Place place(const Ctx<D> &c, int lane) {
+__device__ __forceinline__ Place place(const Ctx<D> &c, int lane, bool fresh) {
+  // fresh: the lane made opaque, so that addresses formed from it stay where they
+  // are used and take no register in the loop over the tiles
+  if (fresh) asm volatile("" : "+v"(lane));
   const int w = c.wave & 3, lo = lane & 15, hi = lane >> 4;
   const bool value = c.wave >= 4;
   return Place{value, value ? lo >> 2 : w, value ? lo & 3 : hi, value ? 4 * w + hi : lo};
@@ -134,7 +137,7 @@ template <int D>
 __device__ __forceinline__ void fetch(const Ctx<D> &c, const TileRef &r, Share<D> &s) {
   typedef Fp4Tile<D> T;
   if (r.own) return;            // loaded where it is written (see widen)
-  const Place l = place(c, c.lane);
+  const Place l = place(c, c.lane, D == 64);
   const char *p = r.p + (l.value ? T::kV : 0);
   if constexpr (D == 128) {
     const uint4 u = *(const uint4 *)(p + (l.b * 64 + l.g * 16 + l.m) * 16);
@@ -182,11 +185,7 @@ __device__ __forceinline__ void widen_pair(const Place &l, const Share<D> &s, co
 // infinity would be a NaN).
 template <int D>
 __device__ __forceinline__ void stage_own(const Ctx<D> &c, const TileRef &r, uint4 *kt, uint4 *vt) {
-  // (the lane made opaque: addresses formed from it here stay here and take no
-  // register in the loop over the tiles)
-  int lane = c.lane;
-  asm volatile("" : "+v"(lane));
-  const Place l = place(c, lane);
+  const Place l = place(c, c.lane, true);
   const char *kv = (l.value ? c.vs : c.ks) + ((int64_t)r.tok + r.j0) * c.stride;
   if (!l.value) {
     const int key = 16 * l.b + l.m;
@@ -226,7 +225,7 @@ __device__ __forceinline__ void widen(const Ctx<D> &c, const TileRef &r, const S
     stage_own(c, r, kt, vt);
     return;
   }
-  const Place l = place(c, c.lane);
+  const Place l = place(c, c.lane, D == 64);
   if (!l.value) {
     const float sc = fp4_scale(s.scale);
 #pragma unroll
@@ -266,18 +265,29 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
     s0[x] = 0.f;
     s1[x] = 0.f;
   }
+  // Fragment addresses: chunk 2 st + g of a row is the row's chunk g with the bits
+  // of st exchanged. (D = 64 forms them for every tile: kept, they would take
+  // the registers that let two workgroups share a CU.)
+  uint32_t kbase = 16 * k_slot<D>(c.n, c.g), vbase = 16 * v_slot(c.n, c.g);
+  if (D == 64) asm volatile("" : "+v"(kbase), "+v"(vbase));
+  auto k_frag = [&](int half, int st) {
+    return as_bf16x8(*(const uint4 *)((const char *)kt + ((kbase ^ (st << 5)) + half * 64 * D)));
+  };
+  auto v_frag = [&](int d, int ks) {
+    return as_bf16x8(*(const uint4 *)((const char *)vt + ((vbase ^ (ks << 5)) + d * 4096)));
+  };
   constexpr int kSteps = D / 16, kAhead = kQkAhead < kSteps ? kQkAhead : kSteps;
   bf16x8 ka[kSteps], kb[kSteps];
 #pragma unroll
   for (int st = 0; st < kAhead; ++st) {
-    ka[st] = as_bf16x8(kt[k_slot<D>(c.n, st * 2 + c.g)]);
-    kb[st] = as_bf16x8(kt[k_slot<D>(32 + c.n, st * 2 + c.g)]);
+    ka[st] = k_frag(0, st);
+    kb[st] = k_frag(1, st);
   }
 #pragma unroll
   for (int st = 0; st < kSteps; ++st) {
     if (st + kAhead < kSteps) {
-      ka[st + kAhead] = as_bf16x8(kt[k_slot<D>(c.n, (st + kAhead) * 2 + c.g)]);
-      kb[st + kAhead] = as_bf16x8(kt[k_slot<D>(32 + c.n, (st + kAhead) * 2 + c.g)]);
+      ka[st + kAhead] = k_frag(0, st + kAhead);
+      kb[st + kAhead] = k_frag(1, st + kAhead);
     }
     s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[st], qf[st], s0, 0, 0, 0);
     s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[st], qf[st], s1, 0, 0, 0);
@@ -336,8 +346,7 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
   for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
-      const bf16x8 vf = as_bf16x8(vt[v_slot(d * 32 + c.n, ks * 2 + c.g)]);
-      a.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ks], a.o[d], 0, 0, 0);
+      a.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(d, ks), pf[ks], a.o[d], 0, 0, 0);
     }
   // V reads run kPvAhead MFMAs ahead
   constexpr int kPv = D / 8, kVAhead = kPvAhead < kPv ? kPvAhead : kPv;
@@ -370,8 +379,10 @@ __device__ __forceinline__ int limit_end(const LinkParams &p, const WorkItem &it
 }
 
 template <int D, bool kLim>
-__global__ __launch_bounds__(kWaves * 64, 2) void link_fp4_prefill_kernel(LinkParams p) {
-  __shared__ uint4 sk0[kTile * D / 8], sk1[kTile * D / 8], sv0[kTile * D / 8], sv1[kTile * D / 8];
+__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_kernel(LinkParams p) {
+  // one array, so that a lane's address serves both buffers
+  __shared__ uint4 lds[4][kTile * D / 8];
+  uint4 *const sk0 = lds[0], *const sk1 = lds[1], *const sv0 = lds[2], *const sv1 = lds[3];
   Ctx<D> c;
   c.lane = threadIdx.x & 63;
   c.wave = uni(threadIdx.x >> 6);
@@ -400,14 +411,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void link_fp4_prefill_kernel(LinkPa
   // this lane's row; a wave without rows only widens its share of every tile
   const bool active = row0 + c.wave * kRowsPerWave < nrows;
   const int row = row0 + c.wave * kRowsPerWave + c.n;
-  const bool rvalid = row < nrows;
-  const int qi = rvalid ? row / group : 0;
-  const int qh = c.kvh * group + (rvalid ? row % group : 0);
-  const int own_last = rvalid ? qi + R.ls - R.lq : -1;
-  const int64_t orow = (int64_t)(R.q0 + qi) * p.n_q_heads + qh;
+  const int qi0 = row < nrows ? row / group : 0;
+  const int own_last = row < nrows ? qi0 + R.ls - R.lq : -1;
+  // row of q and out (formed again after the loop over the tiles, which it would
+  // cost registers)
+  auto out_row = [&](int lane) {
+    const int r = row0 + c.wave * kRowsPerWave + (lane & 31);
+    const int i = r < nrows ? r / group : 0;
+    return (int64_t)(R.q0 + i) * p.n_q_heads + c.kvh * group + (r < nrows ? r % group : 0);
+  };
   DocLim dlm{kNoLimit, kNoLimit};
   if (kLim) {
-    if (rvalid) dlm.dl = p.doc_lim[R.q0 + qi];
+    if (row < nrows) dlm.dl = p.doc_lim[R.q0 + qi0];
     int w = dlm.dl;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) w = min(w, __shfl_xor(w, o));
@@ -432,11 +447,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void link_fp4_prefill_kernel(LinkPa
   }
   bf16x8 qf[D / 16];
   {
-    const uint4 *qrow = (const uint4 *)((const uint16_t *)p.q + orow * D);
+    const uint4 *qrow = (const uint4 *)((const uint16_t *)p.q + out_row(c.lane) * D);
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
       uint4 v = make_uint4(0, 0, 0, 0);
-      if (rvalid) v = qrow[s * 2 + c.g];
+      if (row < nrows) v = qrow[s * 2 + c.g];
       qf[s] = as_bf16x8(v);
     }
   }
@@ -476,6 +491,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void link_fp4_prefill_kernel(LinkPa
   }
 
   // ---- epilogue: O^T[dv][row], dv = 32 d + 8 (x >> 2) + 4 g + (x & 3)
+  int lane = c.lane;
+  asm volatile("" : "+v"(lane));
+  const bool rvalid = row0 + c.wave * kRowsPerWave + (lane & 31) < nrows;
+  const int64_t orow = out_row(lane);
   const float ltot = half_swap_sum(a.l);
   const int nvalid = min(kRowsPerWave, nrows - (row0 + c.wave * kRowsPerWave));
   if (nvalid <= 0) return;
@@ -532,6 +551,8 @@ hipError_t launch(const LinkParams &p, hipStream_t st) {
 }  // namespace
 
 int fp4_prefill_rows_per_block() { return kRows; }
+// resident workgroups per CU (two or four waves per SIMD)
+int fp4_prefill_blocks_per_cu(int d) { return d == 64 ? 2 : 1; }
 
 hipError_t launch_link_fp4_prefill(const LinkParams &p, hipStream_t st, const char **name) {
   *name = "link_fp4_prefill_kernel";

@@ -968,8 +968,8 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     c.over = 2;
     c.min_piece = 1;
   } else if (kern == Kern::Fp4Prefill) {
-    us = d.d_k == 128 ? 1.9 : 1.2;
-    c.slots = cus;
+    us = d.d_k == 128 ? 1.9 : 2.2;
+    c.slots = cus * fp4_prefill_blocks_per_cu(d.d_k);
     c.over = 3;
     c.min_piece = 4;
   } else if (kern == Kern::Fp4) {
@@ -1069,7 +1069,9 @@ void apply_splits(pic_store *s, int32_t n_q_heads, int rows_per_block, Setup &C)
     });
   } else if ((C.kern == Kern::Mfma128 || C.kern == Kern::Fp4Prefill) && !lp.spread) {
     balance_order_d128(s, P, lp, rows_per_block,
-                       s->shape.cus / s->shape.xcds * mfma_d128_blocks_per_cu());
+                       s->shape.cus / s->shape.xcds *
+                           (C.kern == Kern::Mfma128 ? mfma_d128_blocks_per_cu()
+                                                    : fp4_prefill_blocks_per_cu(s->desc.d_k)));
   }
   // The decode kernel reads the own KV in place: nothing to lay out.
   if (C.kern == Kern::Decode128) P.max_own_lp = 0;

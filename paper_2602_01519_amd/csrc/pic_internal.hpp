@@ -460,6 +460,7 @@ hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **nam
 int fp4_rows_per_block(int max_rows);
 hipError_t launch_link_fp4_prefill(const LinkParams &p, hipStream_t st, const char **name);
 int fp4_prefill_rows_per_block();
+int fp4_prefill_blocks_per_cu(int d);
 
 // bf16 MLA (absorbed) link attention: one 576-wide latent kv head, values
 // are the first 512 entries of each latent row.
