@@ -243,21 +243,6 @@ __device__ __forceinline__ void compute_tile(const Tile &x, const bf16x8 (&qf)[N
   }
 }
 
-// Walk over the tiles of a request's documents.
-struct Cursor {
-  const_links links;       // the request's links, from the item's first on
-  int li;
-  const char *base;        // the link's first tile
-  int len, tok0, tile0, end;
-};
-__device__ __forceinline__ void cursor_next(Cursor &c) {
-  ++c.li;
-  c.base = (const char *)c.links[c.li].k;
-  c.len = c.links[c.li].len;
-  c.tok0 = c.links[c.li].tok0;
-  c.tile0 = c.links[c.li].tile0;
-  c.end = c.tile0 + (c.len + kTile - 1) / kTile;
-}
 struct TileInfo {
   const char *p;
   int nvalid, tok;
@@ -305,16 +290,10 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     dmin = __builtin_amdgcn_readfirstlane(dmin);
   }
 
-  Cursor c;
-  c.links = (const_links)p.links + it.link;
-  c.li = 0;
-  c.base = (const char *)it.k;
-  c.len = it.len;
-  c.tok0 = it.tok0;
-  c.tile0 = it.tile0;
-  c.end = it.tile0 + (it.len + kTile - 1) / kTile;
+  LinkCursor<true> c;
+  c.start(p, it);
   auto info = [&](int t) {       // t only grows
-    while (t >= c.end) cursor_next(c);
+    while (t >= c.end) c.next();
     const int tt = t - c.tile0;
     return TileInfo{c.base + ((int64_t)tt * p.n_kv_heads + kvh) * Fp4Tile<D>::kBytes,
                     min(kTile, c.len - tt * kTile), c.tok0 + tt * kTile};
@@ -369,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   if (own0 < t_end) {
     int s0 = it.tok0;             // the own link's: its first own row
     if (it.tile0 < R.doc_tiles) {
-      while (c.tile0 < R.doc_tiles) cursor_next(c);
+      while (c.tile0 < R.doc_tiles) c.next();
       s0 = c.tok0;
     }
     const int64_t at = ((int64_t)s0 * p.n_kv_heads + kvh) * D * 2;

@@ -670,6 +670,8 @@ void write_items(const Setup &C, const LinkEntry *links, WorkItem *out) {
         w.tok0 = L.tok0;
       }
       if (C.kern == Kern::Decode128) w.tok0 = R.s0;   // it masks no linked rows
+      if (C.kern == Kern::Fp4 || C.kern == Kern::Fp4Prefill)
+        w.lp = R.link0 + R.nlinks - 1 - li;            // links that follow
       w.link = li;
       w.q0 = R.q0;
       w.lq = R.lq;

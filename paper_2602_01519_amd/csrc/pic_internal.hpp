@@ -73,8 +73,9 @@ __host__ __device__ __forceinline__ int visible_tiles(const ReqEntry &r, int q_l
 // that load waits for one table read (the request order, the request and a
 // walk over its links were three and more dependent ones). The link fields
 // are those of the entry that holds tile t_begin; later links follow at
-// links[link + 1] ... (for the decode kernel, which masks no linked rows, tok0
-// is the request's first own row)
+// links[link + 1] ... (for the bf16 decode kernel, which masks no linked rows, tok0
+// is the request's first own row; for the 4-bit kernels lp is the number of
+// links that follow)
 struct WorkItem {
   const void *k, *v;
   int32_t len, lp, tile0, tok0;
