@@ -114,22 +114,27 @@ __global__ __launch_bounds__(256) void fp4_copy_pages_kernel(PageCopies c, int64
   *(uint4 *)(pg.dst_k + off) = *(const uint4 *)(pg.src_k + off);
 }
 
-// Values of the linked rows, token-major bf16. grid: (tiles, heads). A link's
-// tiles are found by a walk over the links (a test hook: few links).
+struct GatherLinks {
+  int32_t n;
+  int32_t tile0[kGatherLinks];      // the link's first workgroup
+  const char *page[kGatherLinks];
+  int32_t len[kGatherLinks], tok0[kGatherLinks];
+};
+
+// Values of the linked rows, token-major bf16. grid: (tiles, heads)
 template <int D>
-__global__ __launch_bounds__(256) void fp4_gather_kernel(const LinkEntry *links, int n_links,
-                                                         int heads, uint16_t *k, uint16_t *v) {
+__global__ __launch_bounds__(256) void fp4_gather_kernel(GatherLinks links, int heads, uint16_t *k,
+                                                         uint16_t *v) {
   typedef Fp4Tile<D> T;
   __shared__ uint4 tile[T::kBytes / 16];
-  int li = 0, first = 0;
-  for (; li + 1 < n_links; ++li) {
-    const int n = (links[li].len + 63) / 64;
-    if ((int)blockIdx.x < first + n) break;
-    first += n;
-  }
-  const LinkEntry L = links[li];
-  const int t = blockIdx.x - first, h = blockIdx.y;
-  const uint4 *src = (const uint4 *)((const char *)L.k + ((int64_t)t * heads + h) * T::kBytes);
+  int li = 0;
+  while (li + 1 < links.n && (int)blockIdx.x >= links.tile0[li + 1]) ++li;
+  struct {
+    const char *k;
+    int32_t len, tok0;
+  } const L{links.page[li], links.len[li], links.tok0[li]};
+  const int t = blockIdx.x - links.tile0[li], h = blockIdx.y;
+  const uint4 *src = (const uint4 *)(L.k + ((int64_t)t * heads + h) * T::kBytes);
   for (int i = threadIdx.x; i < T::kBytes / 16; i += 256) tile[i] = src[i];
   __syncthreads();
   const char *b = (const char *)tile;
@@ -197,15 +202,25 @@ hipError_t launch_fp4_copy_pages(const PageCopies &c, int32_t n, int32_t n_layer
   return hipGetLastError();
 }
 
-hipError_t launch_fp4_gather(const LinkEntry *links, int32_t n_links, int32_t tiles, int32_t heads,
-                             int32_t d, void *k, void *v, hipStream_t st) {
+hipError_t launch_fp4_gather(const LinkEntry *links, int32_t n_links, int32_t heads, int32_t d,
+                             void *k, void *v, hipStream_t st) {
+  GatherLinks g{};
+  g.n = n_links;
+  int32_t tiles = 0;
+  for (int32_t i = 0; i < n_links; ++i) {
+    g.tile0[i] = tiles;
+    g.page[i] = (const char *)links[i].k;
+    g.len[i] = links[i].len;
+    g.tok0[i] = links[i].tok0;
+    tiles += (links[i].len + 63) / 64;
+  }
   const dim3 grid((unsigned)tiles, (unsigned)heads);
   if (d == 128)
-    hipLaunchKernelGGL(fp4_gather_kernel<128>, grid, dim3(256), 0, st, links, n_links, heads,
-                       (uint16_t *)k, (uint16_t *)v);
+    hipLaunchKernelGGL(fp4_gather_kernel<128>, grid, dim3(256), 0, st, g, heads, (uint16_t *)k,
+                       (uint16_t *)v);
   else
-    hipLaunchKernelGGL(fp4_gather_kernel<64>, grid, dim3(256), 0, st, links, n_links, heads,
-                       (uint16_t *)k, (uint16_t *)v);
+    hipLaunchKernelGGL(fp4_gather_kernel<64>, grid, dim3(256), 0, st, g, heads, (uint16_t *)k,
+                       (uint16_t *)v);
   return hipGetLastError();
 }
 

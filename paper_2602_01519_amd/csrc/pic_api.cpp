@@ -1315,7 +1315,12 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
     lp.part_m = lp.part_o + C.part_rows * d.d_v;
     lp.part_l = lp.part_m + C.part_rows;
   }
-  if (C.P.max_own_lp > 0 || pro.copy_bytes > 0) {
+  if (is_fp4(d)) {        // own KV read in place: only the tables to copy
+    if (pro.copy_bytes > 0) {
+      const hipError_t e = launch_table_copy(pro.copy_src, pro.copy_dst, pro.copy_bytes, st);
+      if (e != hipSuccess) return hip_fail(e, "table_copy_kernel");
+    }
+  } else if (C.P.max_own_lp > 0 || pro.copy_bytes > 0) {
     hipError_t e = launch_prologue(lp, pro.links, pro.reqs, mla, s->esz, C.P.max_own_lp,
                                    C.own_args.empty() ? nullptr : C.own_args.data(), work,
                                    pro.copy_src, pro.copy_dst, pro.copy_bytes, st);
@@ -2256,6 +2261,14 @@ pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_
   DeviceGuard dg(s->device);
   if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
   const hipStream_t st = (hipStream_t)stream;
+  if (is_fp4(s->desc)) {       // links as kernel arguments: no table to copy
+    for (int32_t i = 0; i < n; i += kGatherLinks) {
+      const hipError_t e = launch_fp4_gather(links.data() + i, std::min(kGatherLinks, n - i),
+                                             s->desc.n_kv_heads, s->desc.d_k, k_out, v_out, st);
+      if (e != hipSuccess) return hip_fail(e, "fp4_gather_kernel");
+    }
+    return PIC_OK;
+  }
   Stage *stage = nullptr;
   pic_status rc = stage_acquire(s, sizeof(LinkEntry) * n, &stage);
   if (rc != PIC_OK) return rc;
@@ -2263,12 +2276,8 @@ pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_
   HIP_TRY(launch_table_copy(stage->host_dev, stage->dev, (int64_t)(sizeof(LinkEntry) * n), st),
           "table_copy_kernel");
   const pic_store_desc &d = s->desc;
-  int64_t tiles = 0;
-  for (const LinkEntry &E : links) tiles += (E.len + kTile - 1) / kTile;
-  hipError_t e = is_fp4(d) ? launch_fp4_gather((const LinkEntry *)stage->dev, n, (int32_t)tiles,
-                                               d.n_kv_heads, d.d_k, k_out, v_out, st)
-                           : launch_gather((const LinkEntry *)stage->dev, n, toks, d.n_kv_heads,
-                                           d.d_k, d.d_v, !gqa, s->esz, k_out, v_out, st);
+  hipError_t e = launch_gather((const LinkEntry *)stage->dev, n, toks, d.n_kv_heads,
+                               d.d_k, d.d_v, !gqa, s->esz, k_out, v_out, st);
   if (e != hipSuccess) return hip_fail(e, "gather_kernel");
   HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");
   stage->pending = true;

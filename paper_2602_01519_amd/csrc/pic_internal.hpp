@@ -376,9 +376,11 @@ hipError_t launch_fp4_copy_pages(const PageCopies &c, int32_t n, int32_t n_layer
 hipError_t launch_fp4_write_rows(const RowView *views, int32_t n_views, const int32_t *rows,
                                  int32_t n, const void *k, const void *v, int32_t heads, int32_t d,
                                  hipStream_t st);
-// tiles: tiles of all links
-hipError_t launch_fp4_gather(const LinkEntry *links, int32_t n_links, int32_t tiles, int32_t heads,
-                             int32_t d, void *k, void *v, hipStream_t st);
+// links: host, at most kGatherLinks, passed as a kernel argument; tok0: a
+// link's first row of k and v
+constexpr int kGatherLinks = 64;
+hipError_t launch_fp4_gather(const LinkEntry *links, int32_t n_links, int32_t heads, int32_t d,
+                             void *k, void *v, hipStream_t st);
 
 // Copies bytes (a multiple of 16) from a host-mapped buffer to the device.
 hipError_t launch_table_copy(const void *src, void *dst, int64_t bytes, hipStream_t st);

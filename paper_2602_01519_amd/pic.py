@@ -143,13 +143,11 @@ def _check(st: int):
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
     if isinstance(x, np.ndarray):
         return x.ctypes.data
-    return x.data_ptr()          # torch tensor
+    return int(x) if isinstance(x, int) else x.data_ptr()    # torch tensor
 
 
 def _host_i32(a):
@@ -358,11 +356,12 @@ class LinkPlan:
                                           int(num_splits), ctypes.byref(h)))
         self.handle = h.value
         self.store = store          # the store must outlive the plan
+        self._run = lib().pic_link_plan_run
 
     def run(self, layer: int, q, k_self, v_self, softmax_scale: float, out, lse=None,
             stream: Optional[int] = None):
-        _check(lib().pic_link_plan_run(self.handle, int(layer), _ptr(q), _ptr(k_self), _ptr(v_self),
-                                       float(softmax_scale), _ptr(out), _ptr(lse), stream))
+        _check(self._run(self.handle, int(layer), _ptr(q), _ptr(k_self), _ptr(v_self),
+                         float(softmax_scale), _ptr(out), _ptr(lse), stream))
 
     def close(self):
         if getattr(self, "handle", None):
@@ -404,6 +403,7 @@ class Rope:
         h = ctypes.c_void_p()
         _check(lib().pic_rope_create(ctypes.byref(desc), ctypes.byref(h)))
         self.handle = h
+        self._apply = lib().pic_rope_apply
 
     def apply(self, n_tokens: int, positions, tensors, transposed: bool = False,
               stream: Optional[int] = None):
@@ -411,10 +411,16 @@ class Rope:
         elements from token to token (0: dense)."""
         if not self.handle:
             raise PicError(ERR_INVALID, "the handle is closed")
-        arr = (RopeTensor * max(1, len(tensors)))(
-            *[RopeTensor(_ptr(x), _ptr(y), int(xs), int(ys), int(h)) for x, y, h, xs, ys in tensors])
-        _check(lib().pic_rope_apply(self.handle, int(n_tokens), _ptr(positions), arr, len(tensors),
-                                    int(bool(transposed)), stream))
+        # pic_rope_tensor is five 8-byte words (n_heads in the low half of the last): an array of
+        # integers costs a third of one of structures
+        words = []
+        for x, y, h, xs, ys in tensors:
+            if not -2 ** 31 <= h < 2 ** 31:
+                raise PicError(ERR_INVALID, "n_heads out of range")
+            words += (_ptr(x) or 0, _ptr(y) or 0, xs, ys, h)
+        arr = (ctypes.c_int64 * len(words))(*words)
+        _check(self._apply(self.handle, n_tokens, _ptr(positions), arr, len(tensors),
+                           1 if transposed else 0, stream))
 
     def close(self):
         if getattr(self, "handle", None):
