@@ -65,6 +65,14 @@ __device__ __forceinline__ int v_slot(int ch, int c) {
   return ch * 8 + (c ^ ((x ^ (x >> 3)) & 7));
 }
 
+// A copy of x that the compiler takes for another value: what is formed from it stays where
+// it is used and takes no register in the loop over the tiles.
+template <typename T>
+__device__ __forceinline__ T fresh(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // A key tile: workgroup-uniform facts.
 struct TileRef {
   const char *p;     // the tile in the cache (kv head applied)
@@ -81,6 +89,9 @@ struct Ctx {
   LinkCursor<D == 64> cur;
   const char *ks, *vs;     // k_self / v_self, kv head applied, token 0 of the batch
   int64_t stride;          // ... bytes per token
+  uint32_t load;           // byte offsets of this lane's share within a cache tile: codes
+                           // (low half), scales
+  uint32_t put;            // ... and of its first chunk within the LDS tile
 
   // Tile t of the request (t only grows across calls). The own link's tok0 is its
   // first row in k_self.
@@ -113,58 +124,70 @@ struct Place {
   int b, g, m;
 };
 template <int D>
-__device__ __forceinline__ Place place(const Ctx<D> &c, int lane, bool fresh) {
-  // fresh: the lane made opaque, so that addresses formed from it stay where they
-  // are used and take no register in the loop over the tiles
-  if (fresh) asm volatile("" : "+v"(lane));
+__device__ __forceinline__ Place place(const Ctx<D> &c, int lane) {
   const int w = c.wave & 3, lo = lane & 15, hi = lane >> 4;
   const bool value = c.wave >= 4;
   return Place{value, value ? lo >> 2 : w, value ? lo & 3 : hi, value ? 4 * w + hi : lo};
 }
 
+// This lane's offsets, formed once. The chunks that it writes follow from the first:
+// key chunk j of its row is the first with j exchanged into the chunk's bits, and channel
+// c of its D/16 is c rows on, with c exchanged into them (both swizzles are linear).
+template <int D>
+__device__ __forceinline__ void set_offsets(Ctx<D> &c) {
+  typedef Fp4Tile<D> T;
+  const Place l = place(c, c.lane);
+  const int unit = D == 128 ? (l.b * 64 + l.g * 16 + l.m) * 16
+                            : ((l.b >> 1) * 64 + l.g * 16 + l.m) * 16 + (l.b & 1) * 8;
+  const int key = 16 * l.b + (l.value ? 4 * l.g : l.m);
+  c.load = ((l.value ? T::kV : 0) + unit) |
+           (l.value ? T::v_scale(key, l.m * (D / 16) / 32) : T::k_scale(key, l.g * (D / 4) / 32)) << 16;
+  c.put = l.value ? 16 * v_slot(l.m * (D / 16), 2 * l.b + (l.g & 1)) + 8 * (l.g >> 1)
+                  : 16 * k_slot<D>(key, l.g * (D / 32));
+}
+
 template <int D>
 __device__ __forceinline__ void fetch(const Ctx<D> &c, const TileRef &r, Share<D> &s) {
-  typedef Fp4Tile<D> T;
   if (r.own) {
     if (D == 128) return;       // loaded where it is written (see stage_own)
     // The same, but one word of each line here, so that it comes from the L2 then:
     // every lane a quarter of a row. (The 128-wide kernel loses 0.5% by it.)
-    const Place l = place(c, c.lane, true);
+    const Place l = place(c, fresh(c.lane));
     const int key = l.value ? 16 * l.b + 4 * l.g + (l.m & 3) : 16 * l.b + l.m;
     const int at = (l.value ? l.m >> 2 : l.g) * (D / 2);
     s.x[0] = *(const uint32_t *)((l.value ? c.vs : c.ks) +
                                  ((int64_t)r.tok + r.j0 + min(key, r.nvalid - 1)) * c.stride + at);
     return;
   }
-  const Place l = place(c, c.lane, D == 64);
-  const char *p = r.p + (l.value ? T::kV : 0);
+  // (fresh: extended to 64 bits here, not kept so)
+  const uint32_t at = fresh(c.load), code = at & 0xffffu, scale = at >> 16;
   if constexpr (D == 128) {
-    const uint4 u = *(const uint4 *)(p + (l.b * 64 + l.g * 16 + l.m) * 16);
+    const uint4 u = *(const uint4 *)(r.p + code);
     s.x[0] = u.x, s.x[1] = u.y, s.x[2] = u.z, s.x[3] = u.w;
   } else {
-    const uint2 u = *(const uint2 *)(p + ((l.b >> 1) * 64 + l.g * 16 + l.m) * 16 + (l.b & 1) * 8);
+    const uint2 u = *(const uint2 *)(r.p + code);
     s.x[0] = u.x, s.x[1] = u.y;
   }
-  if (l.value)
-    s.scale = *(const uint32_t *)(r.p + T::v_scale(16 * l.b + 4 * l.g, l.m * (D / 16) / 32));
+  if (c.wave >= 4)
+    s.scale = *(const uint32_t *)(r.p + scale);
   else
-    s.scale = *(const uint8_t *)(r.p + T::k_scale(16 * l.b + l.m, l.g * (D / 4) / 32));
+    s.scale = *(const uint8_t *)(r.p + scale);
 }
 
 // Pairs of channels (2 kC, 2 kC + 1) of four keys into V^T as four keys of each.
-template <int D, int kC>
-__device__ __forceinline__ void put_pair(const Place &l, uint4 *vt, const uint32_t (&d)[4]) {
-  const int ch = l.m * (D / 16) + 2 * kC, chunk = 2 * l.b + (l.g & 1), half = l.g >> 1;
-  ((uint2 *)vt)[v_slot(ch, chunk) * 2 + half] =
+template <int kC>
+__device__ __forceinline__ void put_pair(uint32_t put, uint4 *vt, const uint32_t (&d)[4]) {
+  char *const p = (char *)vt;
+  *(uint2 *)(p + ((put ^ (32 * kC)) + 256 * kC)) =
       make_uint2(__builtin_amdgcn_perm(d[1], d[0], 0x05040100u),
                  __builtin_amdgcn_perm(d[3], d[2], 0x05040100u));
-  ((uint2 *)vt)[v_slot(ch + 1, chunk) * 2 + half] =
+  *(uint2 *)(p + ((put ^ (32 * kC + 16)) + 256 * kC + 128)) =
       make_uint2(__builtin_amdgcn_perm(d[1], d[0], 0x07060302u),
                  __builtin_amdgcn_perm(d[3], d[2], 0x07060302u));
 }
 
 template <int D, int kC>
-__device__ __forceinline__ void widen_pair(const Place &l, const Share<D> &s, const float (&sc)[4],
+__device__ __forceinline__ void widen_pair(uint32_t put, const Share<D> &s, const float (&sc)[4],
                                            uint4 *vt) {
   uint32_t d[4];
 #pragma unroll
@@ -174,7 +197,7 @@ __device__ __forceinline__ void widen_pair(const Place &l, const Share<D> &s, co
     else
       d[i] = (i & 1) ? fp4_pair<2 + (kC & 1)>(s.x[i >> 1], sc[i]) : fp4_pair<kC & 1>(s.x[i >> 1], sc[i]);
   }
-  put_pair<D, kC>(l, vt, d);
+  put_pair<kC>(put, vt, d);
 }
 
 // An own tile, from k_self / v_self straight to LDS. (Loaded a tile ahead as the
@@ -184,7 +207,8 @@ __device__ __forceinline__ void widen_pair(const Place &l, const Share<D> &s, co
 // infinity would be a NaN).
 template <int D>
 __device__ __forceinline__ void stage_own(const Ctx<D> &c, const TileRef &r, uint4 *kt, uint4 *vt) {
-  const Place l = place(c, c.lane, true);
+  const Place l = place(c, fresh(c.lane));
+  const uint32_t put = fresh(c.put);
   const char *kv = (l.value ? c.vs : c.ks) + ((int64_t)r.tok + r.j0) * c.stride;
   if (!l.value) {
     const int key = 16 * l.b + l.m;
@@ -193,7 +217,7 @@ __device__ __forceinline__ void stage_own(const Ctx<D> &c, const TileRef &r, uin
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) x[j] = *(const uint4 *)(p + 16 * j);
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) kt[k_slot<D>(key, l.g * (D / 32) + j)] = x[j];
+    for (int j = 0; j < D / 32; ++j) *(uint4 *)((char *)kt + (put ^ (16 * j))) = x[j];
     return;
   }
   uint32_t x[D / 32][4];
@@ -209,11 +233,11 @@ __device__ __forceinline__ void stage_own(const Ctx<D> &c, const TileRef &r, uin
       x[j + 1][i] = u.y & keep;
     }
   }
-  put_pair<D, 0>(l, vt, x[0]);
-  put_pair<D, 1>(l, vt, x[1]);
+  put_pair<0>(put, vt, x[0]);
+  put_pair<1>(put, vt, x[1]);
   if constexpr (D == 128) {
-    put_pair<D, 2>(l, vt, x[2]);
-    put_pair<D, 3>(l, vt, x[3]);
+    put_pair<2>(put, vt, x[2]);
+    put_pair<3>(put, vt, x[3]);
   }
 }
 
@@ -225,22 +249,22 @@ __device__ __forceinline__ void widen(const Ctx<D> &c, const TileRef &r, const S
     stage_own(c, r, kt, vt);
     return;
   }
-  const Place l = place(c, c.lane, D == 64);
-  if (!l.value) {
+  const uint32_t put = D == 64 ? fresh(c.put) : c.put;   // (fragment addresses: see compute_tile)
+  if (c.wave < 4) {
     const float sc = fp4_scale(s.scale);
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
-      kt[k_slot<D>(16 * l.b + l.m, l.g * (D / 32) + j)] = fp4_decode8(s.x[j], sc);
+      *(uint4 *)((char *)kt + (put ^ (16 * j))) = fp4_decode8(s.x[j], sc);
     return;
   }
   float sc[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) sc[i] = fp4_scale((s.scale >> (8 * i)) & 255u);
-  widen_pair<D, 0>(l, s, sc, vt);
-  widen_pair<D, 1>(l, s, sc, vt);
+  widen_pair<D, 0>(put, s, sc, vt);
+  widen_pair<D, 1>(put, s, sc, vt);
   if constexpr (D == 128) {
-    widen_pair<D, 2>(l, s, sc, vt);
-    widen_pair<D, 3>(l, s, sc, vt);
+    widen_pair<D, 2>(put, s, sc, vt);
+    widen_pair<D, 3>(put, s, sc, vt);
   }
 }
 
@@ -255,10 +279,11 @@ struct DocLim {
   int dl, wmin;
 };
 
-template <int D, bool kLim>
+// own_last(): last own key that this lane's row sees (formed where a tile needs it).
+template <int D, bool kLim, class OwnLast>
 __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, const uint4 *vt,
                                              const bf16x8 (&qf)[D / 16], Acc<D> &a, const TileRef &r,
-                                             int own_last, const DocLim &dlm, float sc) {
+                                             OwnLast own_last, const DocLim &dlm, float sc) {
   f32x16 s0, s1;
 #pragma unroll
   for (int x = 0; x < 16; ++x) {
@@ -269,14 +294,14 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
   // of st exchanged. (D = 64 forms them for every tile: kept, they would take
   // the registers that let two workgroups share a CU.)
   uint32_t kbase = 16 * k_slot<D>(c.n, c.g), vbase = 16 * v_slot(c.n, c.g);
-  if (D == 64) asm volatile("" : "+v"(kbase), "+v"(vbase));
+  if (D == 64) kbase = fresh(kbase), vbase = fresh(vbase);
   auto k_frag = [&](int half, int st) {
     return as_bf16x8(*(const uint4 *)((const char *)kt + ((kbase ^ (st << 5)) + half * 64 * D)));
   };
   auto v_frag = [&](int d, int ks) {
     return as_bf16x8(*(const uint4 *)((const char *)vt + ((vbase ^ (ks << 5)) + d * 4096)));
   };
-  constexpr int kSteps = D / 16, kAhead = kQkAhead < kSteps ? kQkAhead : kSteps;
+  constexpr int kSteps = D / 16, kAhead = D == 64 ? 4 : kQkAhead;
   bf16x8 ka[kSteps], kb[kSteps];
 #pragma unroll
   for (int st = 0; st < kAhead; ++st) {
@@ -295,10 +320,9 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
   }
   // s0[x] / s1[x]: key 8 (x >> 2) + 4 g + (x & 3) (+ 32)
   if (r.own || r.nvalid < kTile || (kLim && r.tok + kTile > dlm.wmin)) {
-    const int kl = (r.own   ? min(own_last - r.j0, r.nvalid - 1)
-                    : kLim ? min(dlm.dl - r.tok, r.nvalid) - 1
-                           : r.nvalid - 1) -
-                   c.g * 4;
+    int kl = kLim ? min(dlm.dl - r.tok, r.nvalid) - 1 : r.nvalid - 1;
+    if (r.own) kl = min(own_last() - r.j0, r.nvalid - 1);
+    kl -= 4 * (fresh(c.lane) >> 5);
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
       // (opaque: the compiler otherwise chains the comparisons through some
@@ -349,7 +373,7 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
       a.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(d, ks), pf[ks], a.o[d], 0, 0, 0);
     }
   // V reads run kPvAhead MFMAs ahead
-  constexpr int kPv = D / 8, kVAhead = kPvAhead < kPv ? kPvAhead : kPv;
+  constexpr int kPv = D / 8, kVAhead = kPvAhead;
   __builtin_amdgcn_sched_group_barrier(0x100, kVAhead, 0);
 #pragma unroll
   for (int i = 0; i < kPv; ++i) {
@@ -411,8 +435,10 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill
   // this lane's row; a wave without rows only widens its share of every tile
   const bool active = row0 + c.wave * kRowsPerWave < nrows;
   const int row = row0 + c.wave * kRowsPerWave + c.n;
-  const int qi0 = row < nrows ? row / group : 0;
-  const int own_last = row < nrows ? qi0 + R.ls - R.lq : -1;
+  auto own_last = [&]() {
+    const int r = row0 + c.wave * kRowsPerWave + (fresh(c.lane) & 31);
+    return r < nrows ? r / group + R.ls - R.lq : -1;
+  };
   // row of q and out (formed again after the loop over the tiles, which it would
   // cost registers)
   auto out_row = [&](int lane) {
@@ -422,13 +448,14 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill
   };
   DocLim dlm{kNoLimit, kNoLimit};
   if (kLim) {
-    if (row < nrows) dlm.dl = p.doc_lim[R.q0 + qi0];
+    if (row < nrows) dlm.dl = p.doc_lim[R.q0 + row / group];
     int w = dlm.dl;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) w = min(w, __shfl_xor(w, o));
     dlm.wmin = uni(w);
   }
   c.cur.start(p, it);
+  set_offsets(c);
   c.stride = (int64_t)p.n_kv_heads * D * 2;
   c.ks = (const char *)p.k_self + c.kvh * D * 2;
   c.vs = (const char *)p.v_self + c.kvh * D * 2;
@@ -485,8 +512,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill
   }
 
   // ---- epilogue: O^T[dv][row], dv = 32 d + 8 (x >> 2) + 4 g + (x & 3)
-  int lane = c.lane;
-  asm volatile("" : "+v"(lane));
+  const int lane = fresh(c.lane);
   const bool rvalid = row0 + c.wave * kRowsPerWave + (lane & 31) < nrows;
   const int64_t orow = out_row(lane);
   const float ltot = half_swap_sum(a.l);

@@ -417,9 +417,9 @@ class Rope:
         for x, y, h, xs, ys in tensors:
             if not -2 ** 31 <= h < 2 ** 31:
                 raise PicError(ERR_INVALID, "n_heads out of range")
-            words += (_ptr(x) or 0, _ptr(y) or 0, xs, ys, h)
+            words += (_ptr(x) or 0, _ptr(y) or 0, int(xs), int(ys), int(h))
         arr = (ctypes.c_int64 * len(words))(*words)
-        _check(self._apply(self.handle, n_tokens, _ptr(positions), arr, len(tensors),
+        _check(self._apply(self.handle, int(n_tokens), _ptr(positions), arr, len(tensors),
                            1 if transposed else 0, stream))
 
     def close(self):
