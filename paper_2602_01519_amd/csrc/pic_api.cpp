@@ -935,8 +935,24 @@ bool small_tables(const Plan &P) {
 // gains; fp32 gains or loses with how its split count falls.
 constexpr int kStreamSmallRows = 128;
 
-// Most rows per kv head that the one-wave kernel takes.
+// Calls of a 4-bit store that the one-wave kernel takes: at most kFp4FewRows rows
+// per kv head (16 requests of 64 rows, 128-wide heads, over 4..12 links: 45 us, in 256-row
+// workgroups 80), or work that leaves those workgroups too few tiles each to
+// cover their start, counted in tiles per CU. One wave against 256 rows, 32/8
+// heads, us: one request of 148 / 256 / 384 rows over 110 tiles 25 / 26 / 35
+// against 26 / 32 / 34 (3.4, 3.4 and 6.9 tiles per CU), over 220 tiles 30 / 33 / 45
+// against 31 / 36 / 40; 4 requests of 148 rows over 110 tiles (13.8) 42 against 38.
+// 64-wide heads: one request of 512 rows over 110 tiles (6.9) 29 against 36, over 220
+// (13.8) 39 against 42; 4 requests of 256 rows over 110 (13.8) 40 against 39.
 constexpr int kFp4FewRows = 64;
+bool fp4_one_wave(const Plan &P, const pic_store_desc &d, int group, int cus) {
+  if (P.max_rows <= kFp4FewRows) return true;
+  const int block = fp4_prefill_rows_per_block();
+  int64_t tiles = 0;
+  for (const ReqEntry &R : P.reqs)
+    tiles += (int64_t)d.n_kv_heads * (((int64_t)R.lq * group + block - 1) / block) * R.tiles;
+  return tiles <= (int64_t)cus * (d.d_k == 128 ? 6 : 12);
+}
 
 // Costs of a kernel's pieces in its tiles (see choose_splits). Tile times on
 // a full GPU: d128 1.75 us per workgroup (64 keys), MLA 2.0 us (64 keys),
@@ -1173,7 +1189,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   // per-row masks of the flash kernel
   if (kern == Kern::Decode128 && !P.doc_lim.empty()) kern = Kern::Mfma128;
   if (d.dtype == PIC_BF16 && mla && d.d_k == 576 && d.d_v == 512) kern = Kern::Mla;
-  if (fp4) kern = P.max_rows <= kFp4FewRows ? Kern::Fp4 : Kern::Fp4Prefill;
+  if (fp4) kern = fp4_one_wave(P, d, lp.group, s->shape.cus) ? Kern::Fp4 : Kern::Fp4Prefill;
   // A small generic call of a shape the lean kernel is built for (tables as
   // a kernel argument, at most kLeanTiles tiles in all) runs it; other fp32
   // and narrow bf16 GQA calls stream their keys through the matrix cores.

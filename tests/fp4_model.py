@@ -11,7 +11,9 @@ once (2^-8 of it), so per element
 in fp32, off by at most D 2^-24 sum|q k| scale; a relative change e of every probability moves
 out by at most 2 e W, and lse by e. Sums of n probabilities in fp32 (partial sums of lanes
 and pieces: fewer than n steps) add n 2^-24. exp2, the scale and the log-sum-exp's own
-rounding add a few 2^-24 of the logit's size."""
+rounding add a few 2^-24 of the logit's size. What is smaller than 2^-126 may be flushed to
+zero: each of n probabilities, whose sum is at least 1/2 (the largest is about 1 in its own
+unit), and the output: at most (n + 1) 2^-126 (1 + max|v|) in all."""
 import numpy as np
 
 GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6], np.float64)
@@ -55,24 +57,24 @@ def attend(q, k, v, scale, seen):
     out, lse = np.zeros(q.shape), np.full((lq, hq), -np.inf)
     tol, tl = np.zeros(q.shape), np.zeros((lq, hq))
     u = 2.0 ** -24
+    some = seen.any(1)
     for h in range(hq):
         kh, vh = k[:, h // g], v[:, h // g]
-        s = scale * (q[:, h] @ kh.T)
-        size = scale * (np.abs(q[:, h]) @ np.abs(kh).T)
-        for i in range(lq):
-            at = seen[i]
-            if not at.any():
-                continue
-            si = s[i, at]
-            m = si.max()
-            p = np.exp(si - m)
-            w = p / p.sum()
-            out[i, h] = w @ vh[at]
-            lse[i, h] = m + np.log(p.sum())
-            e = u * (d * size[i, at].max() + 4 * np.abs(si).max() + n + 16)
-            tl[i, h] = e + u * 4 * abs(lse[i, h])
-            big = w @ np.abs(vh[at])
-            tol[i, h] = 2.0 ** -8 * np.abs(out[i, h]) + (2.0 ** -8 + 4 * e) * big
+        s = np.where(seen, scale * (q[:, h] @ kh.T), -np.inf)[some]
+        if not len(s):
+            continue
+        size = np.where(seen, scale * (np.abs(q[:, h]) @ np.abs(kh).T), 0.0)[some].max(1)
+        m = s.max(1)
+        p = np.exp(s - m[:, None])
+        total = p.sum(1)
+        w = p / total[:, None]
+        o, z = w @ vh, m + np.log(total)
+        logit = np.where(np.isfinite(s), np.abs(s), 0.0).max(1)
+        e = u * (d * size + 4 * logit + n + 16)
+        tl[some, h] = e + u * 4 * np.abs(z)
+        tol[some, h] = 2.0 ** -8 * np.abs(o) + (2.0 ** -8 + 4 * e[:, None]) * (w @ np.abs(vh)) + \
+            (n + 1) * 2.0 ** -126 * (1 + np.abs(vh).max())
+        out[some, h], lse[some, h] = o, z
     return out, lse, tol, tl
 
 

@@ -118,6 +118,26 @@ FORMS = {
                    False, False, 0),
 }
 
+# Enough work for the 256-row kernel (its own rule: tiles per CU), with what can go wrong in it
+MANY, MORE = (0,) * 14, (0,) * 28
+BLOCKS = {
+    "rows_80_and_6": (128, 16, 8, (1000, 65, 130), [MANY + (1, 2), (2,)], (40, 3), (5, 0), False, False, False, 0),
+    "rows_2_blocks": (128, 16, 8, (1000, 1), [(1,) + MANY, (1,), ()], (150, 33, 2), (0, 64, 3), False, False,
+                      False, 0),
+    "rows_300_64": (64, 16, 8, (1000, 65, 130), [MORE + (1, 2), (1,)], (150, 3), (4, 100), False, False, False, 0),
+    "long_own": (128, 8, 4, (700,), [(0,) * 38], (70,), (900,), False, False, False, 0),
+    "long_own_64": (64, 8, 8, (700,), [(0,) * 38], (70,), (900,), False, False, False, 0),
+    "starts_cross_only": (128, 16, 8, (1000, 65, 130), [MANY + (1, 2, 1), (1,)], (40, 60), None, True, False,
+                          False, 0),
+    "row_limits": (128, 16, 8, (1000, 65, 130), [MANY + (1, 2), (2,), (1, 0)], (140, 3, 40), None, False, True,
+                   False, 0),
+    "row_limits_64": (64, 16, 8, (1000, 65, 130), [MORE + (1, 2), (2,)], (140, 40), None, False, True, False, 0),
+    "row_limits_own": (128, 16, 8, (1000, 65, 130), [MANY + (1, 2), (2,)], (70, 40), (0, 70), True, True, False, 0),
+    "decode_pieces": (128, 64, 8, (1000, 65), [MANY + (1,), (1,)], (16, 9), (3, 0), False, False, True, 7),
+    "odd_group": (64, 24, 8, (1000, 33), [MORE + (1,)], (45,), (20,), False, False, False, 0),
+}
+FORMS.update(BLOCKS)
+
 
 class Call:
     """A batch's inputs on the host and the GPU, and its reference."""
@@ -166,8 +186,8 @@ class Call:
 
     def outputs(self):
         n = self.q.shape[0]
-        return (torch.full((n, self.hq, self.d), 77, dtype=torch.int16, device="cuda"),
-                torch.full((n, self.hq), 5.0, device="cuda"))
+        out = torch.full((n * self.hq * self.d + self.shift,), 77, dtype=torch.int16, device="cuda")
+        return (out[self.shift:].view(n, self.hq, self.d), torch.full((n, self.hq), 5.0, device="cuda"))
 
     def run(self, store, decode=None, pieces=None, entry=None, st=None):
         out, lse = self.outputs()
@@ -202,10 +222,14 @@ def test_link(form):
     c = Call(form)
     print(f"form {form}", flush=True)
     with c.store() as store:
-        check(c.run(store), c.reference())
+        pic.prof_begin()
+        got = c.run(store)
+        name = pic.prof_end()[2]
+        assert name == ("link_fp4_prefill_kernel" if form in BLOCKS else "link_fp4_kernel")
+        check(got, c.reference())
 
 
-@pytest.mark.parametrize("form", ["tails", "prefill_64", "limits_own"])
+@pytest.mark.parametrize("form", ["tails", "prefill_64", "limits_own", "rows_80_and_6", "rows_300_64"])
 def test_unaligned_tensors(form):
     c = Call(form, seed=1, shift=3)
     with c.store() as store:
@@ -224,13 +248,13 @@ def test_decode_as_prefill_and_any_pieces(form):
 
 @pytest.mark.parametrize("std", [1e-3, 40.0])
 def test_flat_and_sharp_softmax(std):
-    c = Call("tails", seed=3, q_std=std)
-    with c.store() as store:
-        check(c.run(store), c.reference())
-        check(c.run(store, decode=False), c.reference())
+    for form in ("tails", "rows_80_and_6", "odd_group"):
+        c = Call(form, seed=3, q_std=std)
+        with c.store() as store:
+            check(c.run(store), c.reference())
 
 
-@pytest.mark.parametrize("form", ["tails", "pieces", "limits_decode", "group_of_forty", "own_only"])
+@pytest.mark.parametrize("form", ["tails", "pieces", "limits_decode", "group_of_forty", "own_only", "decode_pieces"])
 def test_noalloc_returns_the_same_bits(form):
     c = Call(form, seed=4)
     with c.store() as store:
@@ -238,7 +262,7 @@ def test_noalloc_returns_the_same_bits(form):
         assert same(a[0], b[0]) and same(a[1], b[1])
 
 
-@pytest.mark.parametrize("form", ["tails", "prefill", "limits", "pieces"])
+@pytest.mark.parametrize("form", ["tails", "prefill", "limits", "pieces", "rows_2_blocks", "row_limits_64"])
 def test_plans_and_captured_runs_return_the_same_bits(form):
     c = Call(form, seed=5)
     with c.store() as store:
@@ -264,7 +288,7 @@ def test_plans_and_captured_runs_return_the_same_bits(form):
 
 
 def test_calls_in_flight_on_two_streams():
-    c, e = Call("prefill", seed=6), Call("pieces", seed=6)
+    c, e = Call("rows_80_and_6", seed=6), Call("pieces", seed=6)
     with c.store() as s1, e.store() as s2:
         torch.cuda.synchronize()
         streams = [torch.cuda.Stream(), torch.cuda.Stream()]
@@ -353,6 +377,77 @@ def test_layers_past_32_bits_of_offset():
         torch.cuda.synchronize()
         ref = M.attend(q, M.stored(k), M.stored(v), float(np.float32(0.1)), np.ones((2, n), bool))
         check((host(out), lse.cpu().numpy().astype(np.float64)), ref)
+
+
+def test_plan_of_every_layer():
+    """A plan's run on each layer, own KV of the layer, over a chunk with rows written in one."""
+    rng = np.random.default_rng(4)
+    d, hkv, n, layers = 64, 2, 130, 3
+    draw = lambda *s: M.bf16(rng.standard_normal(s))  # noqa: E731
+    k, v = draw(layers, n, hkv, d), draw(layers, n, hkv, d)
+    rows = np.array([0, 63, 64, 129], np.int32)
+    nk, nv = draw(4, hkv, d), draw(4, hkv, d)
+    q, ko, vo = draw(5, 6, d), draw(7, hkv, d), draw(7, hkv, d)
+    with pic.Store(pic.GQA, pic.FP4, hkv, d, d, 1024, n_layers=layers) as store:
+        store.put(1, n, dev(k), dev(v), stream())
+        store.derive(2, 1, rows, stream())
+        store.write_rows(2, 2, rows, dev(nk), dev(nv), stream())
+        args = ([0, 2, 3], [2, 1, 2], [0, 2, 5], [0, 4, 7])
+        with pic.LinkPlan(store, *args, 6, mode=pic.DECODE, chunk_starts=[64, 0, 128]) as plan:
+            sk, sv = M.stored(k), M.stored(v)
+            for l in range(layers):
+                out = torch.empty((5, 6, d), dtype=torch.int16, device="cuda")
+                lse = torch.empty((5, 6), device="cuda")
+                plan.run(l, dev(q), dev(ko), dev(vo), 0.125, out, lse, stream())
+                torch.cuda.synchronize()
+                two = (sk[l].copy(), sv[l].copy())
+                if l == 2:
+                    two[0][rows], two[1][rows] = M.stored(nk), M.stored(nv)
+                ref = M.batch(q, {1: (sk[l], sv[l]), 2: two}, [(2, 1), (2,)], [[64, 0], [128]], ko, vo,
+                              args[2], args[3], 0.125)
+                check((host(out), lse.cpu().numpy().astype(np.float64)), ref)
+
+
+def test_pages_of_removed_chunks_are_taken_whole():
+    """A short chunk on a page that held other rows: nothing of them is read."""
+    rng = np.random.default_rng(5)
+    d, hkv = 128, 1
+    big = np.full((64, hkv, d), np.nan)
+    k, v, q = (M.bf16(rng.standard_normal((3, hkv, d))) for _ in range(3))
+    with pic.Store(pic.GQA, pic.FP4, hkv, d, d, 64) as store:
+        store.put(1, 64, dev(big), dev(big), stream())
+        store.remove(1, stream())
+        store.put(2, 3, dev(k), dev(v), stream())
+        out = torch.empty((3, hkv, d), dtype=torch.int16, device="cuda")
+        lse = torch.empty((3, hkv), device="cuda")
+        pic.link_attn(store, [0, 1], [2], [0, 3], None, hkv, dev(q), None, None, 0.125, out, lse, stream=stream())
+        torch.cuda.synchronize()
+        check((host(out), lse.cpu().numpy().astype(np.float64)),
+              M.attend(q, M.stored(k), M.stored(v), 0.125, np.ones((3, 3), bool)))
+
+
+def test_another_process_links_the_exported_store():
+    import multiprocessing as mp
+
+    import fp4_ipc_child
+    rng = np.random.default_rng(6)
+    d, hkv, n = 128, 2, 100
+    k, v, q = (M.bf16(rng.standard_normal(s)) for s in ((n, hkv, d), (n, hkv, d), (4, 4, d)))
+    with pic.Store(pic.GQA, pic.FP4, hkv, d, d, 256) as store:
+        store.put(9, n, dev(k), dev(v), stream())
+        blob = store.export()
+        ctx = mp.get_context("spawn")
+        results = ctx.Queue()
+        child = ctx.Process(target=fp4_ipc_child.run, args=(blob, M.bits(q), results))
+        child.start()
+        try:
+            got = results.get(timeout=100)
+        finally:
+            child.join(timeout=15)
+        assert not isinstance(got, str), got
+        out = got[0].view(np.uint16).astype(np.uint32) << 16
+        check((out.view(np.float32).astype(np.float64), got[1].astype(np.float64)),
+              M.attend(q, M.stored(k), M.stored(v), 0.125, np.ones((4, n), bool)))
 
 
 def test_infinities_and_nan():
