@@ -278,8 +278,8 @@ pic_status pic_link_decode(pic_store *store, const pic_link_req *req, int32_t n_
  * event). The host tables are copied with hipMemcpyAsync from pageable
  * memory, which the runtime completes before returning (the host therefore
  * waits for the stream's earlier work). Small calls (at most 32 links and 8
- * requests, no per-query limits, any store but bf16 GQA of d 128 and bf16
- * MLA of 576 / 512) run the kernels pic_link_decode runs for them, which take
+ * requests, no per-query limits, any store but bf16 GQA of d 128, bf16
+ * MLA of 576 / 512 and 4-bit ones) run the kernels pic_link_decode runs for them, which take
  * the tables as a kernel argument and read the own KV in place: they use the
  * scratch for split partials only and copy nothing. Every kernel writes what
  * it later reads, so nothing in the scratch has to start at zero.
@@ -289,7 +289,7 @@ pic_status pic_link_decode(pic_store *store, const pic_link_req *req, int32_t n_
  * 64 MiB: its tables (32 B per link and for a request's own KV, 36 B per
  * request, 4 B per query token where limits differ), ceil(L_s / 64) * 64 own tokens *
  * H_kv * (d_k + d_v) * esize per request (also where the kernel reads them in
- * place), and Tq * H_q * splits * (d_v + 2) * 4 B when the keys are split, with
+ * place; nothing for a 4-bit store), and Tq * H_q * splits * (d_v + 2) * 4 B when the keys are split, with
  * one split count for all requests (num_splits, or for 0 about eight
  * workgroups per CU). Such a call launches nothing. A call within the charge
  * whose requests are cut into more pieces than that, or whose 64 B of work

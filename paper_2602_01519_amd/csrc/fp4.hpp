@@ -42,7 +42,6 @@ template <int D>
 struct Fp4Tile {
   static_assert(D == 64 || D == 128, "head widths of the 4-bit kernels");
   static constexpr int kBlocks = D / 32;                 // blocks of a row
-  static constexpr int kUnits = D / 32;                  // 16-byte units per lane, K or V
   static constexpr int kCode = D * 32;                   // bytes of K (or V) codes
   static constexpr int kV = kCode, kKs = 2 * kCode, kVs = kKs + 64 * kBlocks;
   static constexpr int kBytes = kVs + 64 * kBlocks;

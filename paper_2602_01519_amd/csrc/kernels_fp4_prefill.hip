@@ -19,8 +19,8 @@
 // positions of its operand of the second one by where V's keys are written.
 //
 // Softmax: log2 domain, against the running max as it stands; a tile is redone
-// against the new one when a lane's probabilities sum to more than 2^20 (the first
-// tile of a row always is). Sums are fp32 of the probabilities before they are rounded to
+// against the new one when a lane's probabilities sum to more than 2^20, and the
+// first tile in which a row sees a key always is. Sums are fp32 of the probabilities before they are rounded to
 // bf16 for the product.
 #include "fp4.hpp"
 
@@ -349,12 +349,19 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
     }
     return t0 + t1;
   };
-  float ts = probs();
-  if (__builtin_expect(__any(!(ts <= kJumpSum) || (a.m == -INFINITY && ts > 0.f)), 0)) {
-    float tmax = -INFINITY;
+  auto tile_max = [&]() {
+    float t = -INFINITY;
 #pragma unroll
-    for (int x = 0; x < 16; ++x) tmax = fmaxf(fmaxf(tmax, s0[x]), s1[x]);
-    tmax = half_swap_max(tmax);
+    for (int x = 0; x < 16; ++x) t = fmaxf(fmaxf(t, s0[x]), s1[x]);
+    return t;
+  };
+  float ts = probs();
+  bool redo = !(ts <= kJumpSum);
+  // A row that has seen no key yet and sees one here (its probabilities against a
+  // maximum of 0 may all be 0).
+  if (__builtin_expect(__any(a.m == -INFINITY), 0)) redo |= a.m == -INFINITY && tile_max() > -INFINITY;
+  if (__builtin_expect(__any(redo), 0)) {
+    const float tmax = half_swap_max(tile_max());
     const float mnew = fmaxf(a.m, tmax * sc);
     const float alpha = mnew == a.m ? 1.f : __builtin_amdgcn_exp2f(a.m - mnew);
     a.m = mnew;

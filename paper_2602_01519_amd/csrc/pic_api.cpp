@@ -986,11 +986,19 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     c.over = 2;
     c.min_piece = 1;
   } else if (kern == Kern::Fp4Prefill) {
+    // Tiles of 64 keys, every CU full: 1.9 us at 128, 2.4 at 64 (two workgroups to
+    // a CU; 1.5 for one alone). A shorter piece than four tiles writes more partial
+    // sums than it reads of the cache (one request of 148 rows over 110 tiles,
+    // pieces of 2 / 4 / 8 tiles: 40 / 29 / 33 us).
     us = d.d_k == 128 ? 1.9 : 2.2;
     c.slots = cus * fp4_prefill_blocks_per_cu(d.d_k);
     c.over = 3;
     c.min_piece = 4;
   } else if (kern == Kern::Fp4) {
+    // A wave's 64-key tile takes about 1 us alone; four waves of 128-wide heads to
+    // a CU (eight of 64-wide ones) already draw 6.4 TB/s at 1.4 us a tile, and more
+    // pieces only add partial sums (64 decode requests over 16 links of 1024, 1 / 2 /
+    // 3 / 4 / 8 pieces: 238 / 173 / 191 / 179 / 195 us).
     us = 1.4;
     c.slots = (d.d_k == 128 ? 4 : 8) * (int64_t)cus;
     c.over = 2;
@@ -2409,7 +2417,8 @@ pic_status pic_rope_create(const pic_rope_desc *desc, pic_rope **out) {
     return fail(PIC_ERR_UNSUPPORTED, "rot_dim is at most %d and head_dim at most 768", kRopeMost);
   const auto positive = [](double x) { return std::isfinite(x) && x > 0; };
   if (!positive(d.theta)) return fail(PIC_ERR_INVALID, "theta must be positive and finite");
-  if (!positive(d.magnitude)) return fail(PIC_ERR_INVALID, "magnitude must be positive and finite");
+  if (!positive((float)d.magnitude))
+    return fail(PIC_ERR_INVALID, "magnitude must be positive and finite in fp32");
   if (d.scaling < PIC_ROPE_PLAIN || d.scaling > PIC_ROPE_YARN)
     return fail(PIC_ERR_INVALID, "unknown scaling %d", d.scaling);
   if (d.scaling != PIC_ROPE_PLAIN && !positive(d.factor))
@@ -2447,6 +2456,11 @@ pic_status pic_rope_create(const pic_rope_desc *desc, pic_rope **out) {
       keep = 1 - (i - lo) / std::max(hi - lo, 0.001);
     keep = std::min(1.0, std::max(0.0, keep));
     r->rev[i] = (d.scaling == PIC_ROPE_PLAIN ? f : f * (keep + (1 - keep) / d.factor)) / pi2;
+    // (a position is at most 2^31)
+    if (!std::isfinite(r->rev[i] * 4294967296.0)) {
+      delete r;
+      return fail(PIC_ERR_INVALID, "theta and factor give an infinite frequency");
+    }
   }
   *out = r;
   return PIC_OK;

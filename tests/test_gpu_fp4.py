@@ -254,6 +254,19 @@ def test_flat_and_sharp_softmax(std):
             check(c.run(store), c.reference())
 
 
+@pytest.mark.parametrize("form", ["tails", "pieces", "rows_80_and_6", "rows_300_64", "row_limits"])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_logits_far_from_zero(form, sign):
+    """Every logit some hundreds below (above) zero: no probability may be formed against zero."""
+    c = Call(form, seed=9)
+    c.q = M.bf16(8 + 0.25 * c.q)
+    c.raw = {i: (M.bf16(sign * 8 + k), v) for i, (k, v) in c.raw.items()}
+    if c.k_own is not None:
+        c.k_own = M.bf16(sign * 8 + c.k_own)
+    with c.store() as store:
+        check(c.run(store), c.reference())
+
+
 @pytest.mark.parametrize("form", ["tails", "pieces", "limits_decode", "group_of_forty", "own_only", "decode_pieces"])
 def test_noalloc_returns_the_same_bits(form):
     c = Call(form, seed=4)
