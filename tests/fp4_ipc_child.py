@@ -13,7 +13,7 @@ def run(blob, q_bits, results):
         with pic.Store.import_(blob) as store:
             q = torch.from_numpy(q_bits).cuda()
             out = torch.empty_like(q)
-            lse = torch.empty(q.shape[:2], device="cuda")
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
             pic.link_attn(store, [0, 1], [9], [0, q.shape[0]], None, q.shape[1], q, None, None, 0.125, out, lse)
             torch.cuda.synchronize()
             results.put((out.cpu().numpy(), lse.cpu().numpy()))

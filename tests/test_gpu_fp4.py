@@ -187,7 +187,8 @@ class Call:
     def outputs(self):
         n = self.q.shape[0]
         out = torch.full((n * self.hq * self.d + self.shift,), 77, dtype=torch.int16, device="cuda")
-        return (out[self.shift:].view(n, self.hq, self.d), torch.full((n, self.hq), 5.0, device="cuda"))
+        return (out[self.shift:].view(n, self.hq, self.d), torch.full((n, self.hq), 5.0, dtype=torch.float32,
+                                                                   device="cuda"))
 
     def run(self, store, decode=None, pieces=None, entry=None, st=None):
         out, lse = self.outputs()
@@ -339,7 +340,7 @@ def test_fragmented_chunks(d):
         assert same(a, M.stored(k)) and same(b, M.stored(v))
         q = M.bf16(rng.standard_normal((3, 4, d)))
         out = torch.empty((3, 4, d), dtype=torch.int16, device="cuda")
-        lse = torch.empty((3, 4), device="cuda")
+        lse = torch.empty((3, 4), dtype=torch.float32, device="cuda")
         pic.link_attn(store, [0, 1], [9], [0, 3], None, 4, dev(q), None, None, 0.25, out, lse, stream=stream(),
                       chunk_starts=[64])
         torch.cuda.synchronize()
@@ -384,7 +385,7 @@ def test_layers_past_32_bits_of_offset():
         assert same(a, M.stored(k)) and same(b, M.stored(v))
         q = M.bf16(rng.standard_normal((2, hkv, d)))
         out = torch.empty((2, hkv, d), dtype=torch.int16, device="cuda")
-        lse = torch.empty((2, hkv), device="cuda")
+        lse = torch.empty((2, hkv), dtype=torch.float32, device="cuda")
         pic.link_decode(store, [0, 1], [3], [0, 2], None, hkv, dev(q), None, None, 0.1, out, lse,
                         stream=stream(), layer=layers - 1)
         torch.cuda.synchronize()
@@ -410,7 +411,7 @@ def test_plan_of_every_layer():
             sk, sv = M.stored(k), M.stored(v)
             for l in range(layers):
                 out = torch.empty((5, 6, d), dtype=torch.int16, device="cuda")
-                lse = torch.empty((5, 6), device="cuda")
+                lse = torch.empty((5, 6), dtype=torch.float32, device="cuda")
                 plan.run(l, dev(q), dev(ko), dev(vo), 0.125, out, lse, stream())
                 torch.cuda.synchronize()
                 two = (sk[l].copy(), sv[l].copy())
@@ -432,7 +433,7 @@ def test_pages_of_removed_chunks_are_taken_whole():
         store.remove(1, stream())
         store.put(2, 3, dev(k), dev(v), stream())
         out = torch.empty((3, hkv, d), dtype=torch.int16, device="cuda")
-        lse = torch.empty((3, hkv), device="cuda")
+        lse = torch.empty((3, hkv), dtype=torch.float32, device="cuda")
         pic.link_attn(store, [0, 1], [2], [0, 3], None, hkv, dev(q), None, None, 0.125, out, lse, stream=stream())
         torch.cuda.synchronize()
         check((host(out), lse.cpu().numpy().astype(np.float64)),
@@ -476,7 +477,7 @@ def test_infinities_and_nan():
     with pic.Store(pic.GQA, pic.FP4, 1, d, d, 128) as store:
         store.put(1, n, dev(k), dev(v), stream())
         out = torch.empty((3, 2, d), dtype=torch.int16, device="cuda")
-        lse = torch.empty((3, 2), device="cuda")
+        lse = torch.empty((3, 2), dtype=torch.float32, device="cuda")
         pic.link_attn(store, [0, 1], [1], [0, 3], None, 2, dev(q), None, None, 0.125, out, lse,
                       stream=stream(), q_doc_limits=[100, 90, 50])
         torch.cuda.synchronize()

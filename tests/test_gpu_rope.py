@@ -187,7 +187,7 @@ def test_positions_then_4_bit_cache_then_link():
         store.put(1, n, t["k"], t["v"], stream())
         rope.apply(lq, dp[n:], [(t["q"], t["q"], hq, 0, 0), (t["ko"], t["ko"], hkv, 0, 0)], stream=stream())
         out = torch.empty((lq, hq, d), dtype=torch.bfloat16, device="cuda")
-        lse = torch.empty((lq, hq), device="cuda")
+        lse = torch.empty((lq, hq), dtype=torch.float32, device="cuda")
         scale = float(np.float32(d ** -0.5))
         pic.link_attn(store, [0, 1], [1], [0, lq], [0, lq], hq, t["q"], t["ko"], t["vo"], scale, out, lse,
                       stream=stream())
