@@ -1080,6 +1080,26 @@ void apply_splits(pic_store *s, int32_t n_q_heads, int rows_per_block, Setup &C)
   // pieces 43 us).
   if ((C.kern == Kern::Mfma128 || C.kern == Kern::Fp4Prefill) && !P.doc_lim.empty() && lp.nrb > 1)
     lp.spread = 2;
+  // So do calls of the 4-bit kernel whose workgroups the GPU holds at once, and split
+  // calls of requests with different numbers of row blocks: what counts is that the CUs
+  // fill evenly, and among others the empty row blocks of short requests had some CU take
+  // two pieces while another had none. 8 requests of 30..300 tokens, 64-wide heads,
+  // 138 -> 107 us; 16 of 30..200 157 -> 115; 128-wide 233 -> 154; one of 500 tokens 67 -> 60.
+  // (In several rounds the order of the requests counts more: 16 requests of 512 tokens
+  // over 8..20 links 1772 us, spread 1910; 12 of 600 tokens, 64-wide, split, 612 against 642.)
+  if (C.kern == Kern::Fp4Prefill && lp.nrb > 1) {
+    int64_t filled = 0;
+    bool uneven = false;
+    for (int r = 0; r < B; ++r) {
+      const int64_t rows = (int64_t)P.reqs[r].lq * lp.group;
+      const int64_t n = (rows + rows_per_block - 1) / rows_per_block;
+      filled += C.req_splits[r] * n * lp.n_kv_heads;
+      uneven |= n != lp.nrb;
+    }
+    if ((C.splits > 1 && uneven) ||
+        filled <= (int64_t)s->shape.cus * fp4_prefill_blocks_per_cu(s->desc.d_k))
+      lp.spread = 2;
+  }
   C.part_rows = 0;
   C.comb.clear();
   if (C.splits > 1) {
