@@ -63,13 +63,17 @@ __device__ __forceinline__ float row_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-__device__ __forceinline__ uint4 load_nt(const char *p) {
-  const u32x4 w = __builtin_nontemporal_load((global_u32x4)p);
+template <bool kOnce>
+__device__ __forceinline__ uint4 load_codes(const char *p) {
+  const u32x4 w = kOnce ? __builtin_nontemporal_load((global_u32x4)p) : *(global_u32x4)p;
   return make_uint4(w.x, w.y, w.z, w.w);
 }
 
-// A 64-key tile of the cache as loaded.
-template <int D>
+// A 64-key tile of the cache as loaded. kOnce: its codes pass the caches by, as those
+// that nobody else reads should (64 decode requests with 16 documents of their own each,
+// 1 GB: 179 us, cached 210); where several row blocks read them, cached is faster (16
+// requests of 16 tokens over 4..12 of 64 documents, 51 -> 47 us, 64-wide heads 38 -> 34).
+template <int D, bool kOnce>
 struct CacheTile {
   static constexpr int kKeyBlocks = 4;
   uint4 k[D / 32], v[D / 32];
@@ -81,8 +85,8 @@ struct CacheTile {
     const int m = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) {
-      k[j] = load_nt(tile + j * 1024 + lane * 16);
-      v[j] = load_nt(tile + T::kV + j * 1024 + lane * 16);
+      k[j] = load_codes<kOnce>(tile + j * 1024 + lane * 16);
+      v[j] = load_codes<kOnce>(tile + T::kV + j * 1024 + lane * 16);
     }
     const int kc = D == 128 ? g : g >> 1;
     const int vc = m * (D / 16) / 32;
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
                     min(kTile, c.len - tt * kTile), c.tok0 + tt * kTile};
   };
   const int t_begin = it.t_begin, doc_end = min(it.t_end, R.doc_tiles);
-  CacheTile<D> ta, tb;
+  CacheTile<D, NB == 1> ta, tb;
   TileInfo ia{}, ib{};
   if (t_begin < doc_end) {
     ia = info(t_begin);
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     st.l[r] = 0.f;
   }
   const float sc = p.scale_log2;
-  auto doc_tile = [&](const CacheTile<D> &x, const TileInfo &i) {
+  auto doc_tile = [&](const CacheTile<D, NB == 1> &x, const TileInfo &i) {
     const bool masked = i.nvalid < kTile || (kLim && i.tok + kTile > dmin);
     int kl[NB];
 #pragma unroll
