@@ -1,12 +1,19 @@
-// Link attention over a 4-bit chunk cache on gfx950, one wave per piece of
-// work: 16 or 32 rows (query token x query head) of one kv head over a piece of a
-// request's keys. (32 where a request has more than 16: keys and values are widened
-// once for both blocks of 16; 16 requests of 32 rows 42 -> 32 us.)
+// Link attention over a 4-bit chunk cache on gfx950 for calls with few rows per kv
+// head: a workgroup takes 16 or 32 rows (query token x query head) of one kv head over a
+// piece of a request's keys, each of its four waves every fourth 64-key tile of it. (32
+// rows where a request has more than 16: keys and values are widened once for both
+// blocks of 16.)
+//
+// At the end the waves' states become one through LDS, and only then a partial is
+// written, or the output itself: with one wave per piece, four times as many partials
+// were written and combined (one request of 37 tokens over 112 tiles 26.2 -> 20.2 us, of
+// 16 tokens 18.9 -> 13.4; 64 decode requests over 8 shared documents, now in one piece, 76
+// -> 59; 64-wide heads, 37 tokens, 21.8 -> 14.0).
 //
 // Bound by the cache's bytes where a batch fills the GPU: 64 decode requests over 16
-// links of 1024 and 128 own tokens, 32/8 heads x 128, 1.18 GB in 174 us, 6.8 TB/s of
+// links of 1024 and 128 own tokens, 32/8 heads x 128, 1.18 GB in 171 us, 6.9 TB/s of
 // the 7.1 of a plain read stream. Else by the latency of a wave's tiles, about 1 us
-// each.
+// each, between some 3 us of start (tables, queries, first tile) and end.
 //
 // The tiles of the cache hold their codes in the order of the matrix
 // operands (fp4.hpp), so a wave streams them from HBM into registers, 1 KB per
@@ -256,6 +263,15 @@ __device__ __forceinline__ void compute_tile(const Tile &x, const bf16x8 (&qf)[N
   }
 }
 
+// LDS of the merge: per wave and row its output (rows 4 floats apart beyond their
+// length, so that 16 rows' chunks lie in different banks), maximum and sum.
+template <int D, int NB>
+struct Merge {
+  static constexpr int kRows = 16 * NB, kStride = D + 4;
+  static constexpr int kMax = kWaves * kRows * kStride, kSum = kMax + kWaves * kRows;
+  static constexpr int kFloats = kSum + kWaves * kRows;
+};
+
 struct TileInfo {
   const char *p;
   int nvalid, tok;
@@ -264,13 +280,15 @@ struct TileInfo {
 // kLim: rows see different numbers of linked rows.
 template <int D, bool kLim, int NB>
 __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
+  typedef Merge<D, NB> M;
+  __shared__ __align__(16) float lds[M::kFloats];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // Row blocks of a unit (item, kv head) are neighbours: they read the same tiles at
-  // about the same time, mostly from one workgroup. (Workgroups of as many waves as a
-  // unit has row blocks leave SIMDs idle: two of two waves each share two of the
-  // four; 16 requests of 64 rows, 51 -> 40 us.)
-  const int w = blockIdx.x * kWaves + wave, u = w / p.nrb, rb = w % p.nrb;
+  // Row blocks of a unit (item, kv head) are neighbours on one XCD: they read the same
+  // tiles at about the same time. (In the order of the launch: 20.2 -> 18.6 us for one
+  // request of 37 tokens, 189 -> 182 for 32 of 16 over 16 documents of their own.)
+  const UnitBlock ub = unit_of_block(blockIdx.x, p.nrb, p.n_xcd, 0, p.n_items * p.n_kv_heads);
+  const int u = ub.u, rb = ub.rb;
   if (u >= p.n_items * p.n_kv_heads) return;
   const int kvh = u % p.n_kv_heads;
   const WorkItem it = load_item(p.items, u / p.n_kv_heads);
@@ -311,11 +329,12 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     return TileInfo{c.base + ((int64_t)tt * p.n_kv_heads + kvh) * Fp4Tile<D>::kBytes,
                     min(kTile, c.len - tt * kTile), c.tok0 + tt * kTile};
   };
-  const int t_begin = it.t_begin, doc_end = min(it.t_end, R.doc_tiles);
+  // this wave's tiles: every fourth
+  const int t_first = it.t_begin + wave, doc_end = min(it.t_end, R.doc_tiles);
   CacheTile<D, NB == 1> ta, tb;
   TileInfo ia{}, ib{};
-  if (t_begin < doc_end) {
-    ia = info(t_begin);
+  if (t_first < doc_end) {
+    ia = info(t_first);
     ta.load(ia.p, lane);
   }
   bf16x8 qf[NB][D / 32];
@@ -342,23 +361,24 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     for (int r = 0; r < NB; ++r) kl[r] = (kLim ? min(i.nvalid, dl[r] - i.tok) : i.nvalid) - 1;
     compute_tile<D, NB>(x, qf, st, lane, masked, kl, sc);
   };
-  // The load past the last tile reads the last one again, which keeps the
+  // The load past the last tile reads the piece's last one, which keeps the
   // loop free of branches around loads (the compiler waits for every load in
   // flight where such paths meet).
-  for (int t = t_begin; t < doc_end; t += 2) {
-    ib = info(min(t + 1, doc_end - 1));
+  for (int t = t_first; t < doc_end; t += 2 * kWaves) {
+    ib = info(min(t + kWaves, doc_end - 1));
     tb.load(ib.p, lane);
     doc_tile(ta, ia);
-    if (t + 1 >= doc_end) break;
-    ia = info(min(t + 2, doc_end - 1));
+    if (t + kWaves >= doc_end) break;
+    ia = info(min(t + 2 * kWaves, doc_end - 1));
     ta.load(ia.p, lane);
     doc_tile(tb, ib);
   }
   // Own tiles up to the one that holds the block's last visible key.
   const int last_qi = (min(row0 + 16 * NB, nrows) - 1) / group;
   const int t_end = min(it.t_end, visible_tiles(R, last_qi));
-  const int own0 = max(t_begin, R.doc_tiles);
-  if (own0 < t_end) {
+  int own = max(it.t_begin, R.doc_tiles);
+  own += (t_first - own) & (kWaves - 1);
+  if (own < t_end) {
     int s0 = it.tok0;             // the own link's: its first own row
     if (it.tile0 < R.doc_tiles) {
       while (c.tile0 < R.doc_tiles) c.next();
@@ -366,47 +386,82 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     }
     const int64_t at = ((int64_t)s0 * p.n_kv_heads + kvh) * D * 2;
     const int64_t stride = (int64_t)p.n_kv_heads * D * 2;
-    const int k_end = min(R.ls, (t_end - R.doc_tiles) * kTile);
-    for (int j0 = (own0 - R.doc_tiles) * kTile; j0 < k_end; j0 += 32) {
-      OwnTile<D> x;
-      x.load((const char *)p.k_self + at, (const char *)p.v_self + at, stride, j0, R.ls - 1, lane);
-      int kl[NB];
+    for (; own < t_end; own += kWaves) {
+      const int k0 = (own - R.doc_tiles) * kTile, k_end = min(R.ls, k0 + kTile);
+      for (int j0 = k0; j0 < k_end; j0 += 32) {
+        OwnTile<D> x;
+        x.load((const char *)p.k_self + at, (const char *)p.v_self + at, stride, j0, R.ls - 1, lane);
+        int kl[NB];
 #pragma unroll
-      for (int r = 0; r < NB; ++r) kl[r] = min(own_last[r], R.ls - 1) - j0;
-      compute_tile<D, NB>(x, qf, st, lane, true, kl, sc);
+        for (int r = 0; r < NB; ++r) kl[r] = min(own_last[r], R.ls - 1) - j0;
+        compute_tile<D, NB>(x, qf, st, lane, true, kl, sc);
+      }
     }
   }
 
+  // The waves' states of each row become one: its largest maximum M, sums and outputs
+  // times 2^(m - M), added in the order of the waves.
+  float *const mb = lds + M::kMax, *const lb = lds + M::kSum;
 #pragma unroll
   for (int r = 0; r < NB; ++r) {
     const float ltot = row_sum(st.l[r]);
-    if (!rvalid[r]) continue;
-    if (it.part < 0) {
-      const float inv = ltot > 0.f ? 1.f / ltot : 0.f;
-      uint16_t *out = (uint16_t *)p.out + orow[r] * D;
+    st.m[r] = partial_max(st.m[r], ltot);
+    if (g == 0) {
+      mb[wave * M::kRows + 16 * r + n] = st.m[r];
+      lb[wave * M::kRows + 16 * r + n] = ltot;
+    }
+  }
+  __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        __bf16 v[D / 16];
+  for (int r = 0; r < NB; ++r) {
+    float top = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < D / 16; ++b) v[b] = (__bf16)(st.o[r][b][i] * inv);
-        if constexpr (D == 128)
-          *(uint4 *)(out + 8 * (4 * g + i)) = __builtin_bit_cast(uint4, v);
-        else
-          *(uint2 *)(out + 4 * (4 * g + i)) = __builtin_bit_cast(uint2, v);
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mb[w * M::kRows + 16 * r + n]);
+    const float f = __builtin_amdgcn_exp2f(st.m[r] - top);
+    float *row = lds + (wave * M::kRows + 16 * r + n) * M::kStride + D / 4 * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int b = 0; b < D / 16; b += 4) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);      // (a wave that saw no key: not times 0)
+        if (st.m[r] != -INFINITY)
+          v = make_float4(st.o[r][b][i] * f, st.o[r][b + 1][i] * f, st.o[r][b + 2][i] * f,
+                          st.o[r][b + 3][i] * f);
+        *(float4 *)(row + D / 16 * i + b) = v;
       }
-      if (p.lse && g == 0) p.lse[orow[r]] = ltot == 0.f ? -INFINITY : log_sum(st.m[r], ltot);
+  }
+  __syncthreads();
+  // four channels of a row per thread and step
+  for (int e = threadIdx.x; e < M::kRows * (D / 4); e += 64 * kWaves) {
+    const int row = e / (D / 4), ch = e % (D / 4) * 4;
+    if (row0 + row >= nrows) break;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mb[w * M::kRows + row]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float m = mb[w * M::kRows + row];
+      if (m != -INFINITY) sum += lb[w * M::kRows + row] * __builtin_amdgcn_exp2f(m - top);
+      const float4 x = *(const float4 *)(lds + (w * M::kRows + row) * M::kStride + ch);
+      o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+    }
+    const int q = (row0 + row) / group;
+    const int64_t in_req = (int64_t)q * p.n_q_heads + kvh * group + (row0 + row) % group;
+    const int64_t to = (int64_t)R.q0 * p.n_q_heads + in_req;
+    if (it.part < 0) {
+      const float inv = sum > 0.f ? 1.f / sum : 0.f;
+      bf16x4v v;
+      v[0] = (__bf16)(o.x * inv), v[1] = (__bf16)(o.y * inv);
+      v[2] = (__bf16)(o.z * inv), v[3] = (__bf16)(o.w * inv);
+      *(uint2 *)((uint16_t *)p.out + to * D + ch) = __builtin_bit_cast(uint2, v);
+      if (p.lse && ch == 0) p.lse[to] = sum == 0.f ? -INFINITY : log_sum(top, sum);
     } else {
-      const int64_t prow = it.part + (orow[r] - (int64_t)R.q0 * p.n_q_heads);
-      float *po = p.part_o + prow * D;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int b = 0; b < D / 16; b += 4)
-          *(float4 *)(po + (D / 16) * (4 * g + i) + b) =
-              make_float4(st.o[r][b][i], st.o[r][b + 1][i], st.o[r][b + 2][i], st.o[r][b + 3][i]);
-      if (g == 0) {
-        p.part_m[prow] = partial_max(st.m[r], ltot);
-        p.part_l[prow] = ltot;
+      const int64_t prow = it.part + in_req;
+      *(float4 *)(p.part_o + prow * D + ch) = o;
+      if (ch == 0) {
+        p.part_m[prow] = partial_max(top, sum);
+        p.part_l[prow] = sum;
       }
     }
   }
@@ -426,8 +481,8 @@ int fp4_rows_per_block(int max_rows) { return max_rows <= 16 ? 16 : 32; }
 
 hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **name) {
   *name = "link_fp4_kernel";
-  const int64_t units = (int64_t)p.n_items * p.n_kv_heads * p.nrb;
-  const dim3 grid((unsigned)((units + kWaves - 1) / kWaves)), block(64 * kWaves);
+  const int64_t units = (int64_t)p.n_items * p.n_kv_heads;
+  const dim3 grid((unsigned)unit_blocks(units, p.nrb, p.n_xcd, 0)), block(64 * kWaves);
   const bool two = fp4_rows_per_block(p.max_rows) == 32;
   if (p.d_k == 128)
     two ? launch<128, 2>(p, grid, block, st) : launch<128, 1>(p, grid, block, st);

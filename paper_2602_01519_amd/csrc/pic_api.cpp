@@ -14,6 +14,7 @@
 #include <map>
 #include <initializer_list>
 #include <mutex>
+#include <numeric>
 #include <string>
 #include <unordered_map>
 #include <vector>
@@ -935,23 +936,27 @@ bool small_tables(const Plan &P) {
 // gains; fp32 gains or loses with how its split count falls.
 constexpr int kStreamSmallRows = 128;
 
-// Calls of a 4-bit store that the one-wave kernel takes: at most kFp4FewRows rows
-// per kv head (16 requests of 64 rows, 128-wide heads, over 4..12 links: 45 us, in 256-row
-// workgroups 80), or work that leaves those workgroups too few tiles each to
-// cover their start, counted in tiles per CU. One wave against 256 rows, 32/8
-// heads, us: one request of 148 / 256 / 384 rows over 110 tiles 25 / 26 / 35
-// against 26 / 32 / 34 (3.4, 3.4 and 6.9 tiles per CU), over 220 tiles 30 / 33 / 45
-// against 31 / 36 / 40; 4 requests of 148 rows over 110 tiles (13.8) 42 against 38.
-// 64-wide heads: one request of 512 rows over 110 tiles (6.9) 29 against 36, over 220
-// (13.8) 39 against 42; 4 requests of 256 rows over 110 (13.8) 40 against 39.
-constexpr int kFp4FewRows = 64;
-bool fp4_one_wave(const Plan &P, const pic_store_desc &d, int group, int cus) {
-  if (P.max_rows <= kFp4FewRows) return true;
+// Calls of a 4-bit store that the few-row kernel takes: those whose rows fill little of
+// 256-row blocks, at most four and a half 32-row blocks of them (16 requests over 10 links of 300..1024, 128-wide heads, of 48 / 96 / 128 rows: 52 /
+// 80 / 84 us, in 256-row workgroups 90 / 96 / 99; 64-wide 36 / 55 / 57 against 53 / 57 / 60;
+// 32 requests of 64..192 rows 174 against 194, 16 of 40..240, 5.4 blocks, 111 against 101),
+// or work that leaves those workgroups too few tiles each to cover their start, counted in
+// tiles per CU. Few-row against 256-row kernel, 32/8 heads x 128, us: one request of 256
+// rows, 3.8 / 7.1 tiles per CU 25 / 34 against 36 / 39; of 384 rows, 7.6 / 14.2 tiles 33 / 50
+// against 37 / 46; 8 requests of 192 rows, 11.3 / 28.8 tiles 40 / 81 against 41 / 73. 64-wide
+// heads: one of 512 rows, 7.6 / 14.2 tiles 26 / 38 against 38 / 45; 4 of 512 rows, 11.2 / 30.9
+// / 58 tiles 29 / 58 / 102 against 40 / 60 / 92.
+bool fp4_few_rows(const Plan &P, const pic_store_desc &d, int group, int cus) {
   const int block = fp4_prefill_rows_per_block();
-  int64_t tiles = 0;
-  for (const ReqEntry &R : P.reqs)
-    tiles += (int64_t)d.n_kv_heads * (((int64_t)R.lq * group + block - 1) / block) * R.tiles;
-  return tiles <= (int64_t)cus * (d.d_k == 128 ? 6 : 12);
+  int64_t tiles = 0, blocks = 0;       // key tiles of the 256-row blocks, of the 32-row ones
+  for (const ReqEntry &R : P.reqs) {
+    const int64_t rows = (int64_t)R.lq * group;
+    tiles += (rows + block - 1) / block * R.tiles;
+    blocks += (rows + 31) / 32 * R.tiles;
+  }
+  if (2 * blocks <= 9 * tiles) return true;
+  tiles *= d.n_kv_heads;
+  return tiles <= (int64_t)cus * (d.d_k == 128 ? 12 : 24);
 }
 
 // Costs of a kernel's pieces in its tiles (see choose_splits). Tile times on
@@ -959,9 +964,10 @@ bool fp4_one_wave(const Plan &P, const pic_store_desc &d, int group, int cus) {
 // decode 5 us per wave (32 keys, eight waves per CU on the HBM stream),
 // stream kernel below. Partials move at about 4 TB/s, written and read; a
 // combine launch is about 4.5 us.
-// uneven_rows: some request has fewer row blocks than another.
+// uneven_rows: some request has fewer row blocks than another. units: the call's
+// workgroups before any split.
 SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t max_rows,
-                     const StreamShape &ss, bool uneven_rows) {
+                     const StreamShape &ss, bool uneven_rows, int64_t units) {
   const double part_us = (d.d_v + 2) * 8.0 / 4e6;
   SplitCost c{};
   c.max_splits = 256;
@@ -995,14 +1001,17 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     c.over = 3;
     c.min_piece = 4;
   } else if (kern == Kern::Fp4) {
-    // A wave's 64-key tile takes about 1 us alone; four waves of 128-wide heads to
-    // a CU (eight of 64-wide ones) already draw 6.4 TB/s at 1.4 us a tile, and more
-    // pieces only add partial sums (64 decode requests over 16 links of 1024, 1 / 2 /
-    // 3 / 4 / 8 pieces: 238 / 173 / 191 / 179 / 195 us).
-    us = 1.4;
-    c.slots = (d.d_k == 128 ? 4 : 8) * (int64_t)cus;
-    c.over = 2;
-    c.min_piece = 1;
+    // Four waves share a piece: 0.35 us per 64-key tile, about 3 us of start, merge and
+    // stores. Two workgroups to a CU, but one of 32-row blocks where there are fewer of
+    // them than CUs, whose waves' matrix and vector work fills a SIMD (requests of 37
+    // and 16 tokens over 112 tiles, 128-wide: 19.8 and 22.4 us, in pieces for two 22.2 and
+    // 24.8; 16 requests of 16 tokens, 256 units: for two 43, for one 50). A piece of fewer
+    // than four tiles leaves waves idle (one decode request over 33 tiles, pieces of
+    // 4 / 2 tiles: 8.3 / 8.8 us).
+    us = 0.35;
+    c.slots = (max_rows > 16 && units < cus ? 1 : 2) * (int64_t)cus;
+    c.over = 10;
+    c.min_piece = 4;
   } else {
     // Cycles of a wave's 32-key tile. fp32: D / 16 x 16 matrix instructions of
     // 32 cycles per 16 rows. bf16: 22 per row. Measured, 8 requests x 512 tokens
@@ -1080,24 +1089,23 @@ void apply_splits(pic_store *s, int32_t n_q_heads, int rows_per_block, Setup &C)
   // pieces 43 us).
   if ((C.kern == Kern::Mfma128 || C.kern == Kern::Fp4Prefill) && !P.doc_lim.empty() && lp.nrb > 1)
     lp.spread = 2;
-  // So do calls of the 4-bit kernel whose workgroups the GPU holds at once, and split
-  // calls of requests with different numbers of row blocks: what counts is that the CUs
-  // fill evenly, and among others the empty row blocks of short requests had some CU take
-  // two pieces while another had none. 8 requests of 30..300 tokens, 64-wide heads,
-  // 138 -> 107 us; 16 of 30..200 157 -> 115; 128-wide 233 -> 154; one of 500 tokens 67 -> 60.
-  // (In several rounds the order of the requests counts more: 16 requests of 512 tokens
-  // over 8..20 links 1772 us, spread 1910; 12 of 600 tokens, 64-wide, split, 612 against 642.)
+  // So do calls of the 4-bit kernel whose workgroups the GPU holds at once, and those
+  // with empty row blocks, if they are split or more than a third is empty: what counts
+  // is that the CUs fill evenly, and among others the empty ones had some CU take two pieces
+  // while another had none. 8 requests of 30..300 tokens, 64-wide heads, 138 -> 107 us; 16 of
+  // 30..200 157 -> 115, 128-wide 233 -> 154; 24 of 4..200, unsplit, 487 -> 339; one of 500
+  // tokens 67 -> 60. (In several rounds the order of the requests counts more: 16 requests
+  // of 512 tokens over 8..20 links 1772 us, spread 1910; of 400..600 881 against 946; 12 of
+  // 600, 64-wide, split, 612 against 642.)
   if (C.kern == Kern::Fp4Prefill && lp.nrb > 1) {
+    const int64_t all = (int64_t)C.n_items * lp.nrb * lp.n_kv_heads;
     int64_t filled = 0;
-    bool uneven = false;
     for (int r = 0; r < B; ++r) {
       const int64_t rows = (int64_t)P.reqs[r].lq * lp.group;
-      const int64_t n = (rows + rows_per_block - 1) / rows_per_block;
-      filled += C.req_splits[r] * n * lp.n_kv_heads;
-      uneven |= n != lp.nrb;
+      filled += (rows + rows_per_block - 1) / rows_per_block * C.req_splits[r] * lp.n_kv_heads;
     }
-    if ((C.splits > 1 && uneven) ||
-        filled <= (int64_t)s->shape.cus * fp4_prefill_blocks_per_cu(s->desc.d_k))
+    if (filled <= (int64_t)s->shape.cus * fp4_prefill_blocks_per_cu(s->desc.d_k) ||
+        (C.splits > 1 ? filled < all : 3 * filled < 2 * all))
       lp.spread = 2;
   }
   C.part_rows = 0;
@@ -1217,7 +1225,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   // per-row masks of the flash kernel
   if (kern == Kern::Decode128 && !P.doc_lim.empty()) kern = Kern::Mfma128;
   if (d.dtype == PIC_BF16 && mla && d.d_k == 576 && d.d_v == 512) kern = Kern::Mla;
-  if (fp4) kern = fp4_one_wave(P, d, lp.group, s->shape.cus) ? Kern::Fp4 : Kern::Fp4Prefill;
+  if (fp4) kern = fp4_few_rows(P, d, lp.group, s->shape.cus) ? Kern::Fp4 : Kern::Fp4Prefill;
   // A small generic call of a shape the lean kernel is built for (tables as
   // a kernel argument, at most kLeanTiles tiles in all) runs it; other fp32
   // and narrow bf16 GQA calls stream their keys through the matrix cores.
@@ -1283,7 +1291,8 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
       C.req_splits.assign(B, num_splits);
     else
       C.req_splits = choose_splits(tiles, blocks, rows, share,
-                                   split_cost(kern, s->shape.cus, d, P.max_rows, ss, uneven_rows));
+                                   split_cost(kern, s->shape.cus, d, P.max_rows, ss, uneven_rows,
+                                              std::accumulate(blocks.begin(), blocks.end(), int64_t{0})));
     apply_splits(s, n_q_heads, rows_per_block, C);
     while (!given && C.part_bytes > kMostPartBytes && C.splits > 1) fewer_pieces(s, n_q_heads, C);
     // A decode call that the no-alloc entry takes (by its charge) fits its

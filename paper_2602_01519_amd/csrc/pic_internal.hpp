@@ -457,8 +457,8 @@ StreamShape stream_shape(int dtype, int d, int max_rows, bool small);
 hipError_t launch_link_stream(const LinkParams &p, int dtype, int rows, hipStream_t st,
                               const char **name);
 
-// Link attention over a 4-bit store, d_k = d_v in {64, 128}: one wave per 16 or
-// 32 rows and piece, or 256 rows per workgroup.
+// Link attention over a 4-bit store, d_k = d_v in {64, 128}: 16 or 32 rows per
+// workgroup, whose waves share the keys, or 256 rows.
 hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **name);
 int fp4_rows_per_block(int max_rows);
 hipError_t launch_link_fp4_prefill(const LinkParams &p, hipStream_t st, const char **name);

@@ -118,7 +118,7 @@ FORMS = {
                    False, False, 0),
 }
 
-# Enough work for the 256-row kernel (its own rule: tiles per CU), with what can go wrong in it
+# More work, with what can go wrong in long calls
 MANY, MORE = (0,) * 14, (0,) * 28
 BLOCKS = {
     "rows_80_and_6": (128, 16, 8, (1000, 65, 130), [MANY + (1, 2), (2,)], (40, 3), (5, 0), False, False, False, 0),
@@ -136,7 +136,26 @@ BLOCKS = {
     "decode_pieces": (128, 64, 8, (1000, 65), [MANY + (1,), (1,)], (16, 9), (3, 0), False, False, True, 7),
     "odd_group": (64, 24, 8, (1000, 33), [MORE + (1,)], (45,), (20,), False, False, False, 0),
 }
+# Enough rows and work for the 256-row kernel (more than 128 rows, 12 tiles per CU or 24 of
+# 64-wide heads; two of the forms above have them, too)
+M25, M50 = (0,) * 26, (0,) * 50
+WIDE = {
+    "rows_160_and_6": (128, 16, 8, (1000, 65, 130), [M25 + (1, 2), (2,)], (80, 3), (5, 0), False, False, False, 0),
+    "own_900": (128, 8, 4, (700,), [(0,) * 75], (70,), (900,), False, False, False, 0),
+    "own_900_64": (64, 8, 8, (700,), [(0,) * 76], (140,), (900,), False, False, False, 0),
+    "starts_blocks": (128, 16, 8, (1000, 65, 130), [M25 + (1, 2, 1), (1,)], (70, 60), None, True, False, False, 0),
+    "row_limits_own_blocks": (128, 16, 8, (1000, 65, 130), [M25 + (1, 2), (2,)], (70, 40), (0, 70), True, True,
+                              False, 0),
+    "decode_blocks": (128, 128, 8, (1000, 65), [M25 + (1,), (1,)], (16, 9), (3, 0), False, False, True, 7),
+    "row_limits_blocks": (128, 16, 8, (1000, 65, 130), [MANY + (1, 2), (2,), (1, 0)], (200, 3, 40), None, False, True,
+                          False, 0),
+    "row_limits_blocks_64": (64, 16, 8, (1000, 65, 130), [MORE + (1, 2), (2,)], (170, 40), None, False, True, False,
+                             0),
+    "odd_group_blocks": (64, 24, 8, (1000, 33), [M50 + (1,)], (45,), (20,), False, False, False, 0),
+}
 FORMS.update(BLOCKS)
+FORMS.update(WIDE)
+ROWS_256 = ["rows_2_blocks", "rows_300_64"] + list(WIDE)
 
 
 class Call:
@@ -226,11 +245,11 @@ def test_link(form):
         pic.prof_begin()
         got = c.run(store)
         name = pic.prof_end()[2]
-        assert name == ("link_fp4_prefill_kernel" if form in BLOCKS else "link_fp4_kernel")
+        assert name == ("link_fp4_prefill_kernel" if form in ROWS_256 else "link_fp4_kernel")
         check(got, c.reference())
 
 
-@pytest.mark.parametrize("form", ["tails", "prefill_64", "limits_own", "rows_80_and_6", "rows_300_64"])
+@pytest.mark.parametrize("form", ["tails", "prefill_64", "limits_own", "rows_80_and_6", "rows_300_64", "own_900"])
 def test_unaligned_tensors(form):
     c = Call(form, seed=1, shift=3)
     with c.store() as store:
@@ -249,13 +268,14 @@ def test_decode_as_prefill_and_any_pieces(form):
 
 @pytest.mark.parametrize("std", [1e-3, 40.0])
 def test_flat_and_sharp_softmax(std):
-    for form in ("tails", "rows_80_and_6", "odd_group"):
+    for form in ("tails", "rows_80_and_6", "odd_group", "rows_160_and_6", "odd_group_blocks"):
         c = Call(form, seed=3, q_std=std)
         with c.store() as store:
             check(c.run(store), c.reference())
 
 
-@pytest.mark.parametrize("form", ["tails", "pieces", "rows_80_and_6", "rows_300_64", "row_limits"])
+@pytest.mark.parametrize("form", ["tails", "pieces", "rows_80_and_6", "rows_300_64", "row_limits", "rows_160_and_6",
+                                  "row_limits_blocks"])
 @pytest.mark.parametrize("sign", [-1, 1])
 def test_logits_far_from_zero(form, sign):
     """Every logit some hundreds below (above) zero: no probability may be formed against zero."""
@@ -268,7 +288,8 @@ def test_logits_far_from_zero(form, sign):
         check(c.run(store), c.reference())
 
 
-@pytest.mark.parametrize("form", ["tails", "pieces", "limits_decode", "group_of_forty", "own_only", "decode_pieces"])
+@pytest.mark.parametrize("form", ["tails", "pieces", "limits_decode", "group_of_forty", "own_only", "decode_pieces",
+                                  "decode_blocks"])
 def test_noalloc_returns_the_same_bits(form):
     c = Call(form, seed=4)
     with c.store() as store:
@@ -276,7 +297,8 @@ def test_noalloc_returns_the_same_bits(form):
         assert same(a[0], b[0]) and same(a[1], b[1])
 
 
-@pytest.mark.parametrize("form", ["tails", "prefill", "limits", "pieces", "rows_2_blocks", "row_limits_64"])
+@pytest.mark.parametrize("form", ["tails", "prefill", "limits", "pieces", "rows_2_blocks", "row_limits_64",
+                                  "row_limits_blocks_64"])
 def test_plans_and_captured_runs_return_the_same_bits(form):
     c = Call(form, seed=5)
     with c.store() as store:
@@ -302,7 +324,7 @@ def test_plans_and_captured_runs_return_the_same_bits(form):
 
 
 def test_calls_in_flight_on_two_streams():
-    c, e = Call("rows_80_and_6", seed=6), Call("pieces", seed=6)
+    c, e = Call("rows_160_and_6", seed=6), Call("pieces", seed=6)
     with c.store() as s1, e.store() as s2:
         torch.cuda.synchronize()
         streams = [torch.cuda.Stream(), torch.cuda.Stream()]
