@@ -300,7 +300,7 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   // this lane's rows
   const int n = lane & 15, g = lane >> 4;
   bool rvalid[NB];
-  int own_last[NB], dl[NB], dmin = kNoLimit;                // own_last: last visible own key
+  int own_last[NB], dl[NB], dmin = kNoLimit, dmax = 0;                // own_last: last visible own key
   int64_t orow[NB];
 #pragma unroll
   for (int r = 0; r < NB; ++r) {
@@ -313,12 +313,17 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
     if (kLim) {
       if (rvalid[r]) dl[r] = p.doc_lim[R.q0 + qi];
       dmin = min(dmin, dl[r]);
+      dmax = max(dmax, rvalid[r] ? dl[r] : 0);
     }
   }
   if (kLim) {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) dmin = min(dmin, __shfl_xor(dmin, o));
+    for (int o = 8; o > 0; o >>= 1) {
+      dmin = min(dmin, __shfl_xor(dmin, o));
+      dmax = max(dmax, __shfl_xor(dmax, o));
+    }
     dmin = __builtin_amdgcn_readfirstlane(dmin);
+    dmax = __builtin_amdgcn_readfirstlane(dmax);
   }
 
   LinkCursor<true> c;
@@ -363,12 +368,13 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   };
   // The load past the last tile reads the piece's last one, which keeps the
   // loop free of branches around loads (the compiler waits for every load in
-  // flight where such paths meet).
+  // flight where such paths meet). It ends where no row sees a linked one any more.
   for (int t = t_first; t < doc_end; t += 2 * kWaves) {
+    if (kLim && ia.tok >= dmax) break;
     ib = info(min(t + kWaves, doc_end - 1));
     tb.load(ib.p, lane);
     doc_tile(ta, ia);
-    if (t + kWaves >= doc_end) break;
+    if (t + kWaves >= doc_end || (kLim && ib.tok >= dmax)) break;
     ia = info(min(t + 2 * kWaves, doc_end - 1));
     ta.load(ia.p, lane);
     doc_tile(tb, ib);

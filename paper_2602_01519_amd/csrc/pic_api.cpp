@@ -937,15 +937,16 @@ bool small_tables(const Plan &P) {
 constexpr int kStreamSmallRows = 128;
 
 // Calls of a 4-bit store that the few-row kernel takes: those whose rows fill little of
-// 256-row blocks, at most four and a half 32-row blocks of them (16 requests over 10 links of 300..1024, 128-wide heads, of 48 / 96 / 128 rows: 52 /
-// 80 / 84 us, in 256-row workgroups 90 / 96 / 99; 64-wide 36 / 55 / 57 against 53 / 57 / 60;
-// 32 requests of 64..192 rows 174 against 194, 16 of 40..240, 5.4 blocks, 111 against 101),
-// or work that leaves those workgroups too few tiles each to cover their start, counted in
-// tiles per CU. Few-row against 256-row kernel, 32/8 heads x 128, us: one request of 256
-// rows, 3.8 / 7.1 tiles per CU 25 / 34 against 36 / 39; of 384 rows, 7.6 / 14.2 tiles 33 / 50
-// against 37 / 46; 8 requests of 192 rows, 11.3 / 28.8 tiles 40 / 81 against 41 / 73. 64-wide
-// heads: one of 512 rows, 7.6 / 14.2 tiles 26 / 38 against 38 / 45; 4 of 512 rows, 11.2 / 30.9
-// / 58 tiles 29 / 58 / 102 against 40 / 60 / 92.
+// 256-row blocks, at most four and a half 32-row blocks of them (16 requests over 10 links
+// of 300..1024, 128-wide heads, of 48 / 96 / 128 rows: 52 / 80 / 84 us, in 256-row workgroups
+// 90 / 96 / 99; 64-wide 36 / 55 / 57 against 53 / 57 / 60; 32 requests of 64..192 rows 174
+// against 194, 16 of 40..240, 5.4 blocks, 111 against 101), or work that leaves those
+// workgroups too few tiles each to cover their start, counted in tiles per CU. Few-row
+// against 256-row kernel, 32/8 heads x 128, us: one request of 256 rows, 3.8 / 7.1 tiles per
+// CU 25 / 34 against 36 / 39; of 384 rows, 7.6 / 14.2 tiles 33 / 50 against 37 / 46; 8 requests
+// of 192 rows, 11.3 / 28.8 tiles 40 / 81 against 41 / 73. 64-wide heads: one of 512 rows, 7.6 /
+// 14.2 tiles 26 / 38 against 38 / 45; 4 of 512 rows, 11.2 / 30.9 / 58 tiles 29 / 58 / 102 against
+// 40 / 60 / 92.
 bool fp4_few_rows(const Plan &P, const pic_store_desc &d, int group, int cus) {
   const int block = fp4_prefill_rows_per_block();
   int64_t tiles = 0, blocks = 0;       // key tiles of the 256-row blocks, of the 32-row ones
@@ -1276,7 +1277,9 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
       rows[r] = (int64_t)R.lq * n_q_heads;
       uneven_rows |= blocks[r] != d.n_kv_heads * lp.nrb;
       // d128 row blocks end at the farthest limit of their rows: count the
-      // part of the tiles they walk
+      // part of the tiles they walk. (The few-row 4-bit kernel's end there, too, but
+      // its pieces are cheaper than the more of them that this gives: one request of 30
+      // tokens over 110 tiles 16 us, counted 22; 8 of them over 66 36, 39.)
       if ((kern == Kern::Mfma128 || kern == Kern::Fp4Prefill) && !P.doc_lim.empty() && R.ls == 0 &&
           R.nlinks > 0) {
         const LinkEntry &last = P.links[R.link0 + R.nlinks - 1];
