@@ -92,8 +92,8 @@ struct LinkCursor {
     next_tok0 = n->tok0;
     next_tile0 = n->tile0;
   }
-  __device__ __forceinline__ void start(const LinkParams &p, const WorkItem &it) {
-    at = (const_links)p.links + it.link;
+  __device__ __forceinline__ void start(const_links links, const WorkItem &it) {
+    at = links + it.link;
     left = it.lp;
     base = (const char *)it.k;
     len = it.len;

@@ -279,7 +279,7 @@ struct TileInfo {
 
 // kLim: rows see different numbers of linked rows.
 template <int D, bool kLim, int NB>
-__global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
+__device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *items, const_links links) {
   typedef Merge<D, NB> M;
   __shared__ __align__(16) float lds[M::kFloats];
   const int lane = threadIdx.x & 63;
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   const int u = ub.u, rb = ub.rb;
   if (u >= p.n_items * p.n_kv_heads) return;
   const int kvh = u % p.n_kv_heads;
-  const WorkItem it = load_item(p.items, u / p.n_kv_heads);
+  const WorkItem it = load_item(items, u / p.n_kv_heads);
   const ReqEntry R = item_request(it);
   const int group = p.group;
   const int nrows = R.lq * group, row0 = rb * (16 * NB);
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   }
 
   LinkCursor<true> c;
-  c.start(p, it);
+  c.start(links, it);
   auto info = [&](int t) {       // t only grows
     while (t >= c.end) c.next();
     const int tt = t - c.tile0;
@@ -473,9 +473,30 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   }
 }
 
+template <int D, bool kLim, int NB>
+__global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
+  link_body<D, kLim, NB>(p, p.items, (const_links)p.links);
+}
+
+// The tables are read where they are, in the kernel arguments: no kernel copies them
+// first.
+struct TabArgs {
+  LinkParams p;
+  Fp4Tabs t;
+};
 template <int D, int NB>
-void launch(const LinkParams &p, dim3 grid, dim3 block, hipStream_t st) {
-  if (p.doc_lim)
+__global__ __launch_bounds__(256, 2) void link_fp4_tabs_kernel(TabArgs a) {
+  typedef __attribute__((address_space(4))) const char *const_bytes;
+  const const_bytes t = (const_bytes)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(TabArgs, t);
+  link_body<D, false, NB>(a.p, (const WorkItem *)t,
+                          (const_links)(t + a.p.n_items * (int)sizeof(WorkItem)));
+}
+
+template <int D, int NB>
+void launch(const LinkParams &p, const Fp4Tabs *tabs, dim3 grid, dim3 block, hipStream_t st) {
+  if (tabs)
+    hipLaunchKernelGGL((link_fp4_tabs_kernel<D, NB>), grid, block, 0, st, TabArgs{p, *tabs});
+  else if (p.doc_lim)
     hipLaunchKernelGGL((link_fp4_kernel<D, true, NB>), grid, block, 0, st, p);
   else
     hipLaunchKernelGGL((link_fp4_kernel<D, false, NB>), grid, block, 0, st, p);
@@ -485,15 +506,15 @@ void launch(const LinkParams &p, dim3 grid, dim3 block, hipStream_t st) {
 
 int fp4_rows_per_block(int max_rows) { return max_rows <= 16 ? 16 : 32; }
 
-hipError_t launch_link_fp4(const LinkParams &p, hipStream_t st, const char **name) {
+hipError_t launch_link_fp4(const LinkParams &p, const Fp4Tabs *tabs, hipStream_t st, const char **name) {
   *name = "link_fp4_kernel";
   const int64_t units = (int64_t)p.n_items * p.n_kv_heads;
   const dim3 grid((unsigned)unit_blocks(units, p.nrb, p.n_xcd, 0)), block(64 * kWaves);
   const bool two = fp4_rows_per_block(p.max_rows) == 32;
   if (p.d_k == 128)
-    two ? launch<128, 2>(p, grid, block, st) : launch<128, 1>(p, grid, block, st);
+    two ? launch<128, 2>(p, tabs, grid, block, st) : launch<128, 1>(p, tabs, grid, block, st);
   else
-    two ? launch<64, 2>(p, grid, block, st) : launch<64, 1>(p, grid, block, st);
+    two ? launch<64, 2>(p, tabs, grid, block, st) : launch<64, 1>(p, tabs, grid, block, st);
   return hipGetLastError();
 }
 

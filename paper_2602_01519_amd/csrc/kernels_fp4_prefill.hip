@@ -468,7 +468,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill
     for (int o = 32; o > 0; o >>= 1) w = min(w, __shfl_xor(w, o));
     dlm.wmin = uni(w);
   }
-  c.cur.start(p, it);
+  c.cur.start((const_links)p.links, it);
   set_offsets(c);
   c.stride = (int64_t)p.n_kv_heads * D * 2;
   c.ks = (const char *)p.k_self + c.kvh * D * 2;

@@ -1352,6 +1352,14 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
 
 // Enqueues a call whose tables are already on the device (lp.links, reqs,
 // order set): own-KV staging, the attention kernel, the split combine.
+// Whether a 4-bit call's tables go as a kernel argument: few items and links, no limits,
+// and nothing to combine but one request's pieces, which need no table (one request of
+// 37 tokens over 10 links: 26.0 -> 21.4 us, of 4 over 5: 20.4 -> 18.3).
+bool fp4_tabs(const Setup &C) {
+  return C.kern == Kern::Fp4 && C.P.doc_lim.empty() && (C.splits == 1 || C.P.reqs.size() == 1) &&
+         C.n_items * sizeof(WorkItem) + C.P.links.size() * sizeof(LinkEntry) <= kFp4TabBytes;
+}
+
 // timed: the attention launch may be bracketed by the measurement events
 // (pic_prof_begin); the entry point that allocates nothing passes false.
 pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *work,
@@ -1371,7 +1379,13 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
     lp.part_m = lp.part_o + C.part_rows * d.d_v;
     lp.part_l = lp.part_m + C.part_rows;
   }
-  if (is_fp4(d)) {        // own KV read in place: only the tables to copy
+  Fp4Tabs tabs;
+  const bool by_arg = pro.copy_bytes > 0 && fp4_tabs(C);
+  if (by_arg) {
+    write_items(C, C.P.links.data(), (WorkItem *)tabs.b);
+    std::copy(C.P.links.begin(), C.P.links.end(), (LinkEntry *)(tabs.b + C.n_items * sizeof(WorkItem)));
+    lp.comb = nullptr;
+  } else if (is_fp4(d)) { // own KV read in place: only the tables to copy
     if (pro.copy_bytes > 0) {
       const hipError_t e = launch_table_copy(pro.copy_src, pro.copy_dst, pro.copy_bytes, st);
       if (e != hipSuccess) return hip_fail(e, "table_copy_kernel");
@@ -1395,7 +1409,7 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
   else if (C.kern == Kern::Stream)
     e = launch_link_stream(lp, d.dtype, C.stream_rows, st, &name);
   else if (C.kern == Kern::Fp4)
-    e = launch_link_fp4(lp, st, &name);
+    e = launch_link_fp4(lp, by_arg ? &tabs : nullptr, st, &name);
   else if (C.kern == Kern::Fp4Prefill)
     e = launch_link_fp4_prefill(lp, st, &name);
   else
