@@ -73,6 +73,23 @@ inline bool fp4_width(int d_k, int d_v) { return d_k == d_v && (d_k == 64 || d_k
 // Bytes of one page: 64 tokens of every head.
 inline int64_t fp4_page_bytes(int64_t heads, int64_t d) { return heads * 68 * d; }
 
+// A call's tables in its kernel's arguments, read where they are: no kernel copies them
+// first.
+struct Fp4Args {
+  LinkParams p;
+  Fp4Tabs t;
+};
+struct Fp4ArgTabs {
+  const WorkItem *items;
+  const_links links;
+  __device__ __forceinline__ Fp4ArgTabs(int n_items) {
+    typedef __attribute__((address_space(4))) const char *const_bytes;
+    const const_bytes t = (const_bytes)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(Fp4Args, t);
+    items = (const WorkItem *)t;
+    links = (const_links)(t + n_items * (int)sizeof(WorkItem));
+  }
+};
+
 // Walk over the links of a work item. kAhead: the next link's entry is read when
 // the one before begins, so that no tile waits for a table (narrow_heads 143 -> 136
 // us); the 128-wide 256-row kernel, bound by its products, loses 1% by it.

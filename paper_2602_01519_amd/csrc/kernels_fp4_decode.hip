@@ -478,24 +478,17 @@ __global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
   link_body<D, kLim, NB>(p, p.items, (const_links)p.links);
 }
 
-// The tables are read where they are, in the kernel arguments: no kernel copies them
-// first.
-struct TabArgs {
-  LinkParams p;
-  Fp4Tabs t;
-};
+// The tables are read where they are, in the kernel arguments.
 template <int D, int NB>
-__global__ __launch_bounds__(256, 2) void link_fp4_tabs_kernel(TabArgs a) {
-  typedef __attribute__((address_space(4))) const char *const_bytes;
-  const const_bytes t = (const_bytes)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(TabArgs, t);
-  link_body<D, false, NB>(a.p, (const WorkItem *)t,
-                          (const_links)(t + a.p.n_items * (int)sizeof(WorkItem)));
+__global__ __launch_bounds__(256, 2) void link_fp4_tabs_kernel(Fp4Args a) {
+  const Fp4ArgTabs t(a.p.n_items);
+  link_body<D, false, NB>(a.p, t.items, t.links);
 }
 
 template <int D, int NB>
 void launch(const LinkParams &p, const Fp4Tabs *tabs, dim3 grid, dim3 block, hipStream_t st) {
   if (tabs)
-    hipLaunchKernelGGL((link_fp4_tabs_kernel<D, NB>), grid, block, 0, st, TabArgs{p, *tabs});
+    hipLaunchKernelGGL((link_fp4_tabs_kernel<D, NB>), grid, block, 0, st, Fp4Args{p, *tabs});
   else if (p.doc_lim)
     hipLaunchKernelGGL((link_fp4_kernel<D, true, NB>), grid, block, 0, st, p);
   else

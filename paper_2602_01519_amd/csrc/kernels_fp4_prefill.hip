@@ -417,7 +417,7 @@ __device__ __forceinline__ int limit_end(const LinkParams &p, const WorkItem &it
 }
 
 template <int D, bool kLim>
-__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_kernel(LinkParams p) {
+__device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *items, const_links links) {
   // one array, so that a lane's address serves both buffers
   __shared__ uint4 lds[4][kTile * D / 8];
   uint4 *const sk0 = lds[0], *const sk1 = lds[1], *const sv0 = lds[2], *const sv1 = lds[3];
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill
   const UnitBlock ub = unit_of_block(blockIdx.x, p.nrb, p.n_xcd, p.spread, units);
   const int rb = ub.rb;
   if (ub.u >= units) return;
-  const WorkItem it = load_item(p.items, ub.u / p.n_kv_heads);
+  const WorkItem it = load_item(items, ub.u / p.n_kv_heads);
   c.heads = p.n_kv_heads;
   c.kvh = ub.u % p.n_kv_heads;
   c.R = item_request(it);
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill
     for (int o = 32; o > 0; o >>= 1) w = min(w, __shfl_xor(w, o));
     dlm.wmin = uni(w);
   }
-  c.cur.start((const_links)p.links, it);
+  c.cur.start(links, it);
   set_offsets(c);
   c.stride = (int64_t)p.n_kv_heads * D * 2;
   c.ks = (const char *)p.k_self + c.kvh * D * 2;
@@ -571,11 +571,24 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill
   }
 }
 
+template <int D, bool kLim>
+__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_kernel(LinkParams p) {
+  link_body<D, kLim>(p, p.items, (const_links)p.links);
+}
+// The tables are read where they are, in the kernel arguments.
 template <int D>
-hipError_t launch(const LinkParams &p, hipStream_t st) {
+__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_tabs_kernel(Fp4Args a) {
+  const Fp4ArgTabs t(a.p.n_items);
+  link_body<D, false>(a.p, t.items, t.links);
+}
+
+template <int D>
+hipError_t launch(const LinkParams &p, const Fp4Tabs *tabs, hipStream_t st) {
   const int64_t units = (int64_t)p.n_items * p.n_kv_heads;
   const dim3 grid((unsigned)unit_blocks(units, p.nrb, p.n_xcd, p.spread)), block(kWaves * 64);
-  if (p.doc_lim)
+  if (tabs)
+    hipLaunchKernelGGL(link_fp4_prefill_tabs_kernel<D>, grid, block, 0, st, Fp4Args{p, *tabs});
+  else if (p.doc_lim)
     hipLaunchKernelGGL((link_fp4_prefill_kernel<D, true>), grid, block, 0, st, p);
   else
     hipLaunchKernelGGL((link_fp4_prefill_kernel<D, false>), grid, block, 0, st, p);
@@ -588,9 +601,10 @@ int fp4_prefill_rows_per_block() { return kRows; }
 // resident workgroups per CU (two or four waves per SIMD)
 int fp4_prefill_blocks_per_cu(int d) { return d == 64 ? 2 : 1; }
 
-hipError_t launch_link_fp4_prefill(const LinkParams &p, hipStream_t st, const char **name) {
+hipError_t launch_link_fp4_prefill(const LinkParams &p, const Fp4Tabs *tabs, hipStream_t st,
+                                   const char **name) {
   *name = "link_fp4_prefill_kernel";
-  return p.d_k == 128 ? launch<128>(p, st) : launch<64>(p, st);
+  return p.d_k == 128 ? launch<128>(p, tabs, st) : launch<64>(p, tabs, st);
 }
 
 }  // namespace pic

@@ -1354,9 +1354,9 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
 // order set): own-KV staging, the attention kernel, the split combine.
 // Whether a 4-bit call's tables go as a kernel argument: few items and links, no limits,
 // and nothing to combine but one request's pieces, which need no table (one request of
-// 37 tokens over 10 links: 26.0 -> 21.4 us, of 4 over 5: 20.4 -> 18.3).
+// 37 tokens over 10 links 26.0 -> 21.4 us, of 300 over 12 66 -> 62).
 bool fp4_tabs(const Setup &C) {
-  return C.kern == Kern::Fp4 && C.P.doc_lim.empty() && (C.splits == 1 || C.P.reqs.size() == 1) &&
+  return (C.kern == Kern::Fp4 || C.kern == Kern::Fp4Prefill) && C.P.doc_lim.empty() && (C.splits == 1 || C.P.reqs.size() == 1) &&
          C.n_items * sizeof(WorkItem) + C.P.links.size() * sizeof(LinkEntry) <= kFp4TabBytes;
 }
 
@@ -1411,7 +1411,7 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
   else if (C.kern == Kern::Fp4)
     e = launch_link_fp4(lp, by_arg ? &tabs : nullptr, st, &name);
   else if (C.kern == Kern::Fp4Prefill)
-    e = launch_link_fp4_prefill(lp, st, &name);
+    e = launch_link_fp4_prefill(lp, by_arg ? &tabs : nullptr, st, &name);
   else
     e = launch_link_valu(lp, d.dtype, mla, st, &name);
   prof_stop(st, &ev, name);

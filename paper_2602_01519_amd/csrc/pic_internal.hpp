@@ -459,15 +459,18 @@ hipError_t launch_link_stream(const LinkParams &p, int dtype, int rows, hipStrea
 
 // Link attention over a 4-bit store, d_k = d_v in {64, 128}: 16 or 32 rows per
 // workgroup, whose waves share the keys, or 256 rows.
-// Tables of a few-row call with few work items as a kernel argument: the items, then the
-// links. (tabs not NULL: used in place of p.items and p.links; no per-query limits.)
-constexpr int kFp4TabBytes = 2048;
+// Tables of a call with few work items as a kernel argument: the items, then the links.
+// (tabs not NULL: used in place of p.items and p.links; no per-query limits.) With
+// LinkParams within the 4 KB of a kernel's arguments.
+constexpr int kFp4TabBytes = 3584;
 struct alignas(16) Fp4Tabs {
   char b[kFp4TabBytes];
 };
+static_assert(sizeof(LinkParams) + sizeof(Fp4Tabs) <= 4064, "kernel arguments");
 hipError_t launch_link_fp4(const LinkParams &p, const Fp4Tabs *tabs, hipStream_t st, const char **name);
 int fp4_rows_per_block(int max_rows);
-hipError_t launch_link_fp4_prefill(const LinkParams &p, hipStream_t st, const char **name);
+hipError_t launch_link_fp4_prefill(const LinkParams &p, const Fp4Tabs *tabs, hipStream_t st,
+                                   const char **name);
 int fp4_prefill_rows_per_block();
 int fp4_prefill_blocks_per_cu(int d);
 
