@@ -25,7 +25,7 @@
 //
 // Bound by the issue of a SIMD that its two waves share: matrix instructions take 47% of
 // the cycles and vector ones 41% (16 requests of 512 tokens over 8..20 links of 1024, 32/8
-// heads x 128: 1.74 ms, 1130 TFLOP/s; 64-wide heads, 8 requests over 16 links, 880). The next
+// heads x 128: 1.72 ms, 1144 TFLOP/s; 64-wide heads, 8 requests over 16 links, 900). The next
 // tile's scores formed between this one's probabilities, in a second set of registers,
 // measured the same (1727 against 1711 us), although no wave waited for LDS any more;
 // without barriers and widening that would take 1510 us.

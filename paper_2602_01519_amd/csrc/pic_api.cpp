@@ -1350,16 +1350,18 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   return PIC_OK;
 }
 
-// Enqueues a call whose tables are already on the device (lp.links, reqs,
-// order set): own-KV staging, the attention kernel, the split combine.
 // Whether a 4-bit call's tables go as a kernel argument: few items and links, no limits,
 // and nothing to combine but one request's pieces, which need no table (one request of
 // 37 tokens over 10 links 26.0 -> 21.4 us, of 300 over 12 66 -> 62).
 bool fp4_tabs(const Setup &C) {
-  return (C.kern == Kern::Fp4 || C.kern == Kern::Fp4Prefill) && C.P.doc_lim.empty() && (C.splits == 1 || C.P.reqs.size() == 1) &&
+  return (C.kern == Kern::Fp4 || C.kern == Kern::Fp4Prefill) && C.P.doc_lim.empty() &&
+         (C.splits == 1 || C.P.reqs.size() == 1) &&
          C.n_items * sizeof(WorkItem) + C.P.links.size() * sizeof(LinkEntry) <= kFp4TabBytes;
 }
 
+// Enqueues a call whose tables are already on the device (lp.links, reqs,
+// order set) or are copied there first (pro): own-KV staging, the attention
+// kernel, the split combine.
 // timed: the attention launch may be bracketed by the measurement events
 // (pic_prof_begin); the entry point that allocates nothing passes false.
 pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *work,
