@@ -155,6 +155,9 @@ WIDE = {
 }
 FORMS.update(BLOCKS)
 FORMS.update(WIDE)
+# Tables that just fit a kernel's arguments (one item and 110 links) and that do not
+for n in (109, 110, 111):
+    FORMS[f"links_{n}"] = (64, 4, 2, (3, 64, 65), [tuple(i % 3 for i in range(n))], (2,), None, False, False, True, 1)
 ROWS_256 = ["rows_2_blocks", "rows_300_64"] + list(WIDE)
 
 
