@@ -93,7 +93,12 @@ enum { PIC_GQA = 0, PIC_MLA = 1 };      /* pic_store_desc.kind  */
  * with the even index in that list; what lies above 6 * 2^e, infinities too,
  * becomes 6 * 2^e. A block with a NaN reads as NaN throughout. A row's numbers depend
  * on that row alone. The request's own KV is not rounded. Store calls, link
- * calls, plans and export work as for the other dtypes. A NaN in the cached
+ * calls, plans and export work as for the other dtypes. Link calls round each
+ * probability to bf16 for its product with the values (at most 2^-8 of it) and
+ * the output once; sums are fp32. The output is a mean of the values that a row
+ * sees and stays finite for every finite one, cached infinities (6 * 2^125)
+ * among them, but for own values within 1% of bf16's largest; logits have to
+ * lie in the fp32 range. A NaN in the cached
  * or own V, or an infinity in the own V, may reach every row of the requests
  * that link it, also rows that a limit or the causal mask keeps from it; a
  * query row with a NaN or an infinity gives an output row of NaN or zeros. */

@@ -79,14 +79,34 @@ struct Fp4Args {
   LinkParams p;
   Fp4Tabs t;
 };
-struct Fp4ArgTabs {
+// What a workgroup starts a pass over its piece from: its kernel's arguments (LinkParams first),
+// its number, and this thread's lane and wave. kArg: the tables follow in the arguments. All but
+// the wave are read anew for every pass, so that nothing formed from them is kept for the
+// next one.
+template <bool kArg>
+struct Fp4Start {
+  typedef __attribute__((address_space(4))) const char *const_bytes;
+  LinkParams p;
   const WorkItem *items;
   const_links links;
-  __device__ __forceinline__ Fp4ArgTabs(int n_items) {
-    typedef __attribute__((address_space(4))) const char *const_bytes;
-    const const_bytes t = (const_bytes)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(Fp4Args, t);
-    items = (const WorkItem *)t;
-    links = (const_links)(t + n_items * (int)sizeof(WorkItem));
+  int block, lane, wave;
+  __device__ __forceinline__ explicit Fp4Start(int wave_) : wave(wave_) {
+    const_bytes args = (const_bytes)__builtin_amdgcn_kernarg_segment_ptr();
+    block = blockIdx.x;
+    int all = -1;
+    asm volatile("" : "+s"(args), "+s"(block), "+s"(all));
+    lane = __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
+#ifdef __HIP_DEVICE_COMPILE__    // (no copies between address spaces on the host)
+    p = *(__attribute__((address_space(4))) const LinkParams *)args;
+#endif
+    if (kArg) {
+      const const_bytes t = args + offsetof(Fp4Args, t);
+      items = (const WorkItem *)t;
+      links = (const_links)(t + p.n_items * (int)sizeof(WorkItem));
+    } else {
+      items = p.items;
+      links = (const_links)p.links;
+    }
   }
 };
 
@@ -131,6 +151,19 @@ struct LinkCursor {
     if (kAhead) read(at + (--left > 0 ? 1 : 0));
   }
 };
+
+// Large values. A sum of values times probabilities at most 1 leaves the fp32 range where two
+// of 6 * 2^125 meet, though their mean does not, and sooner where the maximum lags behind. A
+// workgroup whose sums come out too large or NaN takes its piece again, against the exact
+// maximum plus fp4_bias: each of the piece's n < 2^bias probabilities is then at most 2^-bias,
+// and no sum exceeds the largest value. What that loses are probabilities below 2^(bias - 126),
+// as the first pass loses those below 2^-126. Outputs, log-sum-exp and the merge of pieces see
+// one power of two in maximum and sums, and need nothing more. Both passes are the same code (a
+// second copy of it made the compiler spill 82 registers); the check costs an instruction per
+// two sums at the end of a piece.
+__device__ __forceinline__ float fp4_bias(int tiles) {
+  return (float)(32 - __builtin_clz(tiles * kTile));
+}
 
 typedef __bf16 fp4_bf16x2 __attribute__((ext_vector_type(2)));
 

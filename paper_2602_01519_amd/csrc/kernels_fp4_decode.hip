@@ -192,11 +192,11 @@ __device__ __forceinline__ void value_pair(const Tile &x, int t, const bf16x8 (&
 }
 
 // kl: last visible key of the tile for this lane's rows (relative to the tile),
-// used where masked.
+// used where masked. bias: added to its maximum.
 template <int D, int NB, class Tile>
 __device__ __forceinline__ void compute_tile(const Tile &x, const bf16x8 (&qf)[NB][D / 32],
                                              State<D, NB> &st, int lane, bool masked,
-                                             const int (&kl)[NB], float sc) {
+                                             const int (&kl)[NB], float sc, float bias) {
   constexpr int kB = Tile::kKeyBlocks;
   f32x4 s[NB][kB];
 #pragma unroll
@@ -231,7 +231,7 @@ __device__ __forceinline__ void compute_tile(const Tile &x, const bf16x8 (&qf)[N
 #pragma unroll
       for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, s[r][b][i]);
     tmax = row_max(tmax);
-    const float mnew = fmaxf(st.m[r], tmax * sc);
+    const float mnew = fmaxf(st.m[r], __builtin_fmaf(tmax, sc, bias));
     if (mnew > st.m[r]) {        // per lane: rescale this row's state
       const float alpha = __builtin_amdgcn_exp2f(st.m[r] - mnew);   // 0 when m = -inf
       st.l[r] *= alpha;
@@ -269,33 +269,39 @@ template <int D, int NB>
 struct Merge {
   static constexpr int kRows = 16 * NB, kStride = D + 4;
   static constexpr int kMax = kWaves * kRows * kStride, kSum = kMax + kWaves * kRows;
-  static constexpr int kFloats = kSum + kWaves * kRows;
+  static constexpr int kFlag = kSum + kWaves * kRows;    // per wave: its sums are too large
+  static constexpr int kFloats = kFlag + kWaves;
 };
+
+// Largest sum that the merge adds four of without leaving the fp32 range.
+constexpr float kSafeSum = 0x1p125f;
 
 struct TileInfo {
   const char *p;
   int nvalid, tok;
 };
 
-// kLim: rows see different numbers of linked rows.
-template <int D, bool kLim, int NB>
-__device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *items, const_links links) {
+// kLim: rows see different numbers of linked rows. big: the second pass (see fp4_bias). Returns
+// whether the workgroup's sums came out too large in the first one (and nothing was written).
+template <int D, bool kLim, int NB, bool kArg>
+__device__ __forceinline__ bool link_body(int wave, bool big) {
+  const Fp4Start<kArg> start(wave);
+  const LinkParams &p = start.p;
   typedef Merge<D, NB> M;
   __shared__ __align__(16) float lds[M::kFloats];
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = start.lane;
   // Row blocks of a unit (item, kv head) are neighbours on one XCD: they read the same
   // tiles at about the same time. (In the order of the launch: 20.2 -> 18.6 us for one
   // request of 37 tokens, 189 -> 182 for 32 of 16 over 16 documents of their own.)
-  const UnitBlock ub = unit_of_block(blockIdx.x, p.nrb, p.n_xcd, 0, p.n_items * p.n_kv_heads);
+  const UnitBlock ub = unit_of_block(start.block, p.nrb, p.n_xcd, 0, p.n_items * p.n_kv_heads);
   const int u = ub.u, rb = ub.rb;
-  if (u >= p.n_items * p.n_kv_heads) return;
+  if (u >= p.n_items * p.n_kv_heads) return false;
   const int kvh = u % p.n_kv_heads;
-  const WorkItem it = load_item(items, u / p.n_kv_heads);
+  const WorkItem it = load_item(start.items, u / p.n_kv_heads);
   const ReqEntry R = item_request(it);
   const int group = p.group;
   const int nrows = R.lq * group, row0 = rb * (16 * NB);
-  if (row0 >= nrows) return;
+  if (row0 >= nrows) return false;
 
   // this lane's rows
   const int n = lane & 15, g = lane >> 4;
@@ -327,7 +333,7 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
   }
 
   LinkCursor<true> c;
-  c.start(links, it);
+  c.start(start.links, it);
   auto info = [&](int t) {       // t only grows
     while (t >= c.end) c.next();
     const int tt = t - c.tile0;
@@ -359,12 +365,13 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
     st.l[r] = 0.f;
   }
   const float sc = p.scale_log2;
+  const float bias = big ? fp4_bias(max(1, it.t_end - it.t_begin)) : 0.f;
   auto doc_tile = [&](const CacheTile<D, NB == 1> &x, const TileInfo &i) {
     const bool masked = i.nvalid < kTile || (kLim && i.tok + kTile > dmin);
     int kl[NB];
 #pragma unroll
     for (int r = 0; r < NB; ++r) kl[r] = (kLim ? min(i.nvalid, dl[r] - i.tok) : i.nvalid) - 1;
-    compute_tile<D, NB>(x, qf, st, lane, masked, kl, sc);
+    compute_tile<D, NB>(x, qf, st, lane, masked, kl, sc, bias);
   };
   // The load past the last tile reads the piece's last one, which keeps the
   // loop free of branches around loads (the compiler waits for every load in
@@ -400,7 +407,7 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
         int kl[NB];
 #pragma unroll
         for (int r = 0; r < NB; ++r) kl[r] = min(own_last[r], R.ls - 1) - j0;
-        compute_tile<D, NB>(x, qf, st, lane, true, kl, sc);
+        compute_tile<D, NB>(x, qf, st, lane, true, kl, sc, bias);
       }
     }
   }
@@ -417,7 +424,24 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
       lb[wave * M::kRows + 16 * r + n] = ltot;
     }
   }
+  if (!big) {       // (not in the second pass: another wave may still read the first one's flags)
+    float most = 0.f;
+#pragma unroll
+    for (int r = 0; r < NB; ++r)
+#pragma unroll
+      for (int b = 0; b < D / 16; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = __builtin_elementwise_maximum(most, fabsf(st.o[r][b][i]));
+    const bool over = __any(!(most <= kSafeSum));
+    if (lane == 0) lds[M::kFlag + wave] = over ? 1.f : 0.f;
+  }
   __syncthreads();
+  if (!big) {
+    float over = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) over += lds[M::kFlag + w];
+    if (__builtin_expect(over != 0.f, 0)) return true;
+  }
 #pragma unroll
   for (int r = 0; r < NB; ++r) {
     float top = -INFINITY;
@@ -438,7 +462,7 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
   }
   __syncthreads();
   // four channels of a row per thread and step
-  for (int e = threadIdx.x; e < M::kRows * (D / 4); e += 64 * kWaves) {
+  for (int e = 64 * wave + lane; e < M::kRows * (D / 4); e += 64 * kWaves) {
     const int row = e / (D / 4), ch = e % (D / 4) * 4;
     if (row0 + row >= nrows) break;
     float top = -INFINITY, sum = 0.f;
@@ -471,18 +495,25 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
       }
     }
   }
+  return false;
+}
+
+template <int D, bool kLim, int NB, bool kArg>
+__device__ __forceinline__ void link_piece() {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (bool big = false; link_body<D, kLim, NB, kArg>(wave, big); big = true) {
+  }
 }
 
 template <int D, bool kLim, int NB>
-__global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams p) {
-  link_body<D, kLim, NB>(p, p.items, (const_links)p.links);
+__global__ __launch_bounds__(256, 2) void link_fp4_kernel(LinkParams) {
+  link_piece<D, kLim, NB, false>();
 }
 
 // The tables are read where they are, in the kernel arguments.
 template <int D, int NB>
-__global__ __launch_bounds__(256, 2) void link_fp4_tabs_kernel(Fp4Args a) {
-  const Fp4ArgTabs t(a.p.n_items);
-  link_body<D, false, NB>(a.p, t.items, t.links);
+__global__ __launch_bounds__(256, 2) void link_fp4_tabs_kernel(Fp4Args) {
+  link_piece<D, false, NB, true>();
 }
 
 template <int D, int NB>

@@ -21,7 +21,7 @@
 // Softmax: log2 domain, against the running max as it stands; a tile is redone
 // against the new one when a lane's probabilities sum to more than 2^20, and the
 // first tile in which a row sees a key always is. Sums are fp32 of the probabilities
-// before they are rounded to bf16 for the product.
+// before they are rounded to bf16 for the product. (Sums that leave the fp32 range: fp4_bias.)
 //
 // Bound by the issue of a SIMD that its two waves share: matrix instructions take 47% of
 // the cycles and vector ones 41% (16 requests of 512 tokens over 8..20 links of 1024, 32/8
@@ -29,6 +29,8 @@
 // tile's scores formed between this one's probabilities, in a second set of registers,
 // measured the same (1727 against 1711 us), although no wave waited for LDS any more;
 // without barriers and widening that would take 1510 us.
+#include <cfloat>
+
 #include "fp4.hpp"
 
 namespace pic {
@@ -286,11 +288,13 @@ struct DocLim {
   int dl, wmin;
 };
 
-// own_last(): last own key that this lane's row sees (formed where a tile needs it).
+// own_last(): last own key that this lane's row sees (formed where a tile needs it). jump:
+// the lane's sum of probabilities above which a tile is redone; bias: added to its maximum.
 template <int D, bool kLim, class OwnLast>
 __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, const uint4 *vt,
                                              const bf16x8 (&qf)[D / 16], Acc<D> &a, const TileRef &r,
-                                             OwnLast own_last, const DocLim &dlm, float sc) {
+                                             OwnLast own_last, const DocLim &dlm, float sc,
+                                             float jump, float bias) {
   f32x16 s0, s1;
 #pragma unroll
   for (int x = 0; x < 16; ++x) {
@@ -363,13 +367,13 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
     return t;
   };
   float ts = probs();
-  bool redo = !(ts <= kJumpSum);
+  bool redo = !(ts <= jump);
   // A row that has seen no key yet and sees one here (its probabilities against a
   // maximum of 0 may all be 0).
   if (__builtin_expect(__any(a.m == -INFINITY), 0)) redo |= a.m == -INFINITY && tile_max() > -INFINITY;
   if (__builtin_expect(__any(redo), 0)) {
     const float tmax = half_swap_max(tile_max());
-    const float mnew = fmaxf(a.m, tmax * sc);
+    const float mnew = fmaxf(a.m, __builtin_fmaf(tmax, sc, bias));
     const float alpha = mnew == a.m ? 1.f : __builtin_amdgcn_exp2f(a.m - mnew);
     a.m = mnew;
     a.l *= alpha;
@@ -416,21 +420,26 @@ __device__ __forceinline__ int limit_end(const LinkParams &p, const WorkItem &it
   return min(t_end, tile0 + (max(0, min(far - tok0, len)) + kTile - 1) / kTile);
 }
 
-template <int D, bool kLim>
-__device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *items, const_links links) {
+// big: the second pass (see fp4_bias). Returns whether the workgroup's sums left the fp32 range
+// in the first one (and nothing was written).
+template <int D, bool kLim, bool kArg>
+__device__ __forceinline__ bool link_body(int wave, bool big) {
+  const Fp4Start<kArg> start(wave);
+  const LinkParams &p = start.p;
   // one array, so that a lane's address serves both buffers
   __shared__ uint4 lds[4][kTile * D / 8];
+  __shared__ int over[kWaves];     // per wave: its sums left the fp32 range
   uint4 *const sk0 = lds[0], *const sk1 = lds[1], *const sv0 = lds[2], *const sv1 = lds[3];
   Ctx<D> c;
-  c.lane = threadIdx.x & 63;
-  c.wave = uni(threadIdx.x >> 6);
+  c.lane = start.lane;
+  c.wave = start.wave;
   c.n = c.lane & 31;
   c.g = c.lane >> 5;
   const int units = p.n_items * p.n_kv_heads;
-  const UnitBlock ub = unit_of_block(blockIdx.x, p.nrb, p.n_xcd, p.spread, units);
+  const UnitBlock ub = unit_of_block(start.block, p.nrb, p.n_xcd, p.spread, units);
   const int rb = ub.rb;
-  if (ub.u >= units) return;
-  const WorkItem it = load_item(items, ub.u / p.n_kv_heads);
+  if (ub.u >= units) return false;
+  const WorkItem it = load_item(start.items, ub.u / p.n_kv_heads);
   c.heads = p.n_kv_heads;
   c.kvh = ub.u % p.n_kv_heads;
   c.R = item_request(it);
@@ -438,7 +447,7 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
   const int group = p.group;
   const int nrows = R.lq * group;
   const int row0 = rb * kRows;
-  if (row0 >= nrows) return;
+  if (row0 >= nrows) return false;
   const int vis = visible_tiles(R, min(nrows - 1, row0 + kRows - 1) / group);
   const int t_begin = it.t_begin;
   int t_end = min(it.t_end, vis);
@@ -468,7 +477,7 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
     for (int o = 32; o > 0; o >>= 1) w = min(w, __shfl_xor(w, o));
     dlm.wmin = uni(w);
   }
-  c.cur.start(links, it);
+  c.cur.start(start.links, it);
   set_offsets(c);
   c.stride = (int64_t)p.n_kv_heads * D * 2;
   c.ks = (const char *)p.k_self + c.kvh * D * 2;
@@ -498,6 +507,7 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
   a.m = -INFINITY;
   a.l = 0.f;
   const float sc = p.scale_log2;
+  const float bias = big ? fp4_bias(max(1, t_end - t_begin)) : 0.f, jump = big ? 0.f : kJumpSum;
 
   if (t_begin < t_end) {
     widen(c, ref0, sh, sk0, sv0);
@@ -514,15 +524,30 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
   for (int t = t_begin; t < t_end; t += 2) {
     ref1 = t + 1 < t_end ? c.tile(t + 1) : ref0;
     fetch(c, ref1, sh);
-    if (active) compute_tile<D, kLim>(c, sk0, sv0, qf, a, ref0, own_last, dlm, sc);
+    if (active) compute_tile<D, kLim>(c, sk0, sv0, qf, a, ref0, own_last, dlm, sc, jump, bias);
     widen(c, ref1, sh, sk1, sv1);
     __syncthreads();
     if (t + 1 >= t_end) break;
     ref0 = t + 2 < t_end ? c.tile(t + 2) : ref1;
     fetch(c, ref0, sh);
-    if (active) compute_tile<D, kLim>(c, sk1, sv1, qf, a, ref1, own_last, dlm, sc);
+    if (active) compute_tile<D, kLim>(c, sk1, sv1, qf, a, ref1, own_last, dlm, sc, jump, bias);
     widen(c, ref0, sh, sk0, sv0);
     __syncthreads();
+  }
+
+  if (!big) {
+    float most = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) most = __builtin_elementwise_maximum(most, fabsf(a.o[d][x]));
+    const bool mine = __any(!(most <= FLT_MAX));
+    if (c.lane == 0) over[c.wave] = mine;
+    __syncthreads();
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) any |= over[w];
+    if (__builtin_expect(any, 0)) return true;
   }
 
   // ---- epilogue: O^T[dv][row], dv = 32 d + 8 (x >> 2) + 4 g + (x & 3)
@@ -531,7 +556,7 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
   const int64_t orow = out_row(lane);
   const float ltot = half_swap_sum(a.l);
   const int nvalid = min(kRowsPerWave, nrows - (row0 + c.wave * kRowsPerWave));
-  if (nvalid <= 0) return;
+  if (nvalid <= 0) return false;
   const float inv = ltot > 0.f ? 1.f / ltot : 0.f;
   const int64_t prow = it.part + (orow - (int64_t)R.q0 * p.n_q_heads);
   if constexpr (D == 128) {
@@ -562,24 +587,31 @@ __device__ __forceinline__ void link_body(const LinkParams &p, const WorkItem *i
         }
       }
   }
-  if (!rvalid || c.g != 0) return;
+  if (!rvalid || c.g != 0) return false;
   if (it.part < 0) {
     if (p.lse) p.lse[orow] = ltot == 0.f ? -INFINITY : log_sum(a.m, ltot);
   } else {
     p.part_m[prow] = partial_max(a.m, ltot);
     p.part_l[prow] = ltot;
   }
+  return false;
+}
+
+template <int D, bool kLim, bool kArg>
+__device__ __forceinline__ void link_piece() {
+  const int wave = uni(threadIdx.x >> 6);
+  for (bool big = false; link_body<D, kLim, kArg>(wave, big); big = true) {
+  }
 }
 
 template <int D, bool kLim>
-__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_kernel(LinkParams p) {
-  link_body<D, kLim>(p, p.items, (const_links)p.links);
+__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_kernel(LinkParams) {
+  link_piece<D, kLim, false>();
 }
 // The tables are read where they are, in the kernel arguments.
 template <int D>
-__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_tabs_kernel(Fp4Args a) {
-  const Fp4ArgTabs t(a.p.n_items);
-  link_body<D, false>(a.p, t.items, t.links);
+__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void link_fp4_prefill_tabs_kernel(Fp4Args) {
+  link_piece<D, false, true>();
 }
 
 template <int D>

@@ -2,6 +2,7 @@
 // attention and the split-K log-sum-exp combine. gfx950 only.
 #include "pic_internal.hpp"
 
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -789,6 +790,12 @@ __device__ __forceinline__ void store_quad<uint16_t>(uint16_t *out, float4 v) {
                              (uint32_t)bf16_rne(v.z) | ((uint32_t)bf16_rne(v.w) << 16));
 }
 
+// The largest magnitude; NaN if one is.
+__device__ __forceinline__ float largest(float4 v) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(v.x), fabsf(v.y)),
+                                       __builtin_elementwise_maximum(fabsf(v.z), fabsf(v.w)));
+}
+
 template <typename T, int kLanes, int kChunks, int kGpr, bool kSkip>
 __global__ __launch_bounds__(256) void combine_kernel(LinkParams p) {
   constexpr int kB = 4;
@@ -907,6 +914,20 @@ __global__ __launch_bounds__(256) void combine_kernel(LinkParams p) {
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
     const int e = 4 * (kLanes * c + lane);
+    if (e < dv && M != -INFINITY && !(largest(acc[c]) <= FLT_MAX)) {
+      // The sums of large values pass the fp32 range before they are divided by L, the
+      // output does not: with weights that sum to one.
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < S; ++s) {
+        const int64_t pr = (int64_t)s * rows + prow;
+        const float m = p.part_m[pr], w = exp2f(m - M) * inv;
+        if (m == -INFINITY) continue;
+        const float4 v = *(const float4 *)(p.part_o + pr * dv + e);
+        a = make_float4(a.x + w * v.x, a.y + w * v.y, a.z + w * v.z, a.w + w * v.w);
+      }
+      store_quad<T>(out + e, a);
+      continue;
+    }
     if (e < dv)
       store_quad<T>(out + e, make_float4(acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv));
   }
