@@ -215,9 +215,9 @@ struct DocLim {
 // causal limit, and in document tiles rows at or past the row's limit.
 // s0[x] / s1[x] hold key (x>>3)*16 + g*8 + (x&7) (+32).
 // kLim: the call carries per-row limits (a separate instantiation, so that
-// calls without them run no limit code).
+// calls without them run no limit code). Returns whether this lane holds a visible key.
 template <bool kLim>
-__device__ __forceinline__ void mask_tile(const Ctx &c, f32x16 &s0, f32x16 &s1, const TileRef &r,
+__device__ __forceinline__ bool mask_tile(const Ctx &c, f32x16 &s0, f32x16 &s1, const TileRef &r,
                                           int lim, const DocLim &dlm) {
   const int nvalid = r.nvalid;
   if (r.own || nvalid < kTile || (kLim && r.tok + kTile > dlm.wmin)) {
@@ -233,7 +233,9 @@ __device__ __forceinline__ void mask_tile(const Ctx &c, f32x16 &s0, f32x16 &s1, 
       if (key > kl) s0[x] = -INFINITY;
       if (key + 32 > kl) s1[x] = -INFINITY;
     }
+    return kl >= 0;
   }
+  return true;
 }
 
 // One tile: S = K Q^T from kt, mask, online softmax (log2 domain, against
@@ -272,13 +274,14 @@ __device__ __forceinline__ void compute_tile(const Ctx &c, const uint4 *kt, cons
     s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[st], qf[st], s1, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
-  mask_tile<kLim>(c, s0, s1, ref, lim, dlm);
+  const bool seen = mask_tile<kLim>(c, s0, s1, ref, lim, dlm);
 
   // Probabilities against the running max as it stands, and this lane's
   // (bf16-rounded) sum of them. The tile's own max is only computed when
   // some lane's sum exceeds 2^64 (a probability could then overflow in a
-  // later sum) or a row with a visible key has no running max yet; the tile
-  // is then redone against the new max.
+  // later sum) or a row with a visible key has no running max yet (whatever its
+  // sum: the probabilities of logits far below zero are all 0 against a max of
+  // zero); the tile is then redone against the new max.
   bf16x8 pf[4];
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
   auto probs = [&]() {
@@ -301,7 +304,7 @@ __device__ __forceinline__ void compute_tile(const Ctx &c, const uint4 *kt, cons
     return ts;
   };
   float ts = probs();
-  if (__builtin_expect(__any(!(ts <= kJumpSum) || (a.m_used == -INFINITY && ts > 0.f)), 0)) {
+  if (__builtin_expect(__any(!(ts <= kJumpSum) || (a.m_used == -INFINITY && seen)), 0)) {
     float tmax = -INFINITY;
 #pragma unroll
     for (int x = 0; x < 16; x += 2) {

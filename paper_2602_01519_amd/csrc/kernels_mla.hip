@@ -370,6 +370,7 @@ __global__ __launch_bounds__(256, 1) void link_mla_kernel(LinkParams p) {
       __builtin_amdgcn_sched_barrier(0);
     }
     // s[x]: key 32 kb_s + (x>>3)*16 + g*8 + (x&7) of row 32 rb_s + n
+    bool seen = true;            // this lane holds a visible key
     if (ref.own || ref.nvalid < kTile || (kLim && ref.tok + kTile > wmin_s)) {
       const int kl = (ref.own ? min(lim[rb_s] - ref.j0, ref.nvalid - 1)
                       : kLim  ? min(dl_s - ref.tok, ref.nvalid) - 1
@@ -378,16 +379,18 @@ __global__ __launch_bounds__(256, 1) void link_mla_kernel(LinkParams p) {
 #pragma unroll
       for (int x = 0; x < 16; ++x)
         if ((x >> 3) * 16 + (x & 7) > kl) s[x] = -INFINITY;
+      seen = kl >= 0;
     }
     // 2. probabilities against the running max as it stands. A lane whose
     // partial sum stays <= 2^64 has every probability <= 2^64; the
     // tile's own max is only computed when some lane of the workgroup fails
-    // that test (or has no running max yet).
+    // that test, or has a visible key and no running max yet (whatever its sum:
+    // the probabilities of logits far below zero are all 0 against a max of zero).
     const float mu = rb_s ? m_used[1] : m_used[0];
     const float lsum0 = lsum;
     const float ts = publish(s, mu);
     lsum += ts;
-    const bool jump = !(ts <= kJumpSum) || (mu == -INFINITY && ts > 0.f);
+    const bool jump = !(ts <= kJumpSum) || (mu == -INFINITY && seen);
     const bool wjump = __any(jump);
     if (lane == 0) ((int *)&sm.jump)[wave] = wjump;
     lds_barrier();
