@@ -21,12 +21,15 @@
 // are copied (out of place only; in place they are not touched). A chunk that
 // the part's end cuts short goes element by element, which keeps every size on
 // the same path.
+#include <algorithm>
+
 #include "pic_internal.hpp"
 
 namespace pic {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMostBlocks = (1 << 24) - 1;     // of kThreads in one launch
 constexpr int kBatch = 2;         // rows whose loads a lane has in flight
 
 template <typename T>
@@ -203,26 +206,39 @@ hipError_t launch_rope(RopeParams p, int dtype, bool half, const DevShape &ds, h
   const int want = 4 * ds.cus;
   p.tokens = p.slots / p.heads < 1 ? 1 : p.slots / p.heads > 8 ? 8 : p.slots / p.heads;
   while (p.tokens > 1 && p.n_tokens / p.tokens < want) --p.tokens;
-  const int blocks = (p.n_tokens + p.tokens - 1) / p.tokens;
+  const int64_t blocks = ((int64_t)p.n_tokens + p.tokens - 1) / p.tokens;
   int parts = 1;
   if (blocks < want) {
     const int most = (p.heads + p.slots - 1) / p.slots;
-    parts = (want + blocks - 1) / blocks;
+    parts = (int)((want + blocks - 1) / blocks);
     if (parts > most) parts = most;
   }
   p.heads_per_block = (p.heads + parts - 1) / parts;
-  const dim3 grid((unsigned)blocks, (unsigned)((p.heads + p.heads_per_block - 1) / p.heads_per_block));
   const size_t lds = (size_t)p.tokens * 2 * ((p.rot / 2 + 7) / 8 * 8) * sizeof(float);
-  if (dtype == 0) {
-    if (half)
-      hipLaunchKernelGGL((rope_kernel<float, true>), grid, dim3(kThreads), lds, st, p);
-    else
-      hipLaunchKernelGGL((rope_kernel<float, false>), grid, dim3(kThreads), lds, st, p);
-  } else {
-    if (half)
-      hipLaunchKernelGGL((rope_kernel<uint16_t, true>), grid, dim3(kThreads), lds, st, p);
-    else
-      hipLaunchKernelGGL((rope_kernel<uint16_t, false>), grid, dim3(kThreads), lds, st, p);
+  // One launch but for very many tokens (2^24 workgroups or more): a launch's threads are
+  // counted in 32 bits, and what lies above is dropped without an error.
+  const int64_t all = p.n_tokens, most = (int64_t)kMostBlocks * p.tokens;
+  const int esz = dtype == 0 ? 4 : 2;
+  for (int64_t at = 0; at < all; at += most) {
+    p.n_tokens = (int32_t)std::min(all - at, most);
+    const dim3 grid((unsigned)((p.n_tokens + (int64_t)p.tokens - 1) / p.tokens),
+                    (unsigned)((p.heads + p.heads_per_block - 1) / p.heads_per_block));
+    if (dtype == 0) {
+      if (half)
+        hipLaunchKernelGGL((rope_kernel<float, true>), grid, dim3(kThreads), lds, st, p);
+      else
+        hipLaunchKernelGGL((rope_kernel<float, false>), grid, dim3(kThreads), lds, st, p);
+    } else {
+      if (half)
+        hipLaunchKernelGGL((rope_kernel<uint16_t, true>), grid, dim3(kThreads), lds, st, p);
+      else
+        hipLaunchKernelGGL((rope_kernel<uint16_t, false>), grid, dim3(kThreads), lds, st, p);
+    }
+    p.positions += p.n_tokens;
+    for (int i = 0; i < p.n_tensors; ++i) {
+      p.t[i].x = (const char *)p.t[i].x + p.n_tokens * p.t[i].x_stride * esz;
+      p.t[i].out = (char *)p.t[i].out + p.n_tokens * p.t[i].out_stride * esz;
+    }
   }
   return hipGetLastError();
 }
