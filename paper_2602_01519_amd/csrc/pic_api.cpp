@@ -936,6 +936,21 @@ bool small_tables(const Plan &P) {
 // gains; fp32 gains or loses with how its split count falls.
 constexpr int kStreamSmallRows = 128;
 
+// Most workgroups of one launch of an attention kernel: a launch's threads, at most 512 per
+// workgroup, are counted in 32 bits, and the runtime drops what lies above without an error.
+// A call has them where it links many requests and one of them is long, since every item
+// (request piece) has room for the longest request's row blocks (512 requests of one token and
+// one of 32,768, 32/8 heads, in blocks of 32 rows: 2^24). Such calls go in several launches.
+constexpr int64_t kMostBlocks = (1 << 23) - 1;
+
+// Items (Valu: requests) of one launch; below 1: not even one fits.
+int64_t launch_items(const Setup &C) {
+  const LinkParams &lp = C.lp;
+  if (C.kern == Kern::Decode128) return kMostBlocks / lp.n_kv_heads;    // a wave each, no row blocks
+  // (unit counts are rounded up to whole rounds of the XCDs, the MLA kernel's to its gangs)
+  return (kMostBlocks - (int64_t)lp.n_xcd * std::max(lp.nrb, lp.gang)) / ((int64_t)lp.nrb * lp.n_kv_heads);
+}
+
 // Calls of a 4-bit store that the few-row kernel takes: those whose rows fill little of
 // 256-row blocks, at most four and a half 32-row blocks of them (16 requests over 10 links
 // of 300..1024, 128-wide heads, of 48 / 96 / 128 rows: 52 / 80 / 84 us, in 256-row workgroups
@@ -947,8 +962,10 @@ constexpr int kStreamSmallRows = 128;
 // of 192 rows, 11.3 / 28.8 tiles 40 / 81 against 41 / 73. 64-wide heads: one of 512 rows, 7.6 /
 // 14.2 tiles 26 / 38 against 38 / 45; 4 of 512 rows, 11.2 / 30.9 / 58 tiles 29 / 58 / 102 against
 // 40 / 60 / 92.
+// (Never those that would need several launches.)
 bool fp4_few_rows(const Plan &P, const pic_store_desc &d, int group, int cus) {
   const int block = fp4_prefill_rows_per_block();
+  if (((int64_t)P.reqs.size() * d.n_kv_heads + 64) * ((P.max_rows + 31) / 32) > kMostBlocks) return false;
   int64_t tiles = 0, blocks = 0;       // key tiles of the 256-row blocks, of the 32-row ones
   for (const ReqEntry &R : P.reqs) {
     const int64_t rows = (int64_t)R.lq * group;
@@ -1306,6 +1323,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
       while (table_layout(C).bytes + C.work_bytes() > kStaticScratchBytes + kStaticScratchSlack &&
              C.splits > 1)
         fewer_pieces(s, n_q_heads, C);
+    if (launch_items(C) < 1) return fail(PIC_ERR_UNSUPPORTED, "too many query rows for one launch");
     return PIC_OK;
   }
 
@@ -1347,6 +1365,9 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   C.part_rows = splits > 1 ? (int64_t)P.total_q * n_q_heads * splits : 0;
   C.part_off = round_up(P.own_bytes, 256);
   C.part_bytes = (size_t)C.part_rows * (d.d_v + 2) * sizeof(float);
+  // (a small call is one launch; the pieces of the vector-ALU kernel are its second dimension)
+  if (launch_items(C) < (!C.small ? 1 : (int64_t)req->batch * (kern == Kern::Stream ? splits : 1)))
+    return fail(PIC_ERR_UNSUPPORTED, "too many query rows for one launch");
   return PIC_OK;
 }
 
@@ -1355,7 +1376,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
 // 37 tokens over 10 links 26.0 -> 21.4 us, of 300 over 12 66 -> 62).
 bool fp4_tabs(const Setup &C) {
   return (C.kern == Kern::Fp4 || C.kern == Kern::Fp4Prefill) && C.P.doc_lim.empty() &&
-         (C.splits == 1 || C.P.reqs.size() == 1) &&
+         (C.splits == 1 || C.P.reqs.size() == 1) && C.n_items <= launch_items(C) &&
          C.n_items * sizeof(WorkItem) + C.P.links.size() * sizeof(LinkEntry) <= kFp4TabBytes;
 }
 
@@ -1401,21 +1422,34 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
   std::pair<hipEvent_t, hipEvent_t> ev{nullptr, nullptr};
   const char *name = "";
   if (timed) prof_start(st, &ev);
-  hipError_t e;
-  if (C.kern == Kern::Decode128)
-    e = launch_link_decode_d128(lp, st, &name);
-  else if (C.kern == Kern::Mla)
-    e = launch_link_mla(lp, st, &name);
-  else if (C.kern == Kern::Mfma128)
-    e = launch_link_mfma_d128(lp, st, &name);
-  else if (C.kern == Kern::Stream)
-    e = launch_link_stream(lp, d.dtype, C.stream_rows, st, &name);
-  else if (C.kern == Kern::Fp4)
-    e = launch_link_fp4(lp, by_arg ? &tabs : nullptr, st, &name);
-  else if (C.kern == Kern::Fp4Prefill)
-    e = launch_link_fp4_prefill(lp, by_arg ? &tabs : nullptr, st, &name);
-  else
-    e = launch_link_valu(lp, d.dtype, mla, st, &name);
+  hipError_t e = hipSuccess;
+  const int64_t all = C.kern == Kern::Valu ? (int64_t)C.P.reqs.size() : C.n_items;
+  const int64_t most = launch_items(C);
+  LinkParams part = lp;
+  for (int64_t at = 0; at < all && e == hipSuccess; at += most) {
+    const int32_t n = (int32_t)std::min(all - at, most);
+    if (C.kern == Kern::Valu) {
+      part.order = lp.order + at;
+      part.n_groups = n * d.n_kv_heads;
+    } else {
+      part.items = lp.items + at;
+      part.n_items = n;
+    }
+    if (C.kern == Kern::Decode128)
+      e = launch_link_decode_d128(part, st, &name);
+    else if (C.kern == Kern::Mla)
+      e = launch_link_mla(part, st, &name);
+    else if (C.kern == Kern::Mfma128)
+      e = launch_link_mfma_d128(part, st, &name);
+    else if (C.kern == Kern::Stream)
+      e = launch_link_stream(part, d.dtype, C.stream_rows, st, &name);
+    else if (C.kern == Kern::Fp4)
+      e = launch_link_fp4(part, by_arg ? &tabs : nullptr, st, &name);
+    else if (C.kern == Kern::Fp4Prefill)
+      e = launch_link_fp4_prefill(part, by_arg ? &tabs : nullptr, st, &name);
+    else
+      e = launch_link_valu(part, d.dtype, mla, st, &name);
+  }
   prof_stop(st, &ev, name);
   if (e != hipSuccess) return hip_fail(e, name);
   if (C.splits > 1) {
