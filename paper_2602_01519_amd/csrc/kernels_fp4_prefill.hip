@@ -400,26 +400,6 @@ __device__ __forceinline__ void compute_tile(const Ctx<D> &c, const uint4 *kt, c
   }
 }
 
-// The tile after the last one of the item that holds a linked row below the
-// farthest limit of query tokens tok_lo .. tok_hi, at most t_end.
-__device__ __forceinline__ int limit_end(const LinkParams &p, const WorkItem &it, int tok_lo,
-                                         int tok_hi, int lane, int t_end) {
-  int far = 0;
-  for (int t = tok_lo + lane; t <= tok_hi; t += 64) far = max(far, p.doc_lim[t]);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) far = max(far, __shfl_xor(far, o));
-  far = uni(far);
-  const const_links links = (const_links)p.links + it.link;
-  int li = 0, tok0 = it.tok0, len = it.len, tile0 = it.tile0;
-  while (far > tok0 + len && tile0 + (len + kTile - 1) / kTile < t_end) {
-    ++li;
-    tok0 = links[li].tok0;
-    len = links[li].len;
-    tile0 = links[li].tile0;
-  }
-  return min(t_end, tile0 + (max(0, min(far - tok0, len)) + kTile - 1) / kTile);
-}
-
 // big: the second pass (see fp4_bias). Returns whether the workgroup's sums left the fp32 range
 // in the first one (and nothing was written).
 template <int D, bool kLim, bool kArg>

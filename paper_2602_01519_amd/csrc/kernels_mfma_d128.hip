@@ -340,26 +340,6 @@ __device__ __forceinline__ void compute_tile(const Ctx &c, const uint4 *kt, cons
   }
 }
 
-// The tile after the last one of the item that holds a linked row below the
-// farthest limit of query tokens tok_lo .. tok_hi, at most t_end.
-__device__ __forceinline__ int limit_end(const LinkParams &p, const WorkItem &it, int tok_lo,
-                                         int tok_hi, int lane, int t_end) {
-  int far = 0;
-  for (int t = tok_lo + lane; t <= tok_hi; t += 64) far = max(far, p.doc_lim[t]);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) far = max(far, __shfl_xor(far, o));
-  far = uni(far);
-  const const_links links = (const_links)p.links + it.link;
-  int li = 0, tok0 = it.tok0, len = it.len, tile0 = it.tile0;
-  while (far > tok0 + len && tile0 + (len + kTile - 1) / kTile < t_end) {
-    ++li;
-    tok0 = links[li].tok0;
-    len = links[li].len;
-    tile0 = links[li].tile0;
-  }
-  return min(t_end, tile0 + (max(0, min(far - tok0, len)) + kTile - 1) / kTile);
-}
-
 // kStages: tile buffer pairs, 2 or 3 (see the tile loops).
 template <bool kLim, int kStages>
 __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void link_mfma_d128_kernel(LinkParams p) {

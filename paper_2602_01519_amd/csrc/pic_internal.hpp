@@ -144,9 +144,10 @@ DevShape device_shape();
 // an XCD and its L2 and are dispatched back to back. Where that would leave
 // XCDs idle (few units, or a last round of them that fills few XCDs: more
 // than a quarter of the places empty), the row blocks of every unit spread
-// over all XCDs instead: block 0 of every unit first, or (spread 2: calls with
-// per-query limits) the last one, whose rows see the most. (The stream kernel
-// spreads them always, see apply_splits.)
+// over all XCDs instead: block 0 of every unit first, or (spread 2) the last one,
+// whose rows see the most and which is the first to be empty: calls of the 256-row
+// kernels with per-query limits, and those of the 4-bit one that fit one round
+// or have empty row blocks. (The stream kernel spreads them always. See apply_splits.)
 inline bool spread_units(int64_t units, int32_t nrb, int32_t n_xcd) {
   return nrb > 1 && 4 * ((units + n_xcd - 1) / n_xcd * n_xcd) > 5 * units;
 }
@@ -194,6 +195,27 @@ __device__ __forceinline__ ReqEntry item_request(const WorkItem &w) {
   R.doc_tiles = w.doc_tiles;
   R.tiles = w.doc_tiles + (w.ls + kTile - 1) / kTile;
   return R;
+}
+
+// Calls with per-query limits and no own KV: the tile after the last one of the item that
+// holds a linked row below the farthest limit of query tokens tok_lo .. tok_hi, at most
+// t_end. (The 256-row kernels end there.)
+__device__ __forceinline__ int limit_end(const LinkParams &p, const WorkItem &it, int tok_lo,
+                                         int tok_hi, int lane, int t_end) {
+  int far = 0;
+  for (int t = tok_lo + lane; t <= tok_hi; t += 64) far = max(far, p.doc_lim[t]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) far = max(far, __shfl_xor(far, o));
+  far = __builtin_amdgcn_readfirstlane(far);
+  const const_links links = (const_links)p.links + it.link;
+  int li = 0, tok0 = it.tok0, len = it.len, tile0 = it.tile0;
+  while (far > tok0 + len && tile0 + (len + kTile - 1) / kTile < t_end) {
+    ++li;
+    tok0 = links[li].tok0;
+    len = links[li].len;
+    tile0 = links[li].tile0;
+  }
+  return min(t_end, tile0 + (max(0, min(far - tok0, len)) + kTile - 1) / kTile);
 }
 
 // The running max a partial (m, l, O) is stored with: -inf only where it holds
