@@ -70,18 +70,6 @@ typedef enum {
 enum { PIC_F32 = 0, PIC_BF16 = 1, PIC_FP4 = 2 };
 enum { PIC_GQA = 0, PIC_MLA = 1 };      /* pic_store_desc.kind  */
 
-/* Shape of a store's chunk caches. d_k and d_v must be multiples of 8.
- * GQA: n_kv_heads >= 1, separate K [.., d_k] and V [.., d_v] per head.
- * MLA: n_kv_heads == 1, d_v <= d_k, the value is the first d_v of each key row.
- * n_layers: cross-attention layers per chunk, 0 or 1 for one. Comb
- *   interleaves L_cross cross-attention layers with the decoder (Sec. 4.2
- *   and 4.3, Fig. 3: 8 among 32 decoder layers; Eq. 12), and each reads its
- *   own K and V of every document; a chunk's caches of all layers are put
- *   together and each link call names its layer.
- * capacity_tokens: pool size in tokens per layer, in pages of 64 tokens.
- * Each chunk occupies its length rounded up to whole pages in every layer,
- * in one run of consecutive pages when a free run is long enough, else in
- * several (removal leaves holes; no copy ever moves a chunk). */
 /* 4-bit stores (dtype PIC_FP4; GQA only, d_k = d_v of 64 or 128, else
  * UNSUPPORTED). Everything that goes in or out is bf16: k and v of pic_store_put
  * and pic_store_write_rows, q, k_self, v_self and out of the link calls, and
@@ -97,11 +85,24 @@ enum { PIC_GQA = 0, PIC_MLA = 1 };      /* pic_store_desc.kind  */
  * probability to bf16 for its product with the values (at most 2^-8 of it) and
  * the output once; sums are fp32. The output is a mean of the values that a row
  * sees and stays finite for every finite one, cached infinities (6 * 2^125)
- * among them, but for own values within 1% of bf16's largest; logits have to
+ * among them, but for own values within 1% of bf16's largest; dot products have to
  * lie in the fp32 range. A NaN in the cached
  * or own V, or an infinity in the own V, may reach every row of the requests
  * that link it, also rows that a limit or the causal mask keeps from it; a
  * query row with a NaN or an infinity gives an output row of NaN or zeros. */
+
+/* Shape of a store's chunk caches. d_k and d_v must be multiples of 8.
+ * GQA: n_kv_heads >= 1, separate K [.., d_k] and V [.., d_v] per head.
+ * MLA: n_kv_heads == 1, d_v <= d_k, the value is the first d_v of each key row.
+ * n_layers: cross-attention layers per chunk, 0 or 1 for one. Comb
+ *   interleaves L_cross cross-attention layers with the decoder (Sec. 4.2
+ *   and 4.3, Fig. 3: 8 among 32 decoder layers; Eq. 12), and each reads its
+ *   own K and V of every document; a chunk's caches of all layers are put
+ *   together and each link call names its layer.
+ * capacity_tokens: pool size in tokens per layer, in pages of 64 tokens.
+ * Each chunk occupies its length rounded up to whole pages in every layer,
+ * in one run of consecutive pages when a free run is long enough, else in
+ * several (removal leaves holes; no copy ever moves a chunk). */
 typedef struct pic_store_desc {
   int32_t kind;
   int32_t dtype;
@@ -255,6 +256,10 @@ typedef struct pic_link_req {
  * over long documents), the library splits each request's keys and merges
  * the partial softmax states exactly, as pic_link_decode does; the result
  * is the same up to floating-point rounding order.
+ * Values above 2^63 in magnitude may give infinities in bf16 GQA stores of
+ * d 128 and bf16 MLA stores of 576 / 512.
+ * UNSUPPORTED: one request's query rows alone pass what one launch holds
+ * (2^23 - 1 workgroups of its row blocks; no limit of the batch).
  * Errors: INVALID, NOT_FOUND, UNSUPPORTED, HIP. */
 pic_status pic_link_attn(pic_store *store, const pic_link_req *req, int32_t n_q_heads,
                          const void *q, const void *k_self, const void *v_self,

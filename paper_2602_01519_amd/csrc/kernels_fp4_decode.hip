@@ -12,7 +12,7 @@
 //
 // Bound by the cache's bytes where a batch fills the GPU: 64 decode requests over 16
 // links of 1024 and 128 own tokens, 32/8 heads x 128, 1.18 GB in 171 us, 6.9 TB/s of
-// the 7.1 of a plain read stream. Else by the latency of a wave's tiles, about 1 us
+// the 7.1 of a plain read stream. Else by the latency of a wave's tiles, about 1.2 us
 // each, between some 3 us of start (tables, queries, first tile) and end.
 //
 // The tiles of the cache hold their codes in the order of the matrix
@@ -76,10 +76,14 @@ __device__ __forceinline__ uint4 load_codes(const char *p) {
   return make_uint4(w.x, w.y, w.z, w.w);
 }
 
-// A 64-key tile of the cache as loaded. kOnce: its codes pass the caches by, as those
-// that nobody else reads should (64 decode requests with 16 documents of their own each,
-// 1 GB: 179 us, cached 210); where several row blocks read them, cached is faster (16
-// requests of 16 tokens over 4..12 of 64 documents, 51 -> 47 us, 64-wide heads 38 -> 34).
+// A 64-key tile of the cache as loaded. kOnce: its codes pass the caches by. Chosen by the
+// rows of a request alone: those of one row block (up to 16 rows), whose documents may be its
+// own (64 decode requests with 16 of their own each, 1 GB: 177 us, cached 207; 64-wide heads
+// 93, 108). Where several row blocks read them, cached is faster (16 requests of 16 tokens
+// over 4..12 of 64 documents, 51 -> 47 us, 64-wide 38 -> 34). Documents that decode requests
+// share would rather be cached, too, from about two readers each on: 64 requests over 16 of
+// 1024 documents 167 us, cached 169 (64-wide 92, 88), of 64 documents 138, 114 (85, 75), over
+// 8 of 8 67, 64 (43, 42), 16 requests of 1..4 tokens over 4..12 of 64 20.3, 20.3 (14.4, 14.0).
 template <int D, bool kOnce>
 struct CacheTile {
   static constexpr int kKeyBlocks = 4;

@@ -1011,7 +1011,8 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     c.min_piece = 1;
   } else if (kern == Kern::Fp4Prefill) {
     // Tiles of 64 keys, every CU full: 1.9 us at 128, 2.4 at 64 (two workgroups to
-    // a CU; 1.5 for one alone). A shorter piece than four tiles writes more partial
+    // a CU; 1.5 for one alone, as some are at a call's end: planned with 2.2, but seven
+    // ragged batches measure the same with 2.4). A shorter piece than four tiles writes more partial
     // sums than it reads of the cache (one request of 148 rows over 110 tiles,
     // pieces of 2 / 4 / 8 tiles: 40 / 29 / 33 us).
     us = d.d_k == 128 ? 1.9 : 2.2;
