@@ -23,9 +23,9 @@
 // first tile in which a row sees a key always is. Sums are fp32 of the probabilities
 // before they are rounded to bf16 for the product. (Sums that leave the fp32 range: fp4_bias.)
 //
-// Bound by the issue of a SIMD that its two waves share: matrix instructions take 47% of
-// the cycles and vector ones 41% (16 requests of 512 tokens over 8..20 links of 1024, 32/8
-// heads x 128: 1.72 ms, 1144 TFLOP/s; 64-wide heads, 8 requests over 16 links, 900). The next
+// Bound by the issue of a SIMD that its two waves share: matrix instructions are busy 48% of
+// the cycles and vector ones issue in 42% (16 requests of 512 tokens over 8..20 links of 1024,
+// 32/8 heads x 128: 1.72 ms, 1144 TFLOP/s; 64-wide heads, 8 requests over 16 links, 900). The next
 // tile's scores formed between this one's probabilities, in a second set of registers,
 // measured the same (1727 against 1711 us), although no wave waited for LDS any more;
 // without barriers and widening that would take 1510 us.

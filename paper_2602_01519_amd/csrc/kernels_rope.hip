@@ -11,8 +11,8 @@
 // reduced there (t - rint t, exact), so that far positions lose nothing: at
 // 2^31 the product's rounding is 2^-24 revolutions. Sine and cosine are then
 // fp32 of at most half a turn. Products in fp32, one rounding to the output.
-// 8192 tokens x (32 + 8) heads x 128, bf16, slices of one projection: 31 us, 5.4 TB/s of a
-// copy's 4.7; 4099 x 17 x 192 fp32, 64 of them turned: 25.5 us, 4.2 TB/s. (The first rows'
+// 8192 tokens x (32 + 8) heads x 128, bf16, slices of one projection: 29.6 us, 5.7 TB/s of a
+// copy's 4.7; 4099 x 17 x 192 fp32, 64 of them turned: 25.8 us, 4.2 TB/s. (The first rows'
 // loads before the angles: 34 and 24.4 us. At most 64 registers, eight waves per
 // SIMD: the latter 27.1 us without.)
 //
