@@ -144,3 +144,14 @@ def test_the_reference_agrees_on_ordinary_values(form):
     c = Call(form, seed=14)
     with c.store() as store:
         check(c, c.run(store))
+
+
+@pytest.mark.parametrize("form", ["own_only", "tails", "own_900", "own_900_64", "limits_own"])
+def test_own_values_near_the_largest(form):
+    """A channel of own values 2.6% below bf16's largest number: their means stay finite."""
+    c = Call(form, seed=15)
+    c.v_own = c.v_own.copy()
+    c.v_own[:, :, 9] = M.bf16(3.3e38)
+    c.v_own[:, :, 40] = M.bf16(np.where(np.arange(len(c.v_own)) % 2, 3.3e38, -3.3e38))[:, None]
+    with c.store() as store:
+        check(c, c.run(store))
