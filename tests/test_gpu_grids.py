@@ -99,12 +99,12 @@ def test_a_batch_of_many_requests_in_pieces():
 
 @pytest.mark.parametrize("links", [1, 40])
 def test_one_request_of_more_than_a_launch(links):
-    """2^30 query rows of one request in blocks of 16: refused on the host, before any tensor is
-    looked at (40 links: not a small call)."""
+    """2^29 query rows of one request (a call has at most 2^30 - 1) in blocks of 16: refused on the
+    host, before any tensor is looked at (40 links: not a small call)."""
     x = torch.zeros(64, 1, 8, dtype=torch.bfloat16, device="cuda")
     st = torch.cuda.current_stream().cuda_stream
     with pic.Store(pic.GQA, pic.BF16, 1, 8, 8, 64) as store:
         store.put(1, 64, x, x, st)
         with pytest.raises(pic.PicError) as e:
-            pic.link_attn(store, [0, links], [1] * links, [0, 1 << 20], None, 1024, x, None, None, 1.0, x, None, stream=st)
+            pic.link_attn(store, [0, links], [1] * links, [0, 1 << 19], None, 1024, x, None, None, 1.0, x, None, stream=st)
         assert e.value.status == pic.ERR_UNSUPPORTED
