@@ -618,7 +618,8 @@ def exact(case, seed):
             qh = q[q0:q0 + lq, h * group:(h + 1) * group].double()
             seen = torch.ones(lq, len(kh), dtype=torch.bool, device="cuda")
             for i in range(lq):
-                seen[i, docs + ls - lq + i + 1:] = False
+                if ls:
+                    seen[i, docs + ls - lq + i + 1:] = False
                 if which is None:
                     ids = _chosen(c, s, s.mine[r], kd[h], qh[i])
                     taken[q0 + i, h, :len(ids)] = torch.tensor(ids, dtype=torch.int32)
