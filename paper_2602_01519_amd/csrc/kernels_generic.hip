@@ -1325,6 +1325,7 @@ hipError_t launch_link_lean(const LinkParams &p, const LeanTabs &t, int dtype, h
 }
 
 int valu_rows_per_block() { return kValuRows; }
+int valu_most_d_v() { return 512; }      // 8 value dims a lane
 
 size_t valu_lds_bytes_for(int esz, int mla, int d_k, int d_v) {
   return valu_lds_bytes(esz, mla, d_k, d_v);

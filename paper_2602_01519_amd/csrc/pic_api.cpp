@@ -1262,6 +1262,8 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   if (kern == Kern::Valu && valu_lds_bytes_for(s->esz, mla, d.d_k, d.d_v) > 160 * 1024)
     return fail(PIC_ERR_UNSUPPORTED, "head widths d_k=%d d_v=%d exceed the generic kernel's LDS",
                 d.d_k, d.d_v);
+  if (kern == Kern::Valu && !C.lean && d.d_v > valu_most_d_v())
+    return fail(PIC_ERR_UNSUPPORTED, "d_v=%d: the generic kernel takes at most %d", d.d_v, valu_most_d_v());
   C.kern = kern;
   StreamShape ss{0, 1, 4};
   if (kern == Kern::Stream) ss = stream_shape(d.dtype, d.d_k, P.max_rows, C.small);

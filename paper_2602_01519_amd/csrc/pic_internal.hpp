@@ -455,6 +455,7 @@ hipError_t launch_prologue(const LinkParams &p, const LinkEntry *links, const Re
 hipError_t launch_link_valu(const LinkParams &p, int dtype, int mla, hipStream_t st,
                             const char **name);
 int valu_rows_per_block();
+int valu_most_d_v();
 
 // bf16 GQA link attention on MFMA, d_k = d_v = 128 (prefill-shaped).
 hipError_t launch_link_mfma_d128(const LinkParams &p, hipStream_t st, const char **name);
