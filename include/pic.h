@@ -122,8 +122,8 @@ typedef struct pic_store pic_store;
 pic_status pic_store_create(const pic_store_desc *desc, pic_store **out);
 
 /* Waits for the device, then frees the store and everything it owns.
- * NULL is accepted and ignored. Errors: INVALID while link plans of the
- * store are alive (destroy them first). */
+ * NULL is accepted and ignored. Errors: INVALID while link plans or block
+ * indexes of the store are alive (destroy them first). */
 pic_status pic_store_destroy(pic_store *store);
 
 /* Compile-stage entry (Sec. 3 steps 3-4): copies one chunk's caches into the
@@ -172,6 +172,60 @@ pic_status pic_store_derive(pic_store *store, uint64_t new_id, uint64_t base_id,
 pic_status pic_store_write_rows(pic_store *store, uint64_t chunk_id, int32_t layer,
                                 int32_t n_rows, const int32_t *rows, const void *k,
                                 const void *v, void *stream);
+
+/* Growing chunks: a request's own tokens kept in the store's pages, so that a decode
+ * step hands over its new tokens only (a generated token is appended to the query
+ * sequence, Sec. 4) and links the chunk behind its documents.
+ * pic_store_open: chunk_id becomes an empty chunk with pages for max_tokens tokens
+ *   reserved (1 .. 2^29 - 1). Host only. Errors: INVALID, EXISTS, OOM (pool full),
+ *   UNSUPPORTED (a 4-bit store).
+ * pic_store_append: tokens offsets[i] .. offsets[i+1]-1 of the sources become the next
+ *   rows of growing chunk chunk_ids[i] in one layer (each layer of a chunk grows by
+ *   calls of its own; a link call sees what its layer holds). With a rotary handle
+ *   (pic_rope_create; its dtype the store's, its head_dim d_k) the keys, and the
+ *   queries where q is given, are turned by their positions on the way, as by
+ *   pic_rope_apply; v is not. Without one they are copied.
+ *     chunk_ids, offsets  host, n_chunks and n_chunks + 1 entries; no id twice
+ *     k  device [n][n_kv_heads][d_k], v [n][n_kv_heads][d_v] (NULL for MLA), n =
+ *        offsets[n_chunks], token t at t * stride elements (0: dense; else at least a
+ *        row: slices of a fused projection)
+ *     q, q_out  device [n][n_q_heads][d_k] (strides alike) or both NULL; q_out may be q
+ *        (same stride); buffers must not overlap otherwise
+ *     positions  device int32 [n], any value (with a handle)
+ *   Several chunks of a batch are one launch. Ordered on `stream`; link calls already
+ *   enqueued on another stream may see either content of a chunk's last page. A captured
+ *   call writes the same rows again when it is replayed. Errors: INVALID (not a growing
+ *   chunk, one that a live plan links, bad arguments), NOT_FOUND, OOM (beyond max_tokens),
+ *   HIP; on an error no chunk has grown.
+ * pic_store_truncate: chunk chunk_ids[i] keeps at most its first n_tokens[i] tokens in
+ *   every layer (n_tokens[i] at most what some layer holds): tokens that were proposed
+ *   and not accepted. The rows taken back are cleared on `stream`. Errors: INVALID, NOT_FOUND,
+ *   HIP.
+ * A growing chunk is linked, gathered, removed and exported like any other (one without
+ * tokens adds no rows; pic_store_lookup: the fewest tokens of any layer, which is also what
+ * an export holds); a link plan takes it as it stands, with as many tokens in every layer,
+ * and it neither grows nor shrinks while the plan lives. pic_store_derive refuses it
+ * (INVALID). */
+pic_status pic_store_open(pic_store *store, uint64_t chunk_id, int64_t max_tokens);
+typedef struct pic_rope pic_rope;
+typedef struct pic_append {
+  int32_t layer;
+  int32_t n_chunks;
+  const uint64_t *chunk_ids;
+  const int32_t *offsets;
+  const void *k;
+  const void *v;
+  int64_t k_stride, v_stride;
+  const pic_rope *rope;      /* or NULL */
+  const int32_t *positions;
+  const void *q;
+  void *q_out;
+  int64_t q_stride, q_out_stride;
+  int32_t n_q_heads;
+} pic_append;
+pic_status pic_store_append(pic_store *store, const pic_append *append, void *stream);
+pic_status pic_store_truncate(pic_store *store, int32_t n, const uint64_t *chunk_ids,
+                              const int64_t *n_tokens, void *stream);
 
 /* Handing a store to another process on the same GPU, in place: the PIC
  * manager of the paper sends the handles of the PICaches it collected to the
@@ -343,6 +397,74 @@ pic_status pic_link_plan_run(pic_link_plan *plan, int32_t layer, const void *q,
                              void *out, float *lse, void *stream);
 pic_status pic_link_plan_destroy(pic_link_plan *plan);
 
+/* Link attention of requests that share linked chunks: users who ask about the same
+ * documents. Group g is the requests request_offsets[g] .. request_offsets[g+1]-1 of the
+ * batch; all of them see the group's shared links (chunk_offsets, chunk_ids, chunk_starts,
+ * as in pic_link_req, by group), then their own links and own KV (req). The result is that of
+ * pic_link_attn with the shared links put before each request's own ones, to
+ * floating-point rounding order; but a group's shared rows are read once for all of its
+ * query tokens, and every row's partial softmax states over both are merged exactly. Chunk
+ * caches depend on no position, so any documents that the requests have in common can be
+ * shared, in any order.
+ *   req: as for pic_link_attn, own links and own KV may be empty; q_doc_limits count the
+ *     rows of a request's own links (shared ones are seen by every query token).
+ *   groups: host arrays, n_groups and n_groups + 1 entries, the last of request_offsets
+ *     the batch. A group may be empty or share nothing.
+ * Tensors, scale and lse as for pic_link_attn. Workspace: fp32 partials of every query row,
+ * about 2 Tq * H_q * (d_v + 2) * 4 bytes or more where keys are split.
+ * pic_link_shared_plan_create: the same, resolved once (req->layer must be 0), run and
+ *   destroyed by pic_link_plan_run and pic_link_plan_destroy: a run enqueues kernels only.
+ * Errors: as pic_link_attn; the plan's also OOM. */
+typedef struct pic_link_groups {
+  int32_t n_groups;
+  const int32_t *request_offsets;
+  const int32_t *chunk_offsets;
+  const uint64_t *chunk_ids;
+  const int32_t *chunk_starts;   /* or NULL */
+} pic_link_groups;
+pic_status pic_link_shared(pic_store *store, const pic_link_req *req,
+                           const pic_link_groups *groups, int32_t n_q_heads, const void *q,
+                           const void *k_self, const void *v_self, float softmax_scale, void *out,
+                           float *lse, void *stream);
+pic_status pic_link_shared_plan_create(pic_store *store, const pic_link_req *req,
+                                       const pic_link_groups *groups, int32_t n_q_heads,
+                                       pic_link_plan **out);
+
+/* Link attention over selected blocks, for long document sets: each query token attends over
+ * the linked blocks that a cheap score finds for it, and over its own KV. A block is 64 tokens of
+ * a linked chunk, from its first linked token on (a chunk's last one may be shorter); a
+ * request's blocks are counted over its links in order. fp32 and bf16 GQA stores, d_k = d_v of
+ * 64 or 128 (else UNSUPPORTED).
+ *   summary  of a block and kv head: the mean of its K rows, rounded to fp32 and then to bf16
+ *   score    of a block for a query token and kv head: the largest dot product of the summary
+ *            with a query head of that kv head's group (summed in 64 bits; NaN counts as -inf)
+ *   taken    the first keep_first and the last keep_last of the request's blocks, then those of
+ *            the largest scores, n_blocks in all (all blocks, if it has no more); of equal
+ *            scores the lower block
+ * A block index holds a store's summaries (n_layers * capacity / 64 * H_kv * d_k * 2 bytes):
+ * pic_index_create: nothing indexed yet. The store must outlive the index
+ *   (pic_store_destroy refuses while one is alive). Errors: INVALID, UNSUPPORTED, OOM, HIP.
+ * pic_index_update: forms the summaries of the listed chunks (host, an id may repeat) in
+ *   one layer, or in all of them for layer -1, as the chunks stand; ordered on `stream`. To be
+ *   called again when a chunk has been written to, has grown (only blocks that grew are
+ *   formed again) or has been put anew. Errors: INVALID, NOT_FOUND, HIP.
+ * pic_index_destroy: waits for the device and frees the index; NULL is ignored.
+ * pic_link_sparse: tensors, scale and lse as for pic_link_attn; req->q_doc_limits must be
+ *   NULL. blocks: device int32 [Tq][n_kv_heads][n_blocks] or NULL: receives the taken blocks,
+ *   ascending, -1 behind them. n_blocks 1 .. 1024, a request's blocks at most 8192 (else
+ *   UNSUPPORTED). One token a request is the ordinary use (a decode step); several are
+ *   computed one by one. Errors: INVALID (also a linked chunk whose summaries in the layer are
+ *   not those of its present content), NOT_FOUND, UNSUPPORTED, OOM, HIP. */
+typedef struct pic_index pic_index;
+pic_status pic_index_create(pic_store *store, pic_index **out);
+pic_status pic_index_update(pic_index *index, int32_t layer, int32_t n, const uint64_t *chunk_ids,
+                            void *stream);
+pic_status pic_index_destroy(pic_index *index);
+pic_status pic_link_sparse(pic_index *index, const pic_link_req *req, int32_t n_q_heads,
+                           int32_t n_blocks, int32_t keep_first, int32_t keep_last, const void *q,
+                           const void *k_self, const void *v_self, float softmax_scale, void *out,
+                           float *lse, int32_t *blocks, void *stream);
+
 /* Test hook: materialises the concatenation (Sec. 4.2) of the listed chunks
  * of one layer, in the given order, reading the pool through the same
  * address resolution the attention kernels use. k_out: device token-major
@@ -452,7 +574,6 @@ typedef struct pic_rope_tensor {
   int64_t x_stride, out_stride;
   int32_t n_heads;
 } pic_rope_tensor;
-typedef struct pic_rope pic_rope;
 pic_status pic_rope_create(const pic_rope_desc *desc, pic_rope **out);
 pic_status pic_rope_destroy(pic_rope *rope);
 pic_status pic_rope_apply(const pic_rope *rope, int32_t n_tokens, const int32_t *positions,

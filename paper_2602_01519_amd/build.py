@@ -29,6 +29,9 @@ SOURCES = [
     "kernels_fp4_decode.hip",
     "kernels_fp4_prefill.hip",
     "kernels_rope.hip",
+    "kernels_append.hip",
+    "kernels_shared.hip",
+    "kernels_sparse.hip",
     "static_scratch.hip",
 ]
 

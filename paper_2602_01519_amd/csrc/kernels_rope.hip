@@ -24,6 +24,7 @@
 #include <algorithm>
 
 #include "pic_internal.hpp"
+#include "rope_row.hpp"
 
 namespace pic {
 namespace {
@@ -32,73 +33,17 @@ constexpr int kThreads = 256;
 constexpr int kMostBlocks = (1 << 24) - 1;     // of kThreads in one launch
 constexpr int kBatch = 2;         // rows whose loads a lane has in flight
 
-template <typename T>
-struct Vec;
-template <>
-struct Vec<float> {
-  static constexpr int n = 4;
-  __device__ static float get(const uint4 &v, int i) {
-    return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
-  }
-  __device__ static uint4 put(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                      __float_as_uint(x[3]));
-  }
-  __device__ static float load(const float *p) { return *p; }
-  __device__ static void store(float *p, float x) { *p = x; }
-};
-template <>
-struct Vec<uint16_t> {
-  static constexpr int n = 8;
-  __device__ static float get(const uint4 &v, int i) {
-    const uint32_t w = i / 2 == 0 ? v.x : i / 2 == 1 ? v.y : i / 2 == 2 ? v.z : v.w;
-    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
-  }
-  __device__ static uint4 put(const float (&x)[8]) {
-    __bf16 v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
-    return __builtin_bit_cast(uint4, v);
-  }
-  __device__ static float load(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
-  __device__ static void store(uint16_t *p, float x) {
-    *p = __builtin_bit_cast(uint16_t, (__bf16)x);
-  }
-};
-
-// 16 bytes read once (nontemporal: 8192 tokens x 40 heads x 128 bf16 in 32.5 us
-// against 36.5).
-__device__ __forceinline__ uint4 load_nt(const void *p) {
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  const u32x4 v = __builtin_nontemporal_load((const u32x4 *)p);
-  return make_uint4(v.x, v.y, v.z, v.w);
-}
-
-// Quotient of small numbers (below 2^22) by a constant's reciprocal.
-__device__ __forceinline__ int div_small(int x, float inv) { return (int)(((float)x + 0.5f) * inv); }
-
 template <typename T, bool kHalf>
 __global__ __launch_bounds__(kThreads, 8) void rope_kernel(RopeParams p) {
-  typedef Vec<T> V;
-  constexpr int N = V::n;
+  constexpr int N = Vec<T>::n;
   extern __shared__ float trig[];     // [token][cos: half][sin: half], each part 16-byte aligned
   const int half = p.rot / 2, part = (half + 7) / 8 * 8;
   const int tok0 = blockIdx.x * p.tokens;
   const int ntok = min(p.tokens, p.n_tokens - tok0);
   const int slot = div_small(threadIdx.x, p.inv_lanes), chunk = threadIdx.x - slot * p.lanes;
   // this lane's piece of a row
-  const bool rot = chunk < p.rot_chunks;
-  int at, len;                        // first element; elements up to the part's end
-  if (rot) {
-    at = p.rot_at + chunk * N;
-    len = (kHalf ? half : p.rot) - chunk * N;
-  } else {
-    const int c = chunk - p.rot_chunks, lead = (p.rot_at + N - 1) / N;
-    at = c < lead ? c * N : p.rot_at + p.rot + (c - lead) * N;
-    len = (c < lead ? p.rot_at : p.width) - at;
-  }
-  const bool whole = len >= N;
-  const int pair0 = kHalf ? chunk * N : chunk * N / 2;
+  const RowPiece pc = row_piece<T, kHalf>(chunk, p.rot_chunks, p.width, p.rot_at, p.rot);
+  const bool rot = pc.rot, whole = pc.len >= N;
   const int h0 = blockIdx.y * p.heads_per_block;
   const int heads = min(p.heads_per_block, p.heads - h0);
   const float inv_heads = 1.f / (float)heads;
@@ -119,8 +64,8 @@ __global__ __launch_bounds__(kThreads, 8) void rope_kernel(RopeParams p) {
       tok[k] = t;
       int i = 0;
       while (h >= p.t[i].heads) h -= p.t[i++].heads;
-      src[k] = (const T *)p.t[i].x + (tok0 + t) * p.t[i].x_stride + h * p.width + at;
-      dst[k] = (T *)p.t[i].out + (tok0 + t) * p.t[i].out_stride + h * p.width + at;
+      src[k] = (const T *)p.t[i].x + (tok0 + t) * p.t[i].x_stride + h * p.width + pc.at;
+      dst[k] = (T *)p.t[i].out + (tok0 + t) * p.t[i].out_stride + h * p.width + pc.at;
       if (whole) {
         a[k] = load_nt(src[k]);
         if (kHalf && rot) b[k] = load_nt(src[k] + half);
@@ -147,40 +92,12 @@ __global__ __launch_bounds__(kThreads, 8) void rope_kernel(RopeParams p) {
         if (whole) {
           *(uint4 *)dst[k] = a[k];
         } else {
-          for (int i = 0; i < len; ++i) dst[k][i] = src[k][i];
+          for (int i = 0; i < pc.len; ++i) dst[k][i] = src[k][i];
         }
         continue;
       }
-      const float *cs = trig + tok[k] * 2 * part + pair0, *sn = cs + part;
-      if (whole) {
-        float x[N], y[N];
-        if (kHalf) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float u = V::get(a[k], i), w = V::get(b[k], i), c = cs[i], s = sn[i];
-            x[i] = u * c - w * s;
-            y[i] = u * s + w * c;
-          }
-          *(uint4 *)dst[k] = V::put(x);
-          *(uint4 *)(dst[k] + half) = V::put(y);
-        } else {
-#pragma unroll
-          for (int i = 0; i < N; i += 2) {
-            const float u = V::get(a[k], i), w = V::get(a[k], i + 1), c = cs[i / 2], s = sn[i / 2];
-            x[i] = u * c - w * s;
-            x[i + 1] = u * s + w * c;
-          }
-          *(uint4 *)dst[k] = V::put(x);
-        }
-      } else {
-        const int step = kHalf ? 1 : 2, other = kHalf ? half : 1;
-        for (int i = 0; i < len; i += step) {
-          const float u = V::load(src[k] + i), w = V::load(src[k] + i + other);
-          const float c = cs[i / step], s = sn[i / step];
-          V::store(dst[k] + i, u * c - w * s);
-          V::store(dst[k] + i + other, u * s + w * c);
-        }
-      }
+      const float *cs = trig + tok[k] * 2 * part + pc.pair0;
+      turn_piece<T, kHalf>(pc, src[k], dst[k], a[k], b[k], half, cs, cs + part);
     }
   }
 }
@@ -189,11 +106,11 @@ __global__ __launch_bounds__(kThreads, 8) void rope_kernel(RopeParams p) {
 
 hipError_t launch_rope(RopeParams p, int dtype, bool half, const DevShape &ds, hipStream_t st) {
   const int n = dtype == 0 ? 4 : 8;
-  p.rot_chunks = (half ? p.rot / 2 + n - 1 : p.rot + n - 1) / n;
+  p.rot_chunks = rot_pieces(n, half, p.rot);
   // copies only where some tensor is not in place
   int copies = 0;
   for (int i = 0; i < p.n_tensors; ++i)
-    if (p.t[i].x != p.t[i].out) copies = (p.rot_at + n - 1) / n + (p.width - p.rot_at - p.rot + n - 1) / n;
+    if (p.t[i].x != p.t[i].out) copies = copy_pieces(n, p.width, p.rot_at, p.rot);
   p.lanes = p.rot_chunks + copies;
   p.slots = kThreads / p.lanes;
   p.inv_lanes = 1.f / (float)p.lanes;

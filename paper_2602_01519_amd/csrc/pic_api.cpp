@@ -12,6 +12,8 @@
 #include <cstring>
 #include <functional>
 #include <map>
+#include <memory>
+#include <new>
 #include <initializer_list>
 #include <mutex>
 #include <numeric>
@@ -52,6 +54,16 @@ pic_status hip_fail(hipError_t e, const char *what) {
     if (e_ != hipSuccess) return hip_fail(e_, what); \
   } while (0)
 
+// Runs the body of an entry point; a host allocation that fails becomes a status.
+template <typename F>
+pic_status guarded(F &&body) {
+  try {
+    return body();
+  } catch (const std::exception &) {
+    return fail(PIC_ERR_OOM, "host allocation failed");
+  }
+}
+
 // Restores the caller's current device on scope exit.
 struct DeviceGuard {
   int prev = -1;
@@ -86,10 +98,26 @@ struct Run {
 };
 
 struct Slot {
+  // Renewed with every change of the content but an append (see pic_index).
+  uint64_t version = 0;
   int64_t len;
   std::vector<Run> runs;
   int64_t plan_refs = 0;   // live link plans that link this chunk
   bool derived = false;    // made by pic_store_derive (rows may be written)
+  // A growing chunk (pic_store_open): its runs cover all reserved pages, len is the fewest
+  // tokens of a layer, layer_len each layer's.
+  bool grows = false;
+  int64_t max_tokens = 0;
+  std::vector<int32_t> layer_len;
+
+  int64_t tokens(int32_t layer) const { return grows ? layer_len[layer] : len; }
+  // Tokens of a run that are there, of a chunk's n.
+  static int32_t filled(const Run &r, int64_t n) {
+    return (int32_t)std::max<int64_t>(0, std::min<int64_t>(r.ntok, n - r.tok0));
+  }
+  bool even() const {      // every layer holds as many tokens
+    return std::all_of(layer_len.begin(), layer_len.end(), [&](int32_t n) { return n == layer_len[0]; });
+  }
 };
 
 // Pinned host table + device copy + completion event. The planner writes a
@@ -150,6 +178,12 @@ DevShape device_shape() {
 }
 }  // namespace pic
 
+// Rotary positions: the description and the angle per position of each pair.
+struct pic_rope {
+  pic_rope_desc desc{};
+  double rev[kRopeMost / 2] = {};   // revolutions per position
+};
+
 struct pic_store {
   pic_store_desc desc{};
   int device = 0;
@@ -165,7 +199,8 @@ struct pic_store {
   std::vector<std::pair<hipEvent_t, std::vector<Run>>> pending;
   int32_t n_layers = 1;
   int64_t layer_bytes = 0;       // bytes of one layer's pool; layer l of a slot is l * layer_bytes on
-  int64_t live_plans = 0;
+  int64_t live_plans = 0, live_indexes = 0;
+  uint64_t versions = 0;         // Slot::version of the newest content
   int64_t k_tok_elems = 0;       // K elements per padded token (all heads)
   int64_t v_tok_elems = 0;       // V elements per padded token (GQA)
   int64_t page_bytes = 0;        // bytes of a 64-token page in one layer
@@ -403,6 +438,7 @@ struct Plan {
   bool self = false;             // requests carry own KV
   int64_t total_self = 0;        // own tokens over the batch
   std::vector<uint64_t> ids;     // every linked chunk id (with repeats)
+  std::vector<int32_t> pages;    // first page of every document link
   // per query token: linked rows visible to it; empty unless the rows of
   // some request see different numbers of them (the kernels mask per row)
   std::vector<int32_t> doc_lim;
@@ -456,6 +492,7 @@ pic_status plan_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, f
   P.links.clear();
   P.links.reserve(n_links + B);
   P.ids.clear();
+  P.pages.clear();
   P.reqs.resize(B);
   P.doc_lim.clear();
   bool mixed_limits = false;
@@ -482,12 +519,16 @@ pic_status plan_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, f
         return fail(PIC_ERR_NOT_FOUND, "request %d link %d: chunk id 0x%llx not in the store", r,
                     c, (unsigned long long)id);
       const Slot &sl = it->second;
+      const int64_t len = sl.tokens(layer);
       const int32_t start = req->chunk_starts ? req->chunk_starts[c0 + c] : 0;
-      if (start < 0 || start % kTile || start >= sl.len)
+      // (a growing chunk may be empty)
+      if (start < 0 || start % kTile || (start >= len && start > 0))
         return fail(PIC_ERR_INVALID,
                     "request %d link %d: start %d must be a multiple of %d below the chunk's %lld "
-                    "tokens", r, c, start, kTile, (long long)sl.len);
-      for (const Run &run : sl.runs) {
+                    "tokens", r, c, start, kTile, (long long)len);
+      for (Run run : sl.runs) {
+        run.ntok = Slot::filled(run, len);
+        if (run.ntok == 0) break;
         if (run.tok0 + run.ntok <= start) continue;
         LinkEntry E = run_entry(s, run, layer);
         // skip the run's pages before `start`
@@ -497,6 +538,7 @@ pic_status plan_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, f
         E.tile0 = (int32_t)tiles;
         E.tok0 = (int32_t)toks;
         P.links.push_back(E);
+        P.pages.push_back((int32_t)(run.page0 + run.skip + skip / kTile));
         tiles += (E.len + kTile - 1) / kTile;
         toks += E.len;
       }
@@ -620,6 +662,9 @@ struct Setup {
   std::vector<CombineEntry> comb;    // their partial rows (when some request is split)
   int32_t tile_keys = kTile;     // keys per tile of the kernel's work items
   int32_t n_items = 0;
+  // every row's softmax state goes to the partials, also of a request in one piece; the
+  // caller sets lp.part_* and merges them
+  bool partial = false;
   bool lean = false;             // a small call the lean kernel runs
   bool small = false;            // tables as a kernel argument, own KV in place
   int32_t rows_per_block = 0;    // rows of a workgroup (decode kernel: wave)
@@ -678,7 +723,7 @@ void write_items(const Setup &C, const LinkEntry *links, WorkItem *out) {
       w.lq = R.lq;
       w.ls = R.ls;
       w.doc_tiles = R.doc_tiles;
-      w.part = S > 1 ? (int32_t)(C.comb[r].part0 + i * C.comb[r].rows) : -1;
+      w.part = S > 1 || C.partial ? (int32_t)(C.comb[r].part0 + i * C.comb[r].rows) : -1;
       *out++ = w;
     }
   }
@@ -1129,13 +1174,15 @@ void apply_splits(pic_store *s, int32_t n_q_heads, int rows_per_block, Setup &C)
   }
   C.part_rows = 0;
   C.comb.clear();
-  if (C.splits > 1) {
+  if (C.splits > 1 || C.partial) {
     C.comb.resize(B);
     for (int r = 0; r < B; ++r) {
       const int32_t S = C.req_splits[r], rows = P.reqs[r].lq * n_q_heads;
       C.comb[r] = CombineEntry{P.reqs[r].q0 * n_q_heads, rows, (int32_t)C.part_rows, S};
-      if (S > 1) C.part_rows += (int64_t)rows * S;
+      if (S > 1 || C.partial) C.part_rows += (int64_t)rows * S;
     }
+  }
+  if (C.splits > 1) {
     // longest pieces first
     std::stable_sort(P.order.begin(), P.order.end(), [&](int32_t a, int32_t b) {
       return (int64_t)P.reqs[a].tiles * C.req_splits[b] > (int64_t)P.reqs[b].tiles * C.req_splits[a];
@@ -1249,14 +1296,14 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   // a kernel argument, at most kLeanTiles tiles in all) runs it; other fp32
   // and narrow bf16 GQA calls stream their keys through the matrix cores.
   if (kern == Kern::Valu && !mla) {
-    if (lean_supported(d.dtype, d.d_k, d.d_v, lp.group) && small_tables(P)) {
+    if (!C.partial && lean_supported(d.dtype, d.d_k, d.d_v, lp.group) && small_tables(P)) {
       int64_t tiles = 0;
       for (const ReqEntry &R : P.reqs) tiles += R.tiles;
       C.lean = tiles <= kLeanTiles;
     }
     if (!C.lean && stream_supported(d.dtype, d.d_k, d.d_v)) kern = Kern::Stream;
   }
-  C.small = small_tables(P) &&
+  C.small = !C.partial && small_tables(P) &&
             (kern == Kern::Valu || (kern == Kern::Stream && (mode == Mode::Decode ||
                                                              P.max_rows <= kStreamSmallRows)));
   if (kern == Kern::Valu && valu_lds_bytes_for(s->esz, mla, d.d_k, d.d_v) > 160 * 1024)
@@ -1322,7 +1369,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
     // scratch, also where uneven requests are cut into more pieces than the
     // charge counts or the work items need more than its slack. Cut here, for
     // both entries, so that their results are the same.
-    if (mode == Mode::Decode && noalloc_charge(s, C, num_splits) <= kStaticScratchBytes)
+    if (mode == Mode::Decode && !C.partial && noalloc_charge(s, C, num_splits) <= kStaticScratchBytes)
       while (table_layout(C).bytes + C.work_bytes() > kStaticScratchBytes + kStaticScratchSlack &&
              C.splits > 1)
         fewer_pieces(s, n_q_heads, C);
@@ -1362,6 +1409,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
       splits = std::max(splits, (int32_t)std::min<int64_t>(16, slots / blocks));
     splits = std::max(1, std::min(splits, P.max_tiles / min_piece));
   }
+  if (C.partial) splits = std::max(splits, 2);   // (the vector-ALU kernel writes partials if split)
   C.splits = splits;
   lp.num_splits = splits;
   lp.spread = kern == Kern::Stream;
@@ -1378,7 +1426,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
 // and nothing to combine but one request's pieces, which need no table (one request of
 // 37 tokens over 10 links 26.0 -> 21.4 us, of 300 over 12 66 -> 62).
 bool fp4_tabs(const Setup &C) {
-  return (C.kern == Kern::Fp4 || C.kern == Kern::Fp4Prefill) && C.P.doc_lim.empty() &&
+  return (C.kern == Kern::Fp4 || C.kern == Kern::Fp4Prefill) && !C.partial && C.P.doc_lim.empty() &&
          (C.splits == 1 || C.P.reqs.size() == 1) && C.n_items <= launch_items(C) &&
          C.n_items * sizeof(WorkItem) + C.P.links.size() * sizeof(LinkEntry) <= kFp4TabBytes;
 }
@@ -1400,7 +1448,7 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
   lp.out = out;
   lp.lse = lse;
   lp.scale_log2 = scale * 1.4426950408889634f;
-  if (C.splits > 1) {
+  if (C.splits > 1 && !C.partial) {
     lp.part_o = (float *)((char *)work + C.part_off);
     lp.part_m = lp.part_o + C.part_rows * d.d_v;
     lp.part_l = lp.part_m + C.part_rows;
@@ -1455,7 +1503,7 @@ pic_status launch_call(const pic_store *s, const Setup &C, LinkParams lp, void *
   }
   prof_stop(st, &ev, name);
   if (e != hipSuccess) return hip_fail(e, name);
-  if (C.splits > 1) {
+  if (C.splits > 1 && !C.partial) {
     e = launch_combine(lp, io_dtype(d), lp.max_rows * d.n_kv_heads, st);
     if (e != hipSuccess) return hip_fail(e, "combine_kernel");
   }
@@ -1582,6 +1630,174 @@ pic_status link_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, c
   return PIC_OK;
 }
 
+// A call of requests that share links in groups: one batch whose requests are the groups (a
+// group's query tokens over its shared links), one of the requests as they are, and the merge
+// of their partials. Tables: [groups' tables][requests' tables][merge entries]; workspace: the
+// requests' own KV laid out, then the partials of both.
+struct SharedCall {
+  Setup pre, own;
+  std::vector<MergeEntry> merge;
+  bool has_pre = false, has_own = false;       // some request sees a key there
+  TableLayout t_pre{}, t_own{};
+  size_t off_own = 0, off_merge = 0, table_bytes = 0, work_bytes = 0;
+  int32_t pieces = 1;                          // most pieces of a row
+};
+
+pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_groups *groups,
+                        int32_t n_q_heads, float scale, int32_t layer, SharedCall &S) {
+  if (!s) return fail(PIC_ERR_INVALID, "store is NULL");
+  if (!req || !groups) return fail(PIC_ERR_INVALID, "req/groups is NULL");
+  const int32_t B = req->batch, G = groups->n_groups;
+  if (B < 0 || G < 0) return fail(PIC_ERR_INVALID, "batch < 0 or n_groups < 0");
+  if (!check_offsets(req->q_offsets, B)) return fail(PIC_ERR_INVALID, "bad q_offsets");
+  if (!check_offsets(groups->request_offsets, G) || groups->request_offsets[G] != B)
+    return fail(PIC_ERR_INVALID, "request_offsets must run from 0 to the batch's %d requests", B);
+  if (!check_offsets(groups->chunk_offsets, G)) return fail(PIC_ERR_INVALID, "bad chunk_offsets of the groups");
+  int32_t most_q = 0, most_group_q = 0;
+  std::vector<int32_t> group_q(G + 1);
+  for (int32_t g = 0; g <= G; ++g) group_q[g] = req->q_offsets[groups->request_offsets[g]];
+  for (int32_t g = 0; g < G; ++g) most_group_q = std::max(most_group_q, group_q[g + 1] - group_q[g]);
+  for (int32_t r = 0; r < B; ++r) most_q = std::max(most_q, req->q_offsets[r + 1] - req->q_offsets[r]);
+  pic_link_req pr{};
+  pr.batch = G;
+  pr.layer = layer;
+  pr.chunk_offsets = groups->chunk_offsets;
+  pr.chunk_ids = groups->chunk_ids;
+  pr.chunk_starts = groups->chunk_starts;
+  pr.q_offsets = group_q.data();
+  S.pre.partial = S.own.partial = true;
+  pic_status rc = setup_call(s, req, n_q_heads, scale, layer, 0, most_q <= 16 ? Mode::Decode : Mode::Prefill, S.own);
+  if (rc != PIC_OK) return rc;
+  rc = setup_call(s, &pr, n_q_heads, scale, layer, 0, most_group_q <= 16 ? Mode::Decode : Mode::Prefill, S.pre);
+  if (rc != PIC_OK) return rc;
+  S.has_pre = S.pre.P.max_tiles > 0;
+  S.has_own = S.own.P.max_tiles > 0;
+  S.merge.resize(B);
+  const auto source = [](const Setup &C, int32_t r, int32_t row, MergeEntry &m, int x) {
+    if (C.kern == Kern::Valu) {                  // pieces of all rows one after another
+      m.part[x] = C.P.reqs[r].q0 * C.lp.n_q_heads + row;
+      m.stride[x] = C.P.total_q * C.lp.n_q_heads;
+      m.splits[x] = C.splits;
+    } else {
+      m.part[x] = C.comb[r].part0 + row;
+      m.stride[x] = C.comb[r].rows;
+      m.splits[x] = C.req_splits[r];
+    }
+  };
+  for (int32_t g = 0; g < G; ++g)
+    for (int32_t r = groups->request_offsets[g]; r < groups->request_offsets[g + 1]; ++r) {
+      MergeEntry &m = S.merge[r];
+      m = MergeEntry{};
+      const ReqEntry &R = S.own.P.reqs[r];
+      m.row0 = R.q0 * n_q_heads;
+      m.rows = R.lq * n_q_heads;
+      if (R.lq == 0) continue;
+      if (S.has_pre && S.pre.P.reqs[g].tiles > 0) source(S.pre, g, (R.q0 - group_q[g]) * n_q_heads, m, 0);
+      if (S.has_own && R.tiles > 0) source(S.own, r, 0, m, 1);
+      S.pieces = std::max(S.pieces, m.splits[0] + m.splits[1]);
+    }
+  S.t_pre = table_layout(S.pre);
+  S.t_own = table_layout(S.own);
+  S.off_own = S.t_pre.bytes;
+  S.off_merge = S.off_own + S.t_own.bytes;
+  S.table_bytes = S.off_merge + round_up(sizeof(MergeEntry) * B, 256);
+  S.work_bytes = S.own.part_off + round_up(S.own.part_bytes, 256) + S.pre.part_bytes;
+  return PIC_OK;
+}
+
+void write_shared_tables(const SharedCall &S, const LinkEntry *pre_links, const LinkEntry *own_links, char *h) {
+  write_tables(S.pre, S.t_pre, pre_links, h);
+  write_tables(S.own, S.t_own, own_links, h + S.off_own);
+  memcpy(h + S.off_merge, S.merge.data(), sizeof(MergeEntry) * S.merge.size());
+}
+
+Partials place_partials(char *at, int64_t rows, int32_t d_v) {
+  Partials p;
+  p.o = (float *)at;
+  p.m = p.o + rows * d_v;
+  p.l = p.m + rows;
+  return p;
+}
+
+// dev: the call's tables (copied there first from host_dev, when not NULL).
+pic_status launch_shared(const pic_store *s, const SharedCall &S, char *dev, const char *host_dev, char *work,
+                         const void *q, const void *k_self, const void *v_self, float scale, void *out,
+                         float *lse, hipStream_t st) {
+  const int32_t d_v = s->desc.d_v;
+  MergeParams m{};
+  m.entries = (const MergeEntry *)(dev + S.off_merge);
+  char *parts = work + S.own.part_off;
+  m.src[1] = place_partials(parts, S.own.part_rows, d_v);
+  m.src[0] = place_partials(parts + round_up(S.own.part_bytes, 256), S.pre.part_rows, d_v);
+  m.out = out;
+  m.lse = lse;
+  m.d_v = d_v;
+  const auto run = [&](const Setup &C, const TableLayout &t, size_t off, const Partials &to, const Prologue &pro,
+                       const void *ks, const void *vs) {
+    LinkParams lp = C.lp;
+    point_tables(C, t, dev + off, lp);
+    lp.part_o = to.o;
+    lp.part_m = to.m;
+    lp.part_l = to.l;
+    return launch_call(s, C, lp, work, pro, q, ks, vs, scale, out, lse, st);
+  };
+  if (S.has_own) {
+    Prologue pro;
+    const char *tables = host_dev ? host_dev : dev;
+    pro.links = (const LinkEntry *)(tables + S.off_own);
+    pro.reqs = (const ReqEntry *)(tables + S.off_own + S.t_own.off_r);
+    if (host_dev) {
+      pro.copy_src = host_dev;
+      pro.copy_dst = dev;
+      pro.copy_bytes = (int64_t)S.table_bytes;
+    }
+    const pic_status rc = run(S.own, S.t_own, S.off_own, m.src[1], pro, k_self, v_self);
+    if (rc != PIC_OK) return rc;
+  } else if (host_dev) {
+    HIP_TRY(launch_table_copy(host_dev, dev, (int64_t)S.table_bytes, st), "table_copy_kernel");
+  }
+  if (S.has_pre) {
+    const pic_status rc = run(S.pre, S.t_pre, 0, m.src[0], Prologue{}, nullptr, nullptr);
+    if (rc != PIC_OK) return rc;
+  }
+  HIP_TRY(launch_merge(m, io_dtype(s->desc), (int32_t)S.merge.size(),
+                       S.own.P.max_rows * s->desc.n_kv_heads, S.pieces, st), "merge_kernel");
+  return PIC_OK;
+}
+
+pic_status shared_link_call(pic_store *s, const pic_link_req *req, const pic_link_groups *groups,
+                            int32_t n_q_heads, const void *q, const void *k_self, const void *v_self,
+                            float scale, void *out, float *lse, hipStream_t st) {
+  SharedCall S;
+  pic_status rc = setup_shared(s, req, groups, n_q_heads, scale, req ? req->layer : 0, S);
+  if (rc != PIC_OK) return rc;
+  if (req->batch == 0) return PIC_OK;
+  rc = check_tensors(s, S.own.P, q, k_self, v_self, out);
+  if (rc != PIC_OK) return rc;
+  if (S.own.P.total_q == 0) return PIC_OK;
+  DeviceGuard dg(s->device);
+  if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+  Stage *stage = nullptr;
+  rc = stage_acquire(s, S.table_bytes, &stage);
+  if (rc == PIC_OK) rc = ensure_work(stage, S.work_bytes);
+  if (rc != PIC_OK) return rc;
+  place_own(s, S.own.P, stage->work, S.own.P.links.data());
+  write_shared_tables(S, S.pre.P.links.data(), S.own.P.links.data(), (char *)stage->host);
+  rc = launch_shared(s, S, (char *)stage->dev, (const char *)stage->host_dev, (char *)stage->work, q, k_self,
+                     v_self, scale, out, lse, st);
+  if (rc != PIC_OK) return rc;
+  HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");
+  stage->pending = true;
+  return PIC_OK;
+}
+
+// Workgroups that share a unit (query token x kv head) of `taken` blocks: as many as the CUs
+// have room for, where each wave of one would take more than two blocks.
+int32_t sparse_splits(int32_t cus, int64_t units, int32_t taken) {
+  const int32_t most = taken / (2 * sparse_waves());
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, cus / std::max<int64_t>(1, units)));
+}
+
 }  // namespace
 
 // A request batch resolved once for repeated calls: the link tables of every
@@ -1599,7 +1815,37 @@ struct pic_link_plan {
   // pic_link_decode run them (tables as a kernel argument)
   bool small = false;
   std::vector<LinkEntry> small_links;
+  // requests that share links (pic_link_shared_plan_create): in place of C
+  std::unique_ptr<SharedCall> shared;
+
+  const Plan &requests() const { return shared ? shared->own.P : C.P; }
 };
+
+namespace {
+
+// A table of one layer's links from layer 0's: layer l of a slot sits l pool layers further
+// on; own-KV links (in the workspace, or read in place with no address) stay.
+std::vector<LinkEntry> layer_links(const pic_store *s, const Plan &P, std::vector<LinkEntry> links, int32_t layer) {
+  std::vector<bool> own(links.size(), false);
+  for (auto &o : P.own) own[o.first] = true;
+  for (size_t i = 0; i < links.size(); ++i)
+    if (!own[i] && links[i].k) {
+      links[i].k = (const char *)links[i].k + (int64_t)layer * s->layer_bytes;
+      links[i].v = (const char *)links[i].v + (int64_t)layer * s->layer_bytes;
+    }
+  return links;
+}
+
+// The growing chunks of a plan, which names every layer's rows, hold as many in each.
+pic_status check_even(const pic_store *s, const std::vector<uint64_t> &ids) {
+  for (uint64_t id : ids)
+    if (!s->map.at(id).even())
+      return fail(PIC_ERR_INVALID, "growing chunk 0x%llx holds more tokens in some layers than in others",
+                  (unsigned long long)id);
+  return PIC_OK;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -1654,6 +1900,9 @@ pic_status pic_store_destroy(pic_store *s) {
   if (s->live_plans > 0)
     return fail(PIC_ERR_INVALID, "%lld link plans of this store are still alive",
                 (long long)s->live_plans);
+  if (s->live_indexes > 0)
+    return fail(PIC_ERR_INVALID, "%lld block indexes of this store are still alive",
+                (long long)s->live_indexes);
   DeviceGuard dg(s->device);
   (void)hipDeviceSynchronize();
   for (Stage &st : s->ring) {
@@ -1743,6 +1992,7 @@ pic_status pic_store_put(pic_store *s, uint64_t chunk_id, int64_t n_tokens, cons
     return hip_fail(e, "put kernels");
   }
   Slot sl;
+  sl.version = ++s->versions;
   sl.len = n_tokens;
   for (const Run &r : runs) s->block_refs[r.page0] = 1;
   ref_pages(s, runs, 1);
@@ -1761,6 +2011,9 @@ pic_status pic_store_derive(pic_store *s, uint64_t new_id, uint64_t base_id, int
                                        (unsigned long long)base_id);
   if (s->map.count(new_id)) return fail(PIC_ERR_EXISTS, "chunk id 0x%llx already stored",
                                         (unsigned long long)new_id);
+  if (bit->second.grows)
+    return fail(PIC_ERR_INVALID, "chunk id 0x%llx grows (pic_store_open) and cannot be derived from",
+                (unsigned long long)base_id);
   const int64_t len = bit->second.len;
   if (!check_rows(rows, n_rows, len))
     return fail(PIC_ERR_INVALID, "rows must be strictly increasing and below the chunk's %lld tokens",
@@ -1843,6 +2096,7 @@ pic_status pic_store_derive(pic_store *s, uint64_t new_id, uint64_t base_id, int
   ref_pages(s, views, 1);
   s->used += n_own * kTile;
   Slot sl;
+  sl.version = ++s->versions;
   sl.len = len;
   sl.runs = std::move(views);
   sl.derived = true;
@@ -1857,7 +2111,7 @@ pic_status pic_store_write_rows(pic_store *s, uint64_t chunk_id, int32_t layer, 
   auto it = s->map.find(chunk_id);
   if (it == s->map.end()) return fail(PIC_ERR_NOT_FOUND, "chunk id 0x%llx not in the store",
                                       (unsigned long long)chunk_id);
-  const Slot &sl = it->second;
+  Slot &sl = it->second;
   if (!sl.derived)
     return fail(PIC_ERR_INVALID, "chunk id 0x%llx was not made by pic_store_derive",
                 (unsigned long long)chunk_id);
@@ -1908,7 +2162,227 @@ pic_status pic_store_write_rows(pic_store *s, uint64_t chunk_id, int32_t layer, 
     ++v0;
   }
   HIP_TRY(flush(n_rows), "write_rows_kernel");
+  sl.version = ++s->versions;
   return PIC_OK;
+}
+
+pic_status pic_store_open(pic_store *s, uint64_t chunk_id, int64_t max_tokens) {
+  if (!s) return fail(PIC_ERR_INVALID, "store is NULL");
+  if (s->imported) return fail(PIC_ERR_INVALID, "the store was imported from another process and is read-only");
+  if (is_fp4(s->desc)) return fail(PIC_ERR_UNSUPPORTED, "4-bit stores have no growing chunks");
+  if (max_tokens <= 0 || max_tokens > INT32_MAX / 4) return fail(PIC_ERR_INVALID, "max_tokens out of range");
+  if (s->map.count(chunk_id)) return fail(PIC_ERR_EXISTS, "chunk id 0x%llx already stored",
+                                          (unsigned long long)chunk_id);
+  DeviceGuard dg(s->device);
+  if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+  return guarded([&] {
+    const int64_t pages = round_up(max_tokens, kTile) / kTile;
+    Slot sl;
+    sl.version = ++s->versions;
+    sl.len = 0;
+    sl.grows = true;
+    sl.max_tokens = max_tokens;
+    sl.layer_len.assign(s->n_layers, 0);
+    std::vector<Run> runs;
+    const pic_status rc = take_pages(s, pages, runs);
+    if (rc != PIC_OK) return rc;
+    int32_t tok = 0;
+    for (Run &r : runs) {
+      r.tok0 = tok;
+      r.ntok = r.pages * kTile;
+      tok += r.ntok;
+    }
+    for (const Run &r : runs) s->block_refs[r.page0] = 1;
+    ref_pages(s, runs, 1);
+    s->used += pages * kTile;
+    sl.runs = std::move(runs);
+    s->map.emplace(chunk_id, std::move(sl));
+    return PIC_OK;
+  });
+}
+
+pic_status pic_store_append(pic_store *s, const pic_append *a, void *stream) {
+  if (!s) return fail(PIC_ERR_INVALID, "store is NULL");
+  if (!a) return fail(PIC_ERR_INVALID, "append is NULL");
+  if (s->imported) return fail(PIC_ERR_INVALID, "the store was imported from another process and is read-only");
+  const pic_store_desc &d = s->desc;
+  const bool gqa = d.kind == PIC_GQA;
+  const int32_t n = a->n_chunks;
+  if (n < 0) return fail(PIC_ERR_INVALID, "n_chunks < 0");
+  if (a->layer < 0 || a->layer >= s->n_layers)
+    return fail(PIC_ERR_INVALID, "layer %d outside the store's %d layers", a->layer, s->n_layers);
+  if (n == 0) return PIC_OK;
+  if (!a->chunk_ids) return fail(PIC_ERR_INVALID, "chunk_ids is NULL");
+  if (!check_offsets(a->offsets, n)) return fail(PIC_ERR_INVALID, "bad offsets");
+  const int64_t total = a->offsets[n];
+  const bool with_q = a->q || a->q_out;
+  AppendParams p{};
+  p.k = a->k;
+  p.v = a->v;
+  p.q = a->q;
+  p.q_out = a->q_out;
+  p.heads = d.n_kv_heads;
+  p.q_heads = with_q ? a->n_q_heads : 0;
+  p.d_k = d.d_k;
+  p.d_v = d.d_v;
+  if (with_q && (a->n_q_heads < 1 || a->n_q_heads > 1024))
+    return fail(PIC_ERR_INVALID, "n_q_heads must be 1..1024");
+  // a row's width, and a stride's default and least
+  const auto strided = [](int64_t stride, int64_t row, int64_t *out) {
+    *out = stride ? stride : row;
+    return *out >= row;
+  };
+  if (!strided(a->k_stride, s->k_tok_elems, &p.k_stride) ||
+      (gqa && !strided(a->v_stride, s->v_tok_elems, &p.v_stride)) ||
+      (with_q && (!strided(a->q_stride, (int64_t)a->n_q_heads * d.d_k, &p.q_stride) ||
+                  !strided(a->q_out_stride, (int64_t)a->n_q_heads * d.d_k, &p.q_out_stride))))
+    return fail(PIC_ERR_INVALID, "a token stride is below its row");
+  if (a->rope) {
+    const pic_rope_desc &rd = a->rope->desc;
+    if (rd.dtype != d.dtype || rd.head_dim != d.d_k)
+      return fail(PIC_ERR_INVALID, "the rotary handle's dtype and head_dim must be the store's (d_k %d)", d.d_k);
+    p.rot_at = rd.rot_at;
+    p.rot = rd.rot_dim;
+    p.magnitude = (float)rd.magnitude;
+    std::copy(a->rope->rev, a->rope->rev + rd.rot_dim / 2, p.rev);
+  }
+  if (total > 0) {
+    if (!a->k || (gqa && !a->v)) return fail(PIC_ERR_INVALID, "k/v is NULL");
+    if (with_q && (!a->q || !a->q_out)) return fail(PIC_ERR_INVALID, "q and q_out come together");
+    if (a->rope && !a->positions) return fail(PIC_ERR_INVALID, "positions is NULL");
+    for (const void *ptr : {a->k, a->v, a->q, (const void *)a->q_out})
+      if ((uintptr_t)ptr % s->esz) return fail(PIC_ERR_INVALID, "a tensor is not aligned to its elements");
+    if (with_q && a->q == a->q_out && p.q_stride != p.q_out_stride)
+      return fail(PIC_ERR_INVALID, "q in place with two strides");
+  }
+  if (!gqa && a->v) return fail(PIC_ERR_INVALID, "v must be NULL for MLA");
+  p.positions = a->positions;
+  return guarded([&] {
+    std::vector<Slot *> slots(n);
+    std::vector<uint64_t> seen(a->chunk_ids, a->chunk_ids + n);
+    std::sort(seen.begin(), seen.end());
+    if (std::adjacent_find(seen.begin(), seen.end()) != seen.end())
+      return fail(PIC_ERR_INVALID, "a chunk is named twice");
+    for (int32_t i = 0; i < n; ++i) {
+      const uint64_t id = a->chunk_ids[i];
+      auto it = s->map.find(id);
+      if (it == s->map.end())
+        return fail(PIC_ERR_NOT_FOUND, "chunk id 0x%llx not in the store", (unsigned long long)id);
+      Slot &sl = it->second;
+      if (!sl.grows)
+        return fail(PIC_ERR_INVALID, "chunk id 0x%llx was not made by pic_store_open", (unsigned long long)id);
+      if (sl.plan_refs > 0)
+        return fail(PIC_ERR_INVALID, "chunk id 0x%llx is linked by %lld live link plans",
+                    (unsigned long long)id, (long long)sl.plan_refs);
+      if (sl.layer_len[a->layer] + (int64_t)(a->offsets[i + 1] - a->offsets[i]) > sl.max_tokens)
+        return fail(PIC_ERR_OOM, "chunk id 0x%llx: %d tokens more than the %lld it was opened with",
+                    (unsigned long long)id, a->offsets[i + 1] - a->offsets[i], (long long)sl.max_tokens);
+      slots[i] = &sl;
+    }
+    if (total == 0) return PIC_OK;
+    DeviceGuard dg(s->device);
+    if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+    const bool half = !a->rope || a->rope->desc.layout == PIC_ROPE_HALF;
+    int64_t tokens = 0;
+    // a launch's workgroups stay far below what it holds (pages x heads x value parts)
+    const int64_t most = std::max<int64_t>(
+        kTile, ((int64_t)1 << 22) / (p.heads * ((p.d_v + 63) / 64 + p.q_heads)) * (kTile / 2));
+    auto flush = [&]() {
+      const hipError_t e = p.n_pieces ? launch_append(p, s->esz, half, s->shape, (hipStream_t)stream) : hipSuccess;
+      p.n_pieces = 0;
+      tokens = 0;
+      return e;
+    };
+    for (int32_t i = 0; i < n; ++i) {
+      int32_t src = a->offsets[i], left = a->offsets[i + 1] - src;
+      int64_t at = slots[i]->layer_len[a->layer];
+      for (const Run &r : slots[i]->runs) {
+        while (left > 0 && at < r.tok0 + r.ntok) {
+          // (a piece ends with a page or with the tokens: a page begun is one launch's)
+          const int64_t room = std::min<int64_t>(kAppendPieceTokens, most) / kTile * kTile - at % kTile;
+          const int32_t m = (int32_t)std::min<int64_t>({left, r.tok0 + r.ntok - at, room});
+          if (p.n_pieces == kAppendPieces || tokens + m > most) HIP_TRY(flush(), "append_kernel");
+          const LinkEntry E = run_entry(s, r, a->layer);
+          p.piece[p.n_pieces++] = AppendPiece{(char *)E.k, gqa ? (char *)E.v : nullptr, E.lp,
+                                              (int32_t)(at - r.tok0), m, src, 0, 0};
+          tokens += m;
+          src += m;
+          left -= m;
+          at += m;
+        }
+      }
+    }
+    HIP_TRY(flush(), "append_kernel");
+    for (int32_t i = 0; i < n; ++i) {
+      Slot &sl = *slots[i];
+      sl.layer_len[a->layer] += a->offsets[i + 1] - a->offsets[i];
+      sl.len = *std::min_element(sl.layer_len.begin(), sl.layer_len.end());
+    }
+    return PIC_OK;
+  });
+}
+
+pic_status pic_store_truncate(pic_store *s, int32_t n, const uint64_t *chunk_ids, const int64_t *n_tokens,
+                              void *stream) {
+  if (!s) return fail(PIC_ERR_INVALID, "store is NULL");
+  if (s->imported) return fail(PIC_ERR_INVALID, "the store was imported from another process and is read-only");
+  if (n < 0 || (n > 0 && (!chunk_ids || !n_tokens))) return fail(PIC_ERR_INVALID, "bad chunk list");
+  return guarded([&] {
+    std::vector<Slot *> slots(n);
+    for (int32_t i = 0; i < n; ++i) {
+      const uint64_t id = chunk_ids[i];
+      auto it = s->map.find(id);
+      if (it == s->map.end())
+        return fail(PIC_ERR_NOT_FOUND, "chunk id 0x%llx not in the store", (unsigned long long)id);
+      Slot &sl = it->second;
+      if (!sl.grows)
+        return fail(PIC_ERR_INVALID, "chunk id 0x%llx was not made by pic_store_open", (unsigned long long)id);
+      if (sl.plan_refs > 0)
+        return fail(PIC_ERR_INVALID, "chunk id 0x%llx is linked by %lld live link plans",
+                    (unsigned long long)id, (long long)sl.plan_refs);
+      if (n_tokens[i] < 0 || n_tokens[i] > *std::max_element(sl.layer_len.begin(), sl.layer_len.end()))
+        return fail(PIC_ERR_INVALID, "chunk id 0x%llx: %lld tokens to keep of fewer", (unsigned long long)id,
+                    (long long)n_tokens[i]);
+      slots[i] = &sl;
+    }
+    DeviceGuard dg(s->device);
+    if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+    ClearParams p{};
+    p.layer_bytes = s->layer_bytes;
+    p.heads = s->desc.n_kv_heads;
+    p.d_k = s->desc.d_k;
+    p.d_v = s->desc.d_v;
+    int32_t pieces = 0;
+    auto flush = [&]() {
+      const hipError_t e = launch_clear_rows(p, pieces, s->n_layers, s->esz, (hipStream_t)stream);
+      pieces = 0;
+      return e;
+    };
+    // the rows taken back on the last page that keeps some: what follows within a page is
+    // zeros (a later page is written to its end when an append begins it)
+    for (int32_t i = 0; i < n; ++i) {
+      const Slot &sl = *slots[i];
+      const int64_t keep = n_tokens[i];
+      const int64_t had = *std::max_element(sl.layer_len.begin(), sl.layer_len.end());
+      const int64_t end = std::min<int64_t>(had, round_up(keep, kTile));
+      if (end <= keep) continue;
+      if (pieces == kClearPieces) HIP_TRY(flush(), "clear_rows_kernel");
+      const Run &r = view_of(sl, keep);
+      const LinkEntry E = run_entry(s, r, 0);
+      p.piece[pieces++] = ClearPiece{(char *)E.k, s->desc.kind == PIC_GQA ? (char *)E.v : nullptr, E.lp,
+                                     (int32_t)(keep - r.tok0), (int32_t)(end - keep)};
+    }
+    HIP_TRY(flush(), "clear_rows_kernel");
+    for (int32_t i = 0; i < n; ++i) {
+      Slot &sl = *slots[i];
+      for (int32_t &l : sl.layer_len) {
+        if (l > n_tokens[i]) sl.version = ++s->versions;
+        l = (int32_t)std::min<int64_t>(l, n_tokens[i]);
+      }
+      sl.len = *std::min_element(sl.layer_len.begin(), sl.layer_len.end());
+    }
+    return PIC_OK;
+  });
 }
 
 pic_status pic_store_remove(pic_store *s, uint64_t chunk_id, void *stream) {
@@ -1980,9 +2454,23 @@ struct ExportRun {
 // process has not returned on the target machines.
 constexpr int64_t kMaxExportBytes = (int64_t(1) << 31) - 1;
 
+// A chunk's runs as they are exported: a growing one's as far as every layer holds tokens
+// (none: the chunk is left out).
+void export_runs(const Slot &sl, std::vector<Run> &runs) {
+  runs.clear();
+  for (Run r : sl.runs) {
+    r.ntok = Slot::filled(r, sl.len);
+    if (r.ntok > 0) runs.push_back(r);
+  }
+}
+
 size_t export_size(const pic_store *s) {
   size_t n = sizeof(ExportHeader);
-  for (const auto &kv : s->map) n += sizeof(ExportChunk) + kv.second.runs.size() * sizeof(ExportRun);
+  std::vector<Run> runs;
+  for (const auto &kv : s->map) {
+    export_runs(kv.second, runs);
+    if (!runs.empty()) n += sizeof(ExportChunk) + runs.size() * sizeof(ExportRun);
+  }
   return n;
 }
 
@@ -2012,19 +2500,21 @@ pic_status pic_store_export(pic_store *s, void *buf, size_t buf_bytes, size_t *b
   h.k_tok_elems = s->k_tok_elems;
   h.v_tok_elems = s->v_tok_elems;
   h.used = s->used;
-  h.n_chunks = (int64_t)s->map.size();
+  for (const auto &kv : s->map) h.n_chunks += kv.second.len > 0;
   h.n_layers = s->n_layers;
   h.esz = s->esz;
   HIP_TRY(hipIpcGetMemHandle(&h.handle, s->pool), "hipIpcGetMemHandle(pool)");
   char *o = (char *)buf;
   memcpy(o, &h, sizeof h);
   o += sizeof h;
+  std::vector<Run> runs;
   for (const auto &kv : s->map) {
-    const ExportChunk ch{kv.first, kv.second.len, (int32_t)kv.second.runs.size(),
-                         kv.second.derived ? 1 : 0};
+    export_runs(kv.second, runs);
+    if (runs.empty()) continue;
+    const ExportChunk ch{kv.first, kv.second.len, (int32_t)runs.size(), kv.second.derived ? 1 : 0};
     memcpy(o, &ch, sizeof ch);
     o += sizeof ch;
-    for (const Run &r : kv.second.runs) {
+    for (const Run &r : runs) {
       const ExportRun er{r.page0, r.pages, r.tok0, r.ntok, r.skip};
       memcpy(o, &er, sizeof er);
       o += sizeof er;
@@ -2069,6 +2559,7 @@ pic_status pic_store_import(const void *buf, size_t buf_bytes, pic_store **out) 
       return fail(PIC_ERR_INVALID, "corrupt chunk record in the exported store");
     }
     Slot sl;
+    sl.version = ++s->versions;
     sl.len = ch.len;
     sl.derived = ch.derived != 0;
     int64_t covered = 0;
@@ -2220,6 +2711,11 @@ pic_status pic_link_plan_create(pic_store *s, const pic_link_req *req, int32_t n
     delete pl;
     return rc;
   }
+  rc = check_even(s, pl->C.P.ids);
+  if (rc != PIC_OK) {
+    delete pl;
+    return rc;
+  }
   pl->store = s;
   pl->batch = req->batch;
   const Plan &P = pl->C.P;
@@ -2231,17 +2727,10 @@ pic_status pic_link_plan_create(pic_store *s, const pic_link_req *req, int32_t n
   pl->small = pl->C.small;
   if (pl->small) {
     pl->small_links.resize((size_t)s->n_layers * nl);
-    std::vector<bool> own_link(nl, false);
-    for (auto &o : P.own) own_link[o.first] = true;
-    for (int32_t l = 0; l < s->n_layers; ++l)
-      for (size_t i = 0; i < nl; ++i) {
-        LinkEntry E = P.links[i];
-        if (!own_link[i] && E.k) {
-          E.k = (const char *)E.k + (int64_t)l * s->layer_bytes;
-          E.v = (const char *)E.v + (int64_t)l * s->layer_bytes;
-        }
-        pl->small_links[(size_t)l * nl + i] = E;
-      }
+    for (int32_t l = 0; l < s->n_layers; ++l) {
+      const std::vector<LinkEntry> at = layer_links(s, P, P.links, l);
+      std::copy(at.begin(), at.end(), pl->small_links.begin() + (size_t)l * nl);
+    }
   }
   const size_t tables = pl->small ? 0 : pl->table_bytes * s->n_layers;
   const size_t bytes = pl->small ? pl->C.part_bytes : tables + pl->C.work_bytes();
@@ -2265,23 +2754,13 @@ pic_status pic_link_plan_create(pic_store *s, const pic_link_req *req, int32_t n
       delete pl;
       return fail(PIC_ERR_HIP, "cannot select the store's device");
     }
-    // Every layer's tables differ only in the chunk links' addresses: layer
-    // l of a slot sits l pool layers further on; own-KV links point at the
-    // plan's workspace in every layer.
+    // Every layer's tables differ only in the chunk links' addresses.
     std::vector<char> host(tables, 0);
     std::vector<LinkEntry> links(P.links);
     place_own(s, P, pl->work, links.data());
-    std::vector<bool> own(nl, false);
-    for (auto &o : P.own) own[o.first] = true;
-    for (int32_t l = 0; l < s->n_layers; ++l) {
-      std::vector<LinkEntry> at(links);
-      for (size_t i = 0; i < nl; ++i)
-        if (!own[i] && at[i].k) {   // (own KV read in place has no address here)
-          at[i].k = (const char *)at[i].k + (int64_t)l * s->layer_bytes;
-          at[i].v = (const char *)at[i].v + (int64_t)l * s->layer_bytes;
-        }
-      write_tables(pl->C, pl->layout, at.data(), host.data() + (size_t)l * pl->table_bytes);
-    }
+    for (int32_t l = 0; l < s->n_layers; ++l)
+      write_tables(pl->C, pl->layout, layer_links(s, P, links, l).data(),
+                   host.data() + (size_t)l * pl->table_bytes);
     hipError_t e = hipMemcpy(pl->dev, host.data(), tables, hipMemcpyHostToDevice);
     if (e != hipSuccess) {
       (void)hipFree(pl->dev);
@@ -2295,6 +2774,58 @@ pic_status pic_link_plan_create(pic_store *s, const pic_link_req *req, int32_t n
   return PIC_OK;
 }
 
+pic_status pic_link_shared(pic_store *s, const pic_link_req *req, const pic_link_groups *groups,
+                           int32_t n_q_heads, const void *q, const void *k_self, const void *v_self,
+                           float softmax_scale, void *out, float *lse, void *stream) {
+  return guarded([&] {
+    return shared_link_call(s, req, groups, n_q_heads, q, k_self, v_self, softmax_scale, out, lse,
+                            (hipStream_t)stream);
+  });
+}
+
+pic_status pic_link_shared_plan_create(pic_store *s, const pic_link_req *req, const pic_link_groups *groups,
+                                       int32_t n_q_heads, pic_link_plan **out) {
+  if (!out) return fail(PIC_ERR_INVALID, "out is NULL");
+  *out = nullptr;
+  if (req && req->layer != 0) return fail(PIC_ERR_INVALID, "req->layer must be 0 (each run names its layer)");
+  return guarded([&] {
+    auto pl = std::make_unique<pic_link_plan>();
+    pl->shared = std::make_unique<SharedCall>();
+    SharedCall &S = *pl->shared;
+    // the scale only has to pass validation here; each run passes its own
+    pic_status rc = setup_shared(s, req, groups, n_q_heads, 1.0f, 0, S);
+    if (rc == PIC_OK) rc = check_even(s, S.own.P.ids);
+    if (rc == PIC_OK) rc = check_even(s, S.pre.P.ids);
+    if (rc != PIC_OK) return rc;
+    pl->store = s;
+    pl->batch = req->batch;
+    pl->table_bytes = S.table_bytes;
+    const size_t tables = S.table_bytes * s->n_layers, bytes = tables + S.work_bytes;
+    if (S.own.P.total_q > 0) {
+      DeviceGuard dg(s->device);
+      if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+      std::vector<char> host(tables, 0);
+      HIP_TRY(hipMalloc(&pl->dev, bytes), "hipMalloc(plan)");
+      pl->work = (char *)pl->dev + tables;
+      std::vector<LinkEntry> links(S.own.P.links);
+      place_own(s, S.own.P, pl->work, links.data());
+      for (int32_t l = 0; l < s->n_layers; ++l)
+        write_shared_tables(S, layer_links(s, S.pre.P, S.pre.P.links, l).data(),
+                            layer_links(s, S.own.P, links, l).data(), host.data() + (size_t)l * S.table_bytes);
+      const hipError_t e = hipMemcpy(pl->dev, host.data(), tables, hipMemcpyHostToDevice);
+      if (e != hipSuccess) {
+        (void)hipFree(pl->dev);
+        return hip_fail(e, "hipMemcpy(plan tables)");
+      }
+    }
+    for (const Plan *P : {&S.own.P, &S.pre.P})
+      for (uint64_t id : P->ids) ++s->map.at(id).plan_refs;
+    ++s->live_plans;
+    *out = pl.release();
+    return PIC_OK;
+  });
+}
+
 pic_status pic_link_plan_run(pic_link_plan *pl, int32_t layer, const void *q, const void *k_self,
                              const void *v_self, float softmax_scale, void *out, float *lse,
                              void *stream) {
@@ -2305,11 +2836,15 @@ pic_status pic_link_plan_run(pic_link_plan *pl, int32_t layer, const void *q, co
   if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.f))
     return fail(PIC_ERR_INVALID, "softmax_scale must be positive and finite");
   if (pl->batch == 0) return PIC_OK;
-  pic_status rc = check_tensors(s, pl->C.P, q, k_self, v_self, out);
+  const Plan &P = pl->requests();
+  pic_status rc = check_tensors(s, P, q, k_self, v_self, out);
   if (rc != PIC_OK) return rc;
-  if (pl->C.P.total_q == 0) return PIC_OK;
+  if (P.total_q == 0) return PIC_OK;
   DeviceGuard dg(s->device);
   if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+  if (pl->shared)
+    return launch_shared(s, *pl->shared, (char *)pl->dev + (size_t)layer * pl->table_bytes, nullptr,
+                         (char *)pl->work, q, k_self, v_self, softmax_scale, out, lse, (hipStream_t)stream);
   if (pl->small)
     return launch_small(s->desc, pl->C,
                         pl->small_links.data() + (size_t)layer * pl->C.P.links.size(),
@@ -2332,13 +2867,260 @@ pic_status pic_link_plan_destroy(pic_link_plan *pl) {
     (void)hipDeviceSynchronize();
     (void)hipFree(pl->dev);
   }
-  for (uint64_t id : pl->C.P.ids) {
-    auto it = pl->store->map.find(id);
-    if (it != pl->store->map.end()) --it->second.plan_refs;
+  for (const Plan *P : {&pl->requests(), pl->shared ? (const Plan *)&pl->shared->pre.P : nullptr}) {
+    if (!P) continue;
+    for (uint64_t id : P->ids) {
+      auto it = pl->store->map.find(id);
+      if (it != pl->store->map.end()) --it->second.plan_refs;
+    }
   }
   --pl->store->live_plans;
   delete pl;
   return PIC_OK;
+}
+
+// Summaries of a store's blocks: which content of each chunk they were formed from (its version,
+// and by layer its tokens then; 0: none).
+struct pic_index {
+  struct Entry {
+    uint64_t version = 0;
+    std::vector<int32_t> tokens;
+  };
+  pic_store *store = nullptr;
+  void *means = nullptr;         // bf16 [layer][page][kv head][d_k]
+  int64_t layer_elems = 0;
+  std::unordered_map<uint64_t, Entry> entries;
+};
+
+pic_status pic_index_create(pic_store *s, pic_index **out) {
+  if (!out) return fail(PIC_ERR_INVALID, "out is NULL");
+  *out = nullptr;
+  if (!s) return fail(PIC_ERR_INVALID, "store is NULL");
+  const pic_store_desc &d = s->desc;
+  if (!sparse_supported(d.dtype, d.kind == PIC_MLA, d.d_k, d.d_v))
+    return fail(PIC_ERR_UNSUPPORTED, "block indexes are for fp32 and bf16 GQA stores with d_k = d_v of 64 or 128");
+  return guarded([&] {
+    auto x = std::make_unique<pic_index>();
+    x->store = s;
+    x->layer_elems = s->capacity / kTile * s->k_tok_elems;
+    DeviceGuard dg(s->device);
+    if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+    HIP_TRY(hipMalloc(&x->means, (size_t)x->layer_elems * 2 * s->n_layers), "hipMalloc(index)");
+    ++s->live_indexes;
+    *out = x.release();
+    return PIC_OK;
+  });
+}
+
+pic_status pic_index_destroy(pic_index *x) {
+  if (!x) return PIC_OK;
+  DeviceGuard dg(x->store->device);
+  (void)hipDeviceSynchronize();
+  (void)hipFree(x->means);
+  --x->store->live_indexes;
+  delete x;
+  return PIC_OK;
+}
+
+pic_status pic_index_update(pic_index *x, int32_t layer, int32_t n, const uint64_t *chunk_ids, void *stream) {
+  if (!x) return fail(PIC_ERR_INVALID, "index is NULL");
+  pic_store *s = x->store;
+  if (layer < -1 || layer >= s->n_layers)
+    return fail(PIC_ERR_INVALID, "layer %d outside the store's %d layers", layer, s->n_layers);
+  if (n < 0 || (n > 0 && !chunk_ids)) return fail(PIC_ERR_INVALID, "bad chunk list");
+  return guarded([&] {
+    for (int32_t i = 0; i < n; ++i)
+      if (!s->map.count(chunk_ids[i]))
+        return fail(PIC_ERR_NOT_FOUND, "chunk id 0x%llx not in the store", (unsigned long long)chunk_ids[i]);
+    DeviceGuard dg(s->device);
+    if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+    MeansParams p{};
+    p.layer_bytes = s->layer_bytes;
+    p.layer_elems = x->layer_elems;
+    p.heads = s->desc.n_kv_heads;
+    // The layers of a call are one launch where they hold alike, else a launch each.
+    std::vector<std::pair<int32_t, int32_t>> layers;      // first, count
+    bool alike = true;
+    for (int32_t i = 0; i < n; ++i) alike &= s->map.at(chunk_ids[i]).even();
+    if (layer >= 0)
+      layers.emplace_back(layer, 1);
+    else if (alike)
+      layers.emplace_back(0, s->n_layers);
+    else
+      for (int32_t l = 0; l < s->n_layers; ++l) layers.emplace_back(l, 1);
+    for (const auto &ls : layers) {
+      p.means = (char *)x->means + (int64_t)ls.first * x->layer_elems * 2;
+      int32_t pieces = 0;
+      auto flush = [&]() {
+        const hipError_t e = launch_block_means(p, pieces, ls.second, s->desc.dtype, s->desc.d_k, (hipStream_t)stream);
+        pieces = 0;
+        return e;
+      };
+      for (int32_t i = 0; i < n; ++i) {
+        const Slot &sl = s->map.at(chunk_ids[i]);
+        pic_index::Entry &e = x->entries[chunk_ids[i]];
+        const int64_t len = sl.tokens(ls.first);
+        // blocks that were complete are as they were
+        int64_t from = 0;
+        if (e.version == sl.version && !e.tokens.empty()) {
+          from = INT64_MAX;
+          for (int32_t l = ls.first; l < ls.first + ls.second; ++l)
+            from = std::min<int64_t>(from, e.tokens[l] >= len ? len : e.tokens[l] / kTile * kTile);
+        }
+        for (const Run &r : sl.runs) {
+          const int64_t n0 = std::max<int64_t>(0, from - r.tok0), n1 = Slot::filled(r, len);
+          if (n0 >= n1) continue;
+          if (pieces == kMeansPieces) HIP_TRY(flush(), "block_means_kernel");
+          const LinkEntry E = run_entry(s, r, ls.first);
+          p.piece[pieces++] = MeansPiece{(const char *)E.k + n0 * s->desc.d_k * s->esz, E.lp,
+                                         (int32_t)(r.page0 + r.skip + n0 / kTile), (int32_t)(n1 - n0)};
+        }
+      }
+      HIP_TRY(flush(), "block_means_kernel");
+      for (int32_t i = 0; i < n; ++i) {
+        const Slot &sl = s->map.at(chunk_ids[i]);
+        pic_index::Entry &e = x->entries[chunk_ids[i]];
+        if (e.version != sl.version || e.tokens.empty()) {
+          e.version = sl.version;
+          e.tokens.assign(s->n_layers, 0);
+        }
+        for (int32_t l = ls.first; l < ls.first + ls.second; ++l) e.tokens[l] = (int32_t)sl.tokens(l);
+      }
+    }
+    // (entries of chunks that are gone are dropped once they outnumber the others)
+    if (x->entries.size() > 2 * s->map.size() + 64)
+      for (auto it = x->entries.begin(); it != x->entries.end();) {
+        auto at = s->map.find(it->first);
+        it = at == s->map.end() || at->second.version != it->second.version ? x->entries.erase(it) : std::next(it);
+      }
+    return PIC_OK;
+  });
+}
+
+pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_heads, int32_t n_blocks,
+                           int32_t keep_first, int32_t keep_last, const void *q, const void *k_self,
+                           const void *v_self, float softmax_scale, void *out, float *lse, int32_t *blocks,
+                           void *stream) {
+  if (!x) return fail(PIC_ERR_INVALID, "index is NULL");
+  if (!req) return fail(PIC_ERR_INVALID, "req is NULL");
+  pic_store *s = x->store;
+  const pic_store_desc &d = s->desc;
+  if (keep_first < 0 || keep_last < 0 || n_blocks < 1 || (int64_t)keep_first + keep_last > n_blocks)
+    return fail(PIC_ERR_INVALID, "n_blocks must be at least 1 and hold keep_first and keep_last");
+  if (n_blocks > kSparseMostTaken)
+    return fail(PIC_ERR_UNSUPPORTED, "n_blocks is at most %d", kSparseMostTaken);
+  if (req->q_doc_limits) return fail(PIC_ERR_INVALID, "q_doc_limits must be NULL");
+  return guarded([&] {
+    Plan P;
+    pic_status rc = plan_call(s, req, n_q_heads, softmax_scale, req->layer, INT32_MAX, P);
+    if (rc != PIC_OK) return rc;
+    const int32_t B = req->batch, tq = P.total_q;
+    if (B == 0) return PIC_OK;
+    rc = check_tensors(s, P, q, k_self, v_self, out);
+    if (rc != PIC_OK) return rc;
+    for (uint64_t id : P.ids) {
+      const Slot &sl = s->map.at(id);
+      const auto e = x->entries.find(id);
+      if (e == x->entries.end() || e->second.version != sl.version ||
+          e->second.tokens[req->layer] != sl.tokens(req->layer))
+        return fail(PIC_ERR_INVALID, "chunk id 0x%llx is not in the index as it stands (pic_index_update)",
+                    (unsigned long long)id);
+    }
+    if (tq == 0) return PIC_OK;
+    SparseParams p{};
+    std::vector<SparseLink> links;
+    std::vector<SparseReq> reqs(B);
+    links.reserve(P.pages.size());
+    for (int32_t r = 0; r < B; ++r) {
+      const ReqEntry &R = P.reqs[r];
+      const int32_t n = R.nlinks - (R.ls > 0);            // (the own KV is the last)
+      reqs[r] = SparseReq{(int32_t)links.size(), n, R.doc_tiles, R.q0, R.lq, R.s0, R.ls, 0};
+      if (R.doc_tiles > kSparseMostBlocks)
+        return fail(PIC_ERR_UNSUPPORTED, "request %d links %d blocks, at most %d", r, R.doc_tiles, kSparseMostBlocks);
+      p.most_blocks = std::max(p.most_blocks, R.doc_tiles);
+      for (int32_t i = 0; i < n; ++i) {
+        const LinkEntry &L = P.links[R.link0 + i];
+        links.push_back(SparseLink{(const char *)L.k, (const char *)L.v, L.len, L.lp, L.tile0,
+                                   P.pages[links.size()]});
+      }
+    }
+    p.q = q;
+    p.k_self = k_self;
+    p.v_self = v_self;
+    p.out = out;
+    p.lse = lse;
+    p.taken = blocks;
+    p.means = (const char *)x->means + (int64_t)req->layer * x->layer_elems * 2;
+    p.total_q = tq;
+    p.n_q_heads = n_q_heads;
+    p.n_kv_heads = d.n_kv_heads;
+    p.group = n_q_heads / d.n_kv_heads;
+    p.n_blocks = n_blocks;
+    p.first = keep_first;
+    p.last = keep_last;
+    p.scale_log2 = softmax_scale * 1.4426950408889634f;
+    p.splits = sparse_splits(s->shape.cus, (int64_t)tq * d.n_kv_heads, std::min(n_blocks, p.most_blocks));
+    DeviceGuard dg(s->device);
+    if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+    const hipStream_t st = (hipStream_t)stream;
+    const size_t off_r = round_up(sizeof(SparseLink) * links.size(), 256);
+    const size_t off_t = off_r + round_up(sizeof(SparseReq) * B, 256);
+    const size_t off_m = off_t + round_up(sizeof(int32_t) * tq, 256);
+    const size_t bytes = off_m + (p.splits > 1 ? round_up(sizeof(MergeEntry) * B, 256) : 0);
+    const bool by_arg = p.splits == 1 && links.size() <= (size_t)kSparseTabLinks && B <= kSparseTabReqs &&
+                        tq <= kSparseTabTokens;
+    std::pair<hipEvent_t, hipEvent_t> ev{nullptr, nullptr};
+    if (by_arg) {
+      SparseTabs t{};
+      std::copy(links.begin(), links.end(), t.links);
+      std::copy(reqs.begin(), reqs.end(), t.reqs);
+      for (int32_t r = 0; r < B; ++r) std::fill(t.token_req + reqs[r].q0, t.token_req + reqs[r].q0 + reqs[r].lq, r);
+      prof_start(st, &ev);
+      const hipError_t e = launch_link_sparse(p, &t, d.dtype, d.d_k, st);
+      prof_stop(st, &ev, "link_sparse_tabs_kernel");
+      HIP_TRY(e, "link_sparse_tabs_kernel");
+      return PIC_OK;
+    }
+    Stage *stage = nullptr;
+    const int64_t rows = (int64_t)tq * n_q_heads;
+    rc = stage_acquire(s, bytes, &stage);
+    if (rc == PIC_OK && p.splits > 1) rc = ensure_work(stage, (size_t)rows * p.splits * (d.d_v + 2) * sizeof(float));
+    if (rc != PIC_OK) return rc;
+    char *h = (char *)stage->host, *dev = (char *)stage->dev;
+    if (!links.empty()) memcpy(h, links.data(), sizeof(SparseLink) * links.size());
+    memcpy(h + off_r, reqs.data(), sizeof(SparseReq) * B);
+    int32_t *token_req = (int32_t *)(h + off_t), most_rows = 0;
+    for (int32_t r = 0; r < B; ++r) {
+      const SparseReq &R = reqs[r];
+      std::fill(token_req + R.q0, token_req + R.q0 + R.lq, r);
+      if (p.splits > 1) {
+        const int32_t row0 = R.q0 * n_q_heads;
+        ((MergeEntry *)(h + off_m))[r] = MergeEntry{row0, R.lq * n_q_heads, {row0, 0}, {(int32_t)rows, 0}, {p.splits, 0}};
+        most_rows = std::max(most_rows, R.lq * n_q_heads);
+      }
+    }
+    HIP_TRY(launch_table_copy(stage->host_dev, dev, (int64_t)bytes, st), "table_copy_kernel");
+    p.links = (const SparseLink *)dev;
+    p.reqs = (const SparseReq *)(dev + off_r);
+    p.token_req = (const int32_t *)(dev + off_t);
+    if (p.splits > 1) p.part = place_partials((char *)stage->work, rows * p.splits, d.d_v);
+    prof_start(st, &ev);
+    const hipError_t e = launch_link_sparse(p, nullptr, d.dtype, d.d_k, st);
+    prof_stop(st, &ev, "link_sparse_kernel");
+    HIP_TRY(e, "link_sparse_kernel");
+    if (p.splits > 1) {
+      MergeParams m{};
+      m.entries = (const MergeEntry *)(dev + off_m);
+      m.src[0] = m.src[1] = p.part;
+      m.out = out;
+      m.lse = lse;
+      m.d_v = d.d_v;
+      HIP_TRY(launch_merge(m, d.dtype, B, most_rows, p.splits, st), "merge_kernel");
+    }
+    HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");
+    stage->pending = true;
+    return PIC_OK;
+  });
 }
 
 pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_t layer,
@@ -2350,18 +3132,23 @@ pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_
   const bool gqa = s->desc.kind == PIC_GQA;
   std::vector<LinkEntry> links;
   links.reserve(n);
-  int64_t toks = 0;
+  int64_t toks = 0, pages = 0;
   for (int32_t i = 0; i < n; ++i) {
     auto it = s->map.find(ids[i]);
     if (it == s->map.end()) return fail(PIC_ERR_NOT_FOUND, "chunk id 0x%llx not in the store",
                                         (unsigned long long)ids[i]);
-    for (const Run &r : it->second.runs) {
+    const int64_t len = it->second.tokens(layer);
+    for (Run r : it->second.runs) {
+      r.ntok = Slot::filled(r, len);
+      if (r.ntok == 0) break;
       LinkEntry E = run_entry(s, r, layer);
-      E.tile0 = 0;
+      E.tile0 = (int32_t)pages;
       E.tok0 = (int32_t)toks;
       links.push_back(E);
       toks += r.ntok;
+      pages += (r.ntok + kTile - 1) / kTile;
     }
+    if (toks > INT32_MAX / 2) return fail(PIC_ERR_INVALID, "too many tokens");
   }
   n = (int32_t)links.size();
   if (toks == 0) return PIC_OK;
@@ -2385,7 +3172,7 @@ pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_
   HIP_TRY(launch_table_copy(stage->host_dev, stage->dev, (int64_t)(sizeof(LinkEntry) * n), st),
           "table_copy_kernel");
   const pic_store_desc &d = s->desc;
-  hipError_t e = launch_gather((const LinkEntry *)stage->dev, n, toks, d.n_kv_heads,
+  hipError_t e = launch_gather((const LinkEntry *)stage->dev, n, pages, d.n_kv_heads,
                                d.d_k, d.d_v, !gqa, s->esz, k_out, v_out, st);
   if (e != hipSuccess) return hip_fail(e, "gather_kernel");
   HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");
@@ -2481,12 +3268,6 @@ pic_status pic_mla_up_v(int32_t n_tokens, int32_t n_heads, const void *o_lat, co
   if (e != hipSuccess) return hip_fail(e, "proj_kernel (up)");
   return PIC_OK;
 }
-
-// Rotary positions: the description and the angle per position of each pair.
-struct pic_rope {
-  pic_rope_desc desc{};
-  double rev[kRopeMost / 2] = {};   // revolutions per position
-};
 
 pic_status pic_rope_create(const pic_rope_desc *desc, pic_rope **out) {
   if (!desc || !out) return fail(PIC_ERR_INVALID, "desc/out is NULL");

@@ -340,7 +340,8 @@ struct PutParams {
   int32_t rows_blocks;            // set by launch_put
 };
 hipError_t launch_put(PutParams pp, int32_t n_layers, hipStream_t st);
-hipError_t launch_gather(const LinkEntry *links, int32_t n_links, int64_t total_tokens,
+// links' tile0: their first page in the list, of `pages` in all.
+hipError_t launch_gather(const LinkEntry *links, int32_t n_links, int64_t pages,
                          int32_t heads, int32_t d_k, int32_t d_v, int32_t mla, int32_t esz,
                          void *k_out, void *v_out, hipStream_t st);
 
@@ -433,6 +434,47 @@ struct RopeParams {
 };
 hipError_t launch_rope(RopeParams p, int dtype, bool half, const DevShape &ds, hipStream_t st);
 
+// New rows of growing chunks (kernel argument): a piece is a chunk's new tokens within one run
+// of pages. group0, page0: its first group of tokens and page among the launch's (set by
+// launch_append with the fields after magnitude).
+constexpr int kAppendPieces = 60, kAppendPieceTokens = 16384;
+struct AppendPiece {
+  char *k, *v;                // the run's K and V blocks, head 0 (v NULL for MLA)
+  int32_t lp;                 // its row stride
+  int32_t row0, n;            // first new row, rows
+  int32_t src0;               // source token of the first
+  int32_t group0, page0;
+};
+struct AppendParams {
+  double rev[kRopeMost / 2];  // revolutions per position of each pair
+  AppendPiece piece[kAppendPieces];
+  const void *k, *v, *q;      // token-major sources (v NULL for MLA; q NULL: none)
+  void *q_out;
+  int64_t k_stride, v_stride, q_stride, q_out_stride;   // elements from token to token
+  const int32_t *positions;   // by source token (rot 0: unused)
+  int32_t n_pieces, heads, q_heads, d_k, d_v, rot_at, rot;
+  float magnitude;
+  int32_t groups, groups_each, pages_each, parts, heads_per_block, tokens;
+  int32_t rot_chunks, lanes, slots, v_heads, v_parts;
+  float inv_lanes, inv_half;
+};
+static_assert(sizeof(AppendParams) <= 4064, "kernel arguments");
+hipError_t launch_append(AppendParams p, int esz, bool half, const DevShape &ds, hipStream_t st);
+
+// Rows of growing chunks that were taken back, to zeros in every layer.
+constexpr int kClearPieces = 96;
+struct ClearPiece {
+  char *k, *v;                // as AppendPiece, layer 0
+  int32_t lp, row0, n;
+};
+struct ClearParams {
+  ClearPiece piece[kClearPieces];
+  int64_t layer_bytes;
+  int32_t heads, d_k, d_v;
+};
+static_assert(sizeof(ClearParams) <= 4064, "kernel arguments");
+hipError_t launch_clear_rows(const ClearParams &p, int32_t n, int32_t n_layers, int esz, hipStream_t st);
+
 // The call's prologue: lays out the own KV of every request (token-major
 // k_self / v_self) like a chunk slot at its own link (the request's last
 // link), zero-padded to lp, in `work` (when max_own_lp > 0) and copies copy_bytes of tables from
@@ -522,6 +564,83 @@ hipError_t static_scratch(void **out);
 // Log-sum-exp merge of split partials into out / lse.
 // max_rows: most rows of one p.comb entry (unused when p.comb is NULL).
 hipError_t launch_combine(const LinkParams &p, int dtype, int32_t max_rows, hipStream_t st);
+
+// Merge of a call's partials from two sources (rows that a group of requests shares, and each
+// request's own): rows row0 .. row0 + rows of out, piece s of row i of source x at its partial
+// row part[x] + s * stride[x] + i.
+struct MergeEntry {
+  int32_t row0, rows;
+  int32_t part[2], stride[2], splits[2];
+};
+struct Partials {
+  float *o, *m, *l;           // [partial row][d_v], [partial row], [partial row]
+};
+struct MergeParams {
+  const MergeEntry *entries;
+  Partials src[2];
+  void *out;
+  float *lse;
+  int32_t d_v, blocks;        // blocks: workgroups of a request (set by launch_merge)
+};
+// max_rows, pieces: most rows and pieces of an entry
+hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows,
+                        int32_t pieces, hipStream_t st);
+
+// Link attention over selected blocks (kernels_sparse.hip). A request's blocks are the 64-token
+// tiles of its links, in order.
+struct SparseLink {
+  const char *k, *v;          // as LinkEntry
+  int32_t len, lp, tile0;
+  int32_t page;               // its first page in the pool (and in the summaries)
+};
+struct SparseReq {
+  int32_t link0, nlinks, blocks;
+  int32_t q0, lq, s0, ls;
+  int32_t pad;
+};
+constexpr int kSparseMostBlocks = 8192;       // of a request
+constexpr int kSparseMostTaken = 1024;
+struct SparseParams {
+  const SparseLink *links;
+  const SparseReq *reqs;
+  const int32_t *token_req;   // by query token
+  const char *means;          // bf16 [page][kv head][d] of the call's layer
+  const void *q, *k_self, *v_self;
+  void *out;
+  float *lse;
+  int32_t *taken;             // [token][kv head][n_blocks], or NULL
+  Partials part;              // splits > 1: piece s of output row i at partial row s * rows + i
+  int32_t total_q, n_q_heads, n_kv_heads, group;
+  int32_t n_blocks, first, last, most_blocks, splits;
+  int32_t token0, col_blocks, cols;   // set by launch_link_sparse
+  float scale_log2;
+};
+constexpr int kSparseTabLinks = 80, kSparseTabReqs = 16, kSparseTabTokens = 64;
+struct SparseTabs {
+  SparseLink links[kSparseTabLinks];
+  SparseReq reqs[kSparseTabReqs];
+  int32_t token_req[kSparseTabTokens];
+};
+static_assert(sizeof(SparseParams) + sizeof(SparseTabs) <= 4064, "kernel arguments");
+bool sparse_supported(int dtype, int mla, int d_k, int d_v);
+int sparse_waves();           // of a workgroup, which share a unit's blocks
+// tabs: used in place of the tables when not NULL
+hipError_t launch_link_sparse(const SparseParams &p, const SparseTabs *tabs, int dtype, int d, hipStream_t st);
+
+// Summaries of runs of pages, in n_layers layers from p's on.
+constexpr int kMeansPieces = 96;
+struct MeansPiece {
+  const char *k;              // K row 0 of head 0 of the run's first page
+  int32_t lp, page, n;        // row stride, first page, tokens
+};
+struct MeansParams {
+  MeansPiece piece[kMeansPieces];
+  void *means;
+  int64_t layer_bytes, layer_elems;
+  int32_t heads;
+};
+static_assert(sizeof(MeansParams) <= 4064, "kernel arguments");
+hipError_t launch_block_means(const MeansParams &p, int32_t n, int32_t n_layers, int dtype, int d, hipStream_t st);
 
 // Tables of a small call (vector-ALU or streaming kernel), passed by value as a kernel
 // argument: the call then needs neither the table copy nor the own-KV

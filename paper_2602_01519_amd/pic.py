@@ -57,6 +57,21 @@ class LinkReq(ctypes.Structure):
                 ("chunk_starts", ctypes.c_void_p), ("q_doc_limits", ctypes.c_void_p)]
 
 
+class LinkGroups(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("request_offsets", ctypes.c_void_p),
+                ("chunk_offsets", ctypes.c_void_p), ("chunk_ids", ctypes.c_void_p),
+                ("chunk_starts", ctypes.c_void_p)]
+
+
+class Append(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_int32), ("n_chunks", ctypes.c_int32),
+                ("chunk_ids", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("rope", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("q", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64), ("n_q_heads", ctypes.c_int32)]
+
+
 class RopeDesc(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("rot_at", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32),
@@ -92,6 +107,9 @@ def lib():
             "pic_store_derive": [vp, u64, u64, i32, vp, vp],
             "pic_store_write_rows": [vp, u64, i32, i32, vp, vp, vp, vp],
             "pic_store_usage": [vp, vp, vp, vp],
+            "pic_store_open": [vp, u64, i64],
+            "pic_store_append": [vp, vp, vp],
+            "pic_store_truncate": [vp, i32, vp, vp, vp],
             "pic_store_export": [vp, vp, ctypes.c_size_t, vp],
             "pic_store_import": [vp, ctypes.c_size_t, vp],
             "pic_link_attn": [vp, vp, i32, vp, vp, vp, f32, vp, vp, vp],
@@ -100,6 +118,12 @@ def lib():
             "pic_debug_gather": [vp, vp, i32, i32, vp, vp, vp],
             "pic_debug_request_order": [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp],
             "pic_link_plan_create": [vp, vp, i32, i32, i32, vp],
+            "pic_link_shared": [vp, vp, vp, i32, vp, vp, vp, f32, vp, vp, vp],
+            "pic_link_shared_plan_create": [vp, vp, vp, i32, vp],
+            "pic_index_create": [vp, vp],
+            "pic_index_update": [vp, i32, i32, vp, vp],
+            "pic_index_destroy": [vp],
+            "pic_link_sparse": [vp, vp, i32, i32, i32, i32, vp, vp, vp, f32, vp, vp, vp, vp],
             "pic_link_plan_run": [vp, i32, vp, vp, vp, f32, vp, vp, vp],
             "pic_link_plan_destroy": [vp],
             "pic_mla_absorb_q": [i32, i32, vp, vp, vp, vp],
@@ -148,6 +172,16 @@ def _ptr(x):
     if isinstance(x, np.ndarray):
         return x.ctypes.data
     return int(x) if isinstance(x, int) else x.data_ptr()    # torch tensor
+
+
+def _token_stride(x) -> int:
+    """Elements from token to token of a torch tensor [tokens][heads][width] whose tokens are dense
+    rows (0: leave it to the call)."""
+    if not hasattr(x, "stride"):
+        return 0
+    if x.dim() != 3 or (x.numel() and (x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]))):
+        raise PicError(ERR_INVALID, "a tensor must be [tokens][heads][width] with dense rows")
+    return x.stride(0) if x.shape[0] > 1 else 0
 
 
 def _host_i32(a):
@@ -208,6 +242,38 @@ class Store:
         r = np.ascontiguousarray(rows, dtype=np.int32)
         _check(lib().pic_store_write_rows(self.handle, int(chunk_id), int(layer), int(r.size),
                                           r.ctypes.data if r.size else None, _ptr(k), _ptr(v), stream))
+
+    def open(self, chunk_id: int, max_tokens: int):
+        """pic_store_open: an empty growing chunk with pages for max_tokens tokens."""
+        _check(lib().pic_store_open(self.handle, int(chunk_id), int(max_tokens)))
+
+    def append(self, chunk_ids, offsets, k, v=None, rope: Optional["Rope"] = None, positions=None,
+               q=None, q_out=None, stream: Optional[int] = None, layer: int = 0, k_stride: int = 0,
+               v_stride: int = 0, q_stride: int = 0, q_out_stride: int = 0, n_q_heads: int = 0):
+        """pic_store_append: tokens offsets[i] .. offsets[i+1]-1 of k and v become the next rows of
+        growing chunk chunk_ids[i]. Of torch tensors [tokens][heads][width] the strides from token
+        to token and the number of query heads are taken from the tensors where they are not given."""
+        if rope is not None and not rope.handle:
+            raise PicError(ERR_INVALID, "the rotary handle is closed")
+        ids = np.ascontiguousarray(chunk_ids, dtype=np.uint64)
+        at = _host_i32(offsets)
+        if len(at) != len(ids) + 1:
+            raise PicError(ERR_INVALID, "offsets must have one entry more than chunk_ids")
+        a = Append(int(layer), len(ids), _addr(ids) if ids.size else None, _addr(at), _ptr(k), _ptr(v),
+                   k_stride or _token_stride(k), v_stride or _token_stride(v),
+                   None if rope is None else rope.handle, _ptr(positions), _ptr(q), _ptr(q_out),
+                   q_stride or _token_stride(q), q_out_stride or _token_stride(q_out),
+                   int(n_q_heads) or (q.shape[1] if hasattr(q, "shape") else 0))
+        _check(lib().pic_store_append(self.handle, ctypes.byref(a), stream))
+
+    def truncate(self, chunk_ids, n_tokens, stream: Optional[int] = None):
+        """pic_store_truncate: growing chunk chunk_ids[i] keeps at most its first n_tokens[i] tokens."""
+        ids = np.ascontiguousarray(chunk_ids, dtype=np.uint64)
+        n = np.ascontiguousarray(n_tokens, dtype=np.int64)
+        if len(n) != len(ids):
+            raise PicError(ERR_INVALID, "n_tokens must have an entry for each chunk")
+        _check(lib().pic_store_truncate(self.handle, len(ids), _addr(ids) if ids.size else None,
+                                        _addr(n) if n.size else None, stream))
 
     def export(self) -> bytes:
         """pic_store_export: a description of the store another process can import."""
@@ -379,6 +445,100 @@ class LinkPlan:
             self.close()
         except Exception:
             pass
+
+
+def _groups(request_offsets, chunk_offsets, chunk_ids, chunk_starts, keep: list):
+    ro, co = _host_i32(request_offsets), _host_i32(chunk_offsets)
+    ids = np.ascontiguousarray(chunk_ids, dtype=np.uint64)
+    st = _host_i32(chunk_starts)
+    if len(ro) != len(co):
+        raise PicError(ERR_INVALID, "request_offsets and chunk_offsets of the groups must be as long")
+    keep += [ro, co, ids, st]
+    return LinkGroups(len(ro) - 1, _addr(ro), _addr(co), _addr(ids) if ids.size else None,
+                      None if st is None or not st.size else _addr(st))
+
+
+def link_shared(store: Store, group_requests, group_offsets, group_ids, chunk_offsets, chunk_ids,
+                q_offsets, self_offsets, n_q_heads: int, q, k_self, v_self, softmax_scale: float, out,
+                lse=None, stream: Optional[int] = None, layer: int = 0, chunk_starts=None,
+                q_doc_limits=None, group_starts=None):
+    """pic_link_shared: link attention of requests that share links in groups. Group g, requests
+    group_requests[g] .. group_requests[g+1]-1, shares group_ids[group_offsets[g]] ..; the other
+    arguments as for link_attn."""
+    keep: list = []
+    req = _req(chunk_offsets, chunk_ids, q_offsets, self_offsets, keep, layer, chunk_starts,
+               q_doc_limits)
+    groups = _groups(group_requests, group_offsets, group_ids, group_starts, keep)
+    _check(lib().pic_link_shared(store.handle, ctypes.byref(req), ctypes.byref(groups), int(n_q_heads),
+                                 _ptr(q), _ptr(k_self), _ptr(v_self), float(softmax_scale), _ptr(out),
+                                 _ptr(lse), stream))
+
+
+class SharedLinkPlan(LinkPlan):
+    """pic_link_shared_plan_create: link_shared's batch resolved once, run per layer / decode step."""
+
+    def __init__(self, store: Store, group_requests, group_offsets, group_ids, chunk_offsets, chunk_ids,
+                 q_offsets, self_offsets, n_q_heads: int, chunk_starts=None, q_doc_limits=None,
+                 group_starts=None):
+        keep: list = []
+        req = _req(chunk_offsets, chunk_ids, q_offsets, self_offsets, keep, chunk_starts=chunk_starts,
+                   q_doc_limits=q_doc_limits)
+        groups = _groups(group_requests, group_offsets, group_ids, group_starts, keep)
+        h = ctypes.c_void_p()
+        _check(lib().pic_link_shared_plan_create(store.handle, ctypes.byref(req), ctypes.byref(groups),
+                                                 int(n_q_heads), ctypes.byref(h)))
+        self.handle = h.value
+        self.store = store          # the store must outlive the plan
+        self._run = lib().pic_link_plan_run
+
+
+class BlockIndex:
+    """pic_index_*: summaries of a store's 64-token blocks, for link_sparse."""
+
+    def __init__(self, store: Store):
+        h = ctypes.c_void_p()
+        _check(lib().pic_index_create(store.handle, ctypes.byref(h)))
+        self.handle = h.value
+        self.store = store          # the store must outlive the index
+
+    def update(self, chunk_ids, layer: int = -1, stream: Optional[int] = None):
+        """pic_index_update: the summaries of the listed chunks as they stand (layer -1: every layer)."""
+        if not self.handle:
+            raise PicError(ERR_INVALID, "the index is closed")
+        ids = np.ascontiguousarray(chunk_ids, dtype=np.uint64)
+        _check(lib().pic_index_update(self.handle, int(layer), len(ids), _addr(ids) if ids.size else None, stream))
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(lib().pic_index_destroy(self.handle))
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def link_sparse(index: BlockIndex, chunk_offsets, chunk_ids, q_offsets, self_offsets, n_q_heads: int,
+                n_blocks: int, q, k_self, v_self, softmax_scale: float, out, lse=None, keep_first: int = 0,
+                keep_last: int = 0, blocks=None, stream: Optional[int] = None, layer: int = 0,
+                chunk_starts=None):
+    """pic_link_sparse: link attention over the n_blocks blocks of each request that score best for a
+    query token; the other arguments as for link_attn."""
+    if not index.handle:
+        raise PicError(ERR_INVALID, "the index is closed")
+    keep: list = []
+    req = _req(chunk_offsets, chunk_ids, q_offsets, self_offsets, keep, layer, chunk_starts)
+    _check(lib().pic_link_sparse(index.handle, ctypes.byref(req), int(n_q_heads), int(n_blocks),
+                                 int(keep_first), int(keep_last), _ptr(q), _ptr(k_self), _ptr(v_self),
+                                 float(softmax_scale), _ptr(out), _ptr(lse), _ptr(blocks), stream))
 
 
 def mla_absorb_q(n_tokens: int, n_heads: int, q, w_uk_t, q_out, stream: Optional[int] = None):
