@@ -194,7 +194,7 @@ def test_runs_of_pages_and_what_they_held():
 
     def attend(hq=4, n=3):
         q = L.draw(rng, pic.BF16, n, hq, 128)
-        out, lse = torch.empty_like(q), torch.empty(n, hq, device="cuda")
+        out, lse = torch.empty_like(q), torch.empty(n, hq, dtype=torch.float32, device="cuda")
         for call in (pic.link_decode, pic.link_attn):
             call(c.store, [0, 1], [77], [0, n], None, hq, q, None, None, 128 ** -0.5, out, lse, stream=L.stream())
             torch.cuda.synchronize()
@@ -239,7 +239,7 @@ def test_layers_grow_by_calls_of_their_own():
         c.check(layer=layer)
     assert [c.store.lookup(i) for i in c.ids] == [3, 5]
     q = L.draw(rng, pic.BF16, 2, 4, 64)
-    out, lse = torch.empty_like(q), torch.empty(2, 4, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(2, 4, dtype=torch.float32, device="cuda")
     for layer in range(3):
         pic.link_decode(c.store, [0, 1, 2], c.ids, [0, 1, 2], None, 4, q, None, None, 0.125, out, lse,
                         stream=L.stream(), layer=layer)
@@ -289,7 +289,7 @@ def test_decode_steps_over_documents_and_their_own_tokens(dtype, d):
         lens = [c.held(r) for r in range(B)]
         docs_n = [sum(len(docs[i][0]) for i in l) for l in links]
         limits = None if lq == 1 else np.concatenate([np.arange(a + n - lq + 1, a + n + 1) for a, n in zip(docs_n, lens)])
-        out, lse = torch.empty_like(q), torch.empty(len(q), hq, device="cuda")
+        out, lse = torch.empty_like(q), torch.empty(len(q), hq, dtype=torch.float32, device="cuda")
         pic.link_decode(c.store, L.offsets([len(l) + 1 for l in links]), [x for l, i in zip(links, c.ids) for x in l + [i]],
                         L.offsets([lq] * B), None, hq, q, None, None, scale, out, lse, stream=L.stream(), q_doc_limits=limits)
         torch.cuda.synchronize()

@@ -82,7 +82,7 @@ class Batch:
 
     def buffers(self):
         out = torch.full((len(self.q), self.hq, self.dv), 7.0, dtype=self.q.dtype, device="cuda")
-        return out, torch.full(self.q.shape[:2], 3.0, device="cuda")
+        return out, torch.full(self.q.shape[:2], 3.0, dtype=torch.float32, device="cuda")
 
     def call(self, layer=0, stream=None, out=None, lse=None):
         if out is None:
@@ -250,7 +250,7 @@ def test_growing_chunks_behind_shared_documents():
             pos = torch.arange(sum(n), dtype=torch.int32, device="cuda") + 270
             store.append([10 + r for r in range(4)], at, k, v, rope, pos, stream=L.stream())
             q = L.draw(rng, pic.BF16, 4, 8, 128)
-            out, lse = torch.empty_like(q), torch.empty(4, 8, device="cuda")
+            out, lse = torch.empty_like(q), torch.empty(4, 8, dtype=torch.float32, device="cuda")
             pic.link_shared(store, [0, 4], [0, 1], [1], range(5), [10 + r for r in range(4)], range(5), None, 8, q, None,
                             None, b.scale, out, lse, stream=L.stream())
             torch.cuda.synchronize()

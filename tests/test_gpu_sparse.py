@@ -55,7 +55,7 @@ class Case:
                 None if self.own is None else L.offsets(self.own), self.hq)
 
     def buffers(self, n_blocks):
-        return (torch.full_like(self.q, 7.0), torch.full(self.q.shape[:2], 3.0, device="cuda"),
+        return (torch.full_like(self.q, 7.0), torch.full(self.q.shape[:2], 3.0, dtype=torch.float32, device="cuda"),
                 torch.full((len(self.q), self.hkv, n_blocks), -9, dtype=torch.int32, device="cuda"))
 
     def call(self, n_blocks, first=0, last=0, layer=0, bufs=None, stream=None):
@@ -266,7 +266,7 @@ def test_longest_requests(blocks, ok):
         with pic.BlockIndex(store) as index:
             index.update([1], stream=L.stream())
             q = L.draw(rng, pic.BF16, 1, 2, 64)
-            out, lse = torch.full_like(q, 7.0), torch.zeros(1, 2, device="cuda")
+            out, lse = torch.full_like(q, 7.0), torch.zeros(1, 2, dtype=torch.float32, device="cuda")
             taken = torch.full((1, 1, 1024), -9, dtype=torch.int32, device="cuda")
             call = lambda m: pic.link_sparse(index, [0, 1], [1], [0, 1], None, 2, m, q, None, None, 0.125, out, lse,  # noqa: E731
                                              keep_first=1, keep_last=1, blocks=taken, stream=L.stream())
