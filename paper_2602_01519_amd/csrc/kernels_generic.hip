@@ -46,10 +46,10 @@ typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 // the list). 16-byte pieces; one element a thread, with a search for each element's link, took
 // 6144 tokens x 8 heads x 128 bf16 in GATHER_OLD us, now GATHER_NEW.
 template <typename E>
-__global__ __launch_bounds__(256) void gather_kernel(const LinkEntry *__restrict__ links,
-                                                     int32_t n_links, int64_t units, int32_t heads,
-                                                     int32_t d_k, int32_t d_v, int32_t v_parts,
-                                                     E *__restrict__ k_out, E *__restrict__ v_out) {
+__device__ __forceinline__ void gather_pages(const LinkEntry *__restrict__ links, int32_t n_links,
+                                             int64_t units, int32_t heads, int32_t d_k, int32_t d_v,
+                                             int32_t v_parts, E *__restrict__ k_out,
+                                             E *__restrict__ v_out) {
   constexpr int N = 16 / sizeof(E);
   constexpr int ROW = 64 + N;                // padded LDS row (elements)
   __shared__ __attribute__((aligned(16))) E tile[64 * ROW];
@@ -96,6 +96,24 @@ __global__ __launch_bounds__(256) void gather_kernel(const LinkEntry *__restrict
     }
     __syncthreads();
   }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void gather_kernel(const LinkEntry *links, int32_t n_links,
+                                                     int64_t units, int32_t heads, int32_t d_k,
+                                                     int32_t d_v, int32_t v_parts, E *k_out, E *v_out) {
+  gather_pages<E>(links, n_links, units, heads, d_k, d_v, v_parts, k_out, v_out);
+}
+struct GatherLinks {
+  LinkEntry link[kGatherArgs];
+};
+static_assert(sizeof(GatherLinks) <= 3960, "kernel arguments");
+template <typename E>
+__global__ __launch_bounds__(256) void gather_args_kernel(GatherLinks links, int32_t n_links,
+                                                          int64_t units, int32_t heads, int32_t d_k,
+                                                          int32_t d_v, int32_t v_parts, E *k_out,
+                                                          E *v_out) {
+  gather_pages<E>(links.link, n_links, units, heads, d_k, d_v, v_parts, k_out, v_out);
 }
 
 // Rows written into chunk slots (rows recomputed at link time): row i of the
@@ -1477,18 +1495,25 @@ hipError_t launch_write_rows(const RowView *views, int32_t n_views, const int32_
 
 hipError_t launch_gather(const LinkEntry *links, int32_t n_links, int64_t pages,
                          int32_t heads, int32_t d_k, int32_t d_v, int32_t mla, int32_t esz,
-                         void *k_out, void *v_out, hipStream_t st) {
+                         bool host, void *k_out, void *v_out, hipStream_t st) {
   const int32_t v_parts = mla ? 0 : (d_v + 63) / 64;
   const int64_t units = pages * heads * (v_parts + 1);
   if (units == 0) return hipSuccess;
-  const unsigned blocks = (unsigned)std::min<int64_t>(units, 65536);
-  if (esz == 2)
-    hipLaunchKernelGGL(gather_kernel<uint16_t>, dim3(blocks), dim3(256), 0, st, links, n_links,
-                       units, heads, d_k, d_v, v_parts, (uint16_t *)k_out, (uint16_t *)v_out);
-  else
-    hipLaunchKernelGGL(gather_kernel<uint32_t>, dim3(blocks), dim3(256), 0, st, links, n_links,
-                       units, heads, d_k, d_v, v_parts, (uint32_t *)k_out, (uint32_t *)v_out);
-  return hipGetLastError();
+  const dim3 grid((unsigned)std::min<int64_t>(units, 65536));
+  const auto go = [&](auto e) {
+    typedef decltype(e) E;
+    if (host) {
+      GatherLinks args;
+      std::copy(links, links + n_links, args.link);
+      hipLaunchKernelGGL(gather_args_kernel<E>, grid, dim3(256), 0, st, args, n_links, units, heads, d_k,
+                         d_v, v_parts, (E *)k_out, (E *)v_out);
+    } else {
+      hipLaunchKernelGGL(gather_kernel<E>, grid, dim3(256), 0, st, links, n_links, units, heads, d_k, d_v,
+                         v_parts, (E *)k_out, (E *)v_out);
+    }
+    return hipGetLastError();
+  };
+  return esz == 2 ? go(uint16_t()) : go(uint32_t());
 }
 
 hipError_t launch_prologue(const LinkParams &p, const LinkEntry *links, const ReqEntry *reqs,

@@ -5,8 +5,7 @@
 //
 // Bound by the partials' bytes, for few rows by latency: as in combine_kernel, kLanes lanes take
 // a row (16, 32 or 64: d_v up to 64, 128, more), kGpr groups of them share a row's pieces where
-// these are many, and a group has kB pieces' loads in flight. Values of pieces that hold no key
-// of the row (m = -inf) are not read.
+// these are many, and a group has kB pieces' loads in flight.
 #include <algorithm>
 #include <cfloat>
 
@@ -83,8 +82,11 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeParams p) {
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
         const int at = 4 * (kLanes * c + lane);
-        v[k][c] = at < dv && pc[k].m != -INFINITY ? *(const float4 *)(pc[k].o + at)
-                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+        // (with p.sparse the values of a piece that holds no key may be unwritten: they wait for
+        // the maxima)
+        v[k][c] = at < dv && s0 + k * kGpr < S && (!p.sparse || pc[k].m != -INFINITY)
+                      ? *(const float4 *)(pc[k].o + at)
+                      : make_float4(0.f, 0.f, 0.f, 0.f);
       }
     if (top == -INFINITY) continue;
     rescale(top);

@@ -507,8 +507,8 @@ __device__ __forceinline__ void select_blocks(const uint64_t *key, int n, int ta
 }
 
 template <typename T, int D>
-__device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseLink *links, const SparseReq *reqs,
-                                            const int32_t *token_req) {
+__device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseLink *links,
+                                            const SparseToken *tokens) {
   constexpr int kCols = sizeof(T) == 4 ? 4 : 16;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -518,7 +518,7 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   const int cb = x % p.col_blocks;
   x /= p.col_blocks;
   const int kvh = x % p.n_kv_heads, tok = p.token0 + x / p.n_kv_heads;
-  const SparseReq R = reqs[token_req[tok]];
+  const SparseToken R = tokens[tok];
   const int n = R.blocks, take = min(n, p.n_blocks);
   const Layout at = layout_of<T, D>(p.most_blocks, p.n_blocks, p.cols);
   int32_t *page = (int32_t *)(lds + at.page);
@@ -577,7 +577,7 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   const int64_t own_at = R.s0 * u.own_stride + kvh * D * (int)sizeof(T);
   u.k_own = (const char *)p.k_self + own_at;
   u.v_own = (const char *)p.v_self + own_at;
-  u.own = R.ls > 0 ? tok - R.q0 + 1 + R.ls - R.lq : 0;
+  u.own = R.own;
   const int stride = p.cols;            // columns of a wave's state
   float *o = (float *)lds, *m = o + kWaves * stride * D, *l = m + kWaves * stride;
   attend<D>(u, q, cols, split * kWaves + wave, p.splits * kWaves, lane, p.scale_log2, lds + at.extra,
@@ -628,12 +628,12 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
 
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, 1) void link_sparse_kernel(SparseParams p) {
-  link_sparse<T, D>(p, p.links, p.reqs, p.token_req);
+  link_sparse<T, D>(p, p.links, p.tokens);
 }
 // Tables of a small call as a kernel argument.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, 1) void link_sparse_tabs_kernel(SparseParams p, SparseTabs t) {
-  link_sparse<T, D>(p, t.links, t.reqs, t.token_req);
+  link_sparse<T, D>(p, t.links, t.tokens);
 }
 
 template <typename T, int D>

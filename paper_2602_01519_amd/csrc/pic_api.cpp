@@ -1732,6 +1732,7 @@ pic_status launch_shared(const pic_store *s, const SharedCall &S, char *dev, con
   m.out = out;
   m.lse = lse;
   m.d_v = d_v;
+  m.sparse = S.own.lp.skip_empty;
   const auto run = [&](const Setup &C, const TableLayout &t, size_t off, const Partials &to, const Prologue &pro,
                        const void *ks, const void *vs) {
     LinkParams lp = C.lp;
@@ -3029,12 +3030,14 @@ pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_he
     if (tq == 0) return PIC_OK;
     SparseParams p{};
     std::vector<SparseLink> links;
-    std::vector<SparseReq> reqs(B);
+    std::vector<SparseToken> tokens(tq);
     links.reserve(P.pages.size());
     for (int32_t r = 0; r < B; ++r) {
       const ReqEntry &R = P.reqs[r];
       const int32_t n = R.nlinks - (R.ls > 0);            // (the own KV is the last)
-      reqs[r] = SparseReq{(int32_t)links.size(), n, R.doc_tiles, R.q0, R.lq, R.s0, R.ls, 0};
+      for (int32_t i = 0; i < R.lq; ++i)
+        tokens[R.q0 + i] = SparseToken{(int32_t)links.size(), n, R.doc_tiles, R.s0,
+                                       R.ls > 0 ? i + 1 + R.ls - R.lq : 0, {0, 0, 0}};
       if (R.doc_tiles > kSparseMostBlocks)
         return fail(PIC_ERR_UNSUPPORTED, "request %d links %d blocks, at most %d", r, R.doc_tiles, kSparseMostBlocks);
       p.most_blocks = std::max(p.most_blocks, R.doc_tiles);
@@ -3063,18 +3066,15 @@ pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_he
     DeviceGuard dg(s->device);
     if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
     const hipStream_t st = (hipStream_t)stream;
-    const size_t off_r = round_up(sizeof(SparseLink) * links.size(), 256);
-    const size_t off_t = off_r + round_up(sizeof(SparseReq) * B, 256);
-    const size_t off_m = off_t + round_up(sizeof(int32_t) * tq, 256);
+    const size_t off_t = round_up(sizeof(SparseLink) * links.size(), 256);
+    const size_t off_m = off_t + round_up(sizeof(SparseToken) * tq, 256);
     const size_t bytes = off_m + (p.splits > 1 ? round_up(sizeof(MergeEntry) * B, 256) : 0);
-    const bool by_arg = p.splits == 1 && links.size() <= (size_t)kSparseTabLinks && B <= kSparseTabReqs &&
-                        tq <= kSparseTabTokens;
+    const bool by_arg = p.splits == 1 && links.size() <= (size_t)kSparseTabLinks && tq <= kSparseTabTokens;
     std::pair<hipEvent_t, hipEvent_t> ev{nullptr, nullptr};
     if (by_arg) {
       SparseTabs t{};
       std::copy(links.begin(), links.end(), t.links);
-      std::copy(reqs.begin(), reqs.end(), t.reqs);
-      for (int32_t r = 0; r < B; ++r) std::fill(t.token_req + reqs[r].q0, t.token_req + reqs[r].q0 + reqs[r].lq, r);
+      std::copy(tokens.begin(), tokens.end(), t.tokens);
       prof_start(st, &ev);
       const hipError_t e = launch_link_sparse(p, &t, d.dtype, d.d_k, st);
       prof_stop(st, &ev, "link_sparse_tabs_kernel");
@@ -3088,21 +3088,16 @@ pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_he
     if (rc != PIC_OK) return rc;
     char *h = (char *)stage->host, *dev = (char *)stage->dev;
     if (!links.empty()) memcpy(h, links.data(), sizeof(SparseLink) * links.size());
-    memcpy(h + off_r, reqs.data(), sizeof(SparseReq) * B);
-    int32_t *token_req = (int32_t *)(h + off_t), most_rows = 0;
-    for (int32_t r = 0; r < B; ++r) {
-      const SparseReq &R = reqs[r];
-      std::fill(token_req + R.q0, token_req + R.q0 + R.lq, r);
-      if (p.splits > 1) {
-        const int32_t row0 = R.q0 * n_q_heads;
-        ((MergeEntry *)(h + off_m))[r] = MergeEntry{row0, R.lq * n_q_heads, {row0, 0}, {(int32_t)rows, 0}, {p.splits, 0}};
-        most_rows = std::max(most_rows, R.lq * n_q_heads);
-      }
+    memcpy(h + off_t, tokens.data(), sizeof(SparseToken) * tq);
+    int32_t most_rows = 0;
+    for (int32_t r = 0; p.splits > 1 && r < B; ++r) {
+      const int32_t row0 = P.reqs[r].q0 * n_q_heads, n = P.reqs[r].lq * n_q_heads;
+      ((MergeEntry *)(h + off_m))[r] = MergeEntry{row0, n, {row0, 0}, {(int32_t)rows, 0}, {p.splits, 0}};
+      most_rows = std::max(most_rows, n);
     }
     HIP_TRY(launch_table_copy(stage->host_dev, dev, (int64_t)bytes, st), "table_copy_kernel");
     p.links = (const SparseLink *)dev;
-    p.reqs = (const SparseReq *)(dev + off_r);
-    p.token_req = (const int32_t *)(dev + off_t);
+    p.tokens = (const SparseToken *)(dev + off_t);
     if (p.splits > 1) p.part = place_partials((char *)stage->work, rows * p.splits, d.d_v);
     prof_start(st, &ev);
     const hipError_t e = launch_link_sparse(p, nullptr, d.dtype, d.d_k, st);
@@ -3165,15 +3160,21 @@ pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_
     }
     return PIC_OK;
   }
+  const pic_store_desc &d = s->desc;
+  if (n <= kGatherArgs) {
+    const hipError_t e = launch_gather(links.data(), n, pages, d.n_kv_heads, d.d_k, d.d_v, !gqa, s->esz, true,
+                                       k_out, v_out, st);
+    if (e != hipSuccess) return hip_fail(e, "gather_kernel");
+    return PIC_OK;
+  }
   Stage *stage = nullptr;
   pic_status rc = stage_acquire(s, sizeof(LinkEntry) * n, &stage);
   if (rc != PIC_OK) return rc;
   memcpy(stage->host, links.data(), sizeof(LinkEntry) * n);
   HIP_TRY(launch_table_copy(stage->host_dev, stage->dev, (int64_t)(sizeof(LinkEntry) * n), st),
           "table_copy_kernel");
-  const pic_store_desc &d = s->desc;
   hipError_t e = launch_gather((const LinkEntry *)stage->dev, n, pages, d.n_kv_heads,
-                               d.d_k, d.d_v, !gqa, s->esz, k_out, v_out, st);
+                               d.d_k, d.d_v, !gqa, s->esz, false, k_out, v_out, st);
   if (e != hipSuccess) return hip_fail(e, "gather_kernel");
   HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");
   stage->pending = true;

@@ -340,10 +340,12 @@ struct PutParams {
   int32_t rows_blocks;            // set by launch_put
 };
 hipError_t launch_put(PutParams pp, int32_t n_layers, hipStream_t st);
-// links' tile0: their first page in the list, of `pages` in all.
+// links' tile0: their first page in the list, of `pages` in all. host: the links are in host
+// memory, at most kGatherArgs of them, and go as a kernel argument.
+constexpr int kGatherArgs = 120;
 hipError_t launch_gather(const LinkEntry *links, int32_t n_links, int64_t pages,
                          int32_t heads, int32_t d_k, int32_t d_v, int32_t mla, int32_t esz,
-                         void *k_out, void *v_out, hipStream_t st);
+                         bool host, void *k_out, void *v_out, hipStream_t st);
 
 // Page copies of a derived chunk (kernel argument): pages of 64 tokens, kv
 // head 0 of layer 0 (head h at + h * lp * width elements); v NULL for MLA.
@@ -580,7 +582,9 @@ struct MergeParams {
   Partials src[2];
   void *out;
   float *lse;
-  int32_t d_v, blocks;        // blocks: workgroups of a request (set by launch_merge)
+  int32_t d_v;
+  int32_t sparse;             // values of pieces that hold no key may be unwritten
+  int32_t blocks;             // workgroups of a request (set by launch_merge)
 };
 // max_rows, pieces: most rows and pieces of an entry
 hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows,
@@ -593,17 +597,16 @@ struct SparseLink {
   int32_t len, lp, tile0;
   int32_t page;               // its first page in the pool (and in the summaries)
 };
-struct SparseReq {
+struct SparseToken {          // a query token: its request's links and blocks, its own keys
   int32_t link0, nlinks, blocks;
-  int32_t q0, lq, s0, ls;
-  int32_t pad;
+  int32_t s0, own;            // first own row of the request, own keys that the token sees
+  int32_t pad[3];
 };
 constexpr int kSparseMostBlocks = 8192;       // of a request
 constexpr int kSparseMostTaken = 1024;
 struct SparseParams {
   const SparseLink *links;
-  const SparseReq *reqs;
-  const int32_t *token_req;   // by query token
+  const SparseToken *tokens;
   const char *means;          // bf16 [page][kv head][d] of the call's layer
   const void *q, *k_self, *v_self;
   void *out;
@@ -615,11 +618,10 @@ struct SparseParams {
   int32_t token0, col_blocks, cols;   // set by launch_link_sparse
   float scale_log2;
 };
-constexpr int kSparseTabLinks = 80, kSparseTabReqs = 16, kSparseTabTokens = 64;
+constexpr int kSparseTabLinks = 88, kSparseTabTokens = 32;
 struct SparseTabs {
   SparseLink links[kSparseTabLinks];
-  SparseReq reqs[kSparseTabReqs];
-  int32_t token_req[kSparseTabTokens];
+  SparseToken tokens[kSparseTabTokens];
 };
 static_assert(sizeof(SparseParams) + sizeof(SparseTabs) <= 4064, "kernel arguments");
 bool sparse_supported(int dtype, int mla, int d_k, int d_v);
