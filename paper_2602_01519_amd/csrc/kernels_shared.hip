@@ -36,14 +36,25 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeParams p) {
   const int grp = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, sub = grp % kGpr;
   typedef __attribute__((address_space(4))) const MergeEntry *const_entries;
   const int r = blockIdx.x / p.blocks, b = blockIdx.x - r * p.blocks;
-  const const_entries e = (const_entries)p.entries + r;
-  const int nrows = e->rows;
+  MergeEntry e = p.one;
+  if (p.entries) {
+    const const_entries t = (const_entries)p.entries + r;
+    e.row0 = t->row0;
+    e.rows = t->rows;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      e.part[i] = t->part[i];
+      e.stride[i] = t->stride[i];
+      e.splits[i] = t->splits[i];
+    }
+  }
+  const int nrows = e.rows;
   if (b * kRows >= nrows) return;
   const int i = b * kRows + grp / kGpr;
   const bool valid = i < nrows;
-  const int sa = e->splits[0], S = valid ? sa + e->splits[1] : 0, dv = p.d_v;
-  const int64_t at_a = (int64_t)e->part[0] + i, at_b = (int64_t)e->part[1] + i;
-  const int64_t step_a = e->stride[0], step_b = e->stride[1];
+  const int sa = e.splits[0], S = valid ? sa + e.splits[1] : 0, dv = p.d_v;
+  const int64_t at_a = (int64_t)e.part[0] + i, at_b = (int64_t)e.part[1] + i;
+  const int64_t step_a = e.stride[0], step_b = e.stride[1];
   struct Piece {
     const float *o;
     float m, l;
@@ -126,7 +137,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeParams p) {
     }
   }
   if (!valid) return;
-  const int64_t orow = (int64_t)e->row0 + i;
+  const int64_t orow = (int64_t)e.row0 + i;
   T *out = (T *)p.out + orow * dv;
   const float inv = M == -INFINITY ? 0.f : 1.f / L;
 #pragma unroll
@@ -159,7 +170,7 @@ hipError_t launch_merge_t(MergeParams p, int32_t batch, int32_t max_rows, int32_
     const int most = std::max(1, ((1 << 24) - 1) / p.blocks);
     const MergeEntry *all = p.entries;
     for (int32_t at = 0; at < batch; at += most) {
-      p.entries = all + at;
+      p.entries = all ? all + at : nullptr;
       hipLaunchKernelGGL((merge_kernel<T, kLanes, kChunks, kGpr>),
                          dim3((unsigned)p.blocks * std::min(most, batch - at)), dim3(256), 0, st, p);
     }

@@ -89,13 +89,18 @@ __device__ __forceinline__ float col_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// LDS of a workgroup, for at most n blocks of a request, k taken ones and cols columns. The
-// merge of the waves' states reuses it from the start.
+// LDS of a workgroup, for at most n blocks of a request, k taken ones and cols columns. The own
+// values' way to their operand uses it before, the merge of the waves' states after.
 struct Layout {
   uint32_t page, link, sel_k, sel_v, sel_n, extra, bytes;
 };
+// A wave's own values on their way to the value operand (bf16).
 template <typename T, int D>
-__host__ __device__ __forceinline__ Layout layout_of(int n, int k, int cols) {
+__host__ __device__ constexpr uint32_t own_scratch() {
+  return sizeof(T) == 4 ? 0 : kT * (2 * D + 16);
+}
+template <typename T, int D>
+__host__ __device__ __forceinline__ Layout layout_of(int n, int k, int cols, bool own) {
   constexpr int kCols = sizeof(T) == 4 ? 4 : 16;
   Layout l;
   l.page = 8u * n;                      // keys: 8 bytes a block from 0
@@ -108,6 +113,7 @@ __host__ __device__ __forceinline__ Layout layout_of(int n, int k, int cols) {
   l.bytes = l.extra + (sizeof(T) == 4 ? 4u * kCols * D + 4u * kWaves * kCols * 64 : 0u);
   const uint32_t merge = 4u * kWaves * cols * (D + 2);
   if (l.bytes < merge) l.bytes = merge;
+  if (own && l.bytes < own_scratch<T, D>() * kWaves) l.bytes = own_scratch<T, D>() * kWaves;
   return l;
 }
 
@@ -153,9 +159,12 @@ __device__ __forceinline__ void load_tile(const char *k, const char *v, int half
   for (int b = 0; b < D / 16; ++b) x.v[b] = load_nt(v + voff + 16 * b * kT * 2);
 }
 // Own keys j0 .. read in place; keys past `last` reread it (their scores are masked), their
-// values are zeros.
+// values are zeros. The values go through LDS (`scratch`, this wave's): gathered from memory two
+// bytes at a time, as eight rounds of dependent loads, an own tile held its wave for 16 us in
+// a batch that fills HBM.
 template <int D>
-__device__ __forceinline__ void load_own(const Unit &u, int j0, int last, int lane, Tile<D> &x) {
+__device__ __forceinline__ void load_own(const Unit &u, int j0, int last, int lane, char *scratch, Tile<D> &x) {
+  constexpr int kRow = 2 * D + 16;      // padded row (bytes)
   const int grp = lane >> 4, m = lane & 15;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
@@ -163,21 +172,28 @@ __device__ __forceinline__ void load_own(const Unit &u, int j0, int last, int la
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) x.k[b * (D / 32) + s] = *(const uint4 *)(row + 64 * s);
   }
-  uint32_t w[D / 16][4];
+  uint4 v[D / 16];
 #pragma unroll
-  for (int b = 0; b < D / 16; ++b)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[b][i] = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int key = j0 + 8 * grp + i;
-    const uint16_t *row = (const uint16_t *)(u.v_own + min(key, last) * u.own_stride) + m;
-    const uint32_t keep = key <= last ? 0xffffu : 0u;
-#pragma unroll
-    for (int b = 0; b < D / 16; ++b) w[b][i >> 1] |= (row[16 * b] & keep) << (16 * (i & 1));
+  for (int i = 0; i < D / 16; ++i) {
+    const int key = (i * 64 + lane) / (D / 8), c = lane % (D / 8);
+    v[i] = *(const uint4 *)(u.v_own + min(j0 + key, last) * u.own_stride + 16 * c);
+    if (j0 + key > last) v[i] = make_uint4(0, 0, 0, 0);
   }
 #pragma unroll
-  for (int b = 0; b < D / 16; ++b) x.v[b] = make_uint4(w[b][0], w[b][1], w[b][2], w[b][3]);
+  for (int i = 0; i < D / 16; ++i)
+    *(uint4 *)(scratch + (i * 64 + lane) / (D / 8) * kRow + 16 * (lane % (D / 8))) = v[i];
+  __builtin_amdgcn_wave_barrier();
+  const char *at = scratch + 8 * grp * kRow + 2 * m;
+#pragma unroll
+  for (int b = 0; b < D / 16; ++b) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = *(const uint16_t *)(at + 2 * i * kRow + 32 * b) |
+             (uint32_t)*(const uint16_t *)(at + (2 * i + 1) * kRow + 32 * b) << 16;
+    x.v[b] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __builtin_amdgcn_wave_barrier();
 }
 
 // nvalid: keys of the tile that count (may be 0 or less).
@@ -223,13 +239,17 @@ __device__ __forceinline__ void compute_tile(const Tile<D> &x, int nvalid, const
     st.o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x.v[b]), pf, st.o[b], 0, 0, 0);
 }
 
-// Wave w of W: blocks w, w + W, ...; own tiles from the other end. Its state to LDS:
-// o [cols][D], m and l [cols].
+// A wave's share of a unit: own tiles (before the selection, which they do not wait for), then
+// blocks w, w + W, ... of those taken, then its state to LDS (o [cols][D], m and l [cols]).
+template <typename T, int D>
+struct Attention;
+
 template <int D>
-__device__ __forceinline__ void attend(const Unit &u, const uint16_t *q, int cols, int w, int W, int lane, float sc,
-                                       char *, float *o_out, float *m_out, float *l_out) {
+struct Attention<uint16_t, D> {
   bf16x8 qf[D / 32];
-  {
+  State<D> st;
+
+  __device__ __forceinline__ void start(const uint16_t *q, int cols, int lane, char *) {
     const int col = lane & 15;
     const uint4 *row = (const uint4 *)(q + min(col, cols - 1) * D);
 #pragma unroll
@@ -238,81 +258,93 @@ __device__ __forceinline__ void attend(const Unit &u, const uint16_t *q, int col
       if (col >= cols) x = make_uint4(0, 0, 0, 0);
       qf[s] = as_bf16x8(x);
     }
-  }
-  State<D> st;
 #pragma unroll
-  for (int b = 0; b < D / 16; ++b) st.o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  st.m = -INFINITY;
-  st.l = 0.f;
-  Tile<D> ta, tb;
-  const char *k = nullptr, *v = nullptr;
-  int n = 0;
-  auto block = [&](int i) {
-    k = uniform(u.k[i]);
-    v = uniform(u.v[i]);
-    n = __builtin_amdgcn_readfirstlane(u.n[i]);
-  };
-  if (w < u.taken) {
-    block(w);
-    load_tile<D>(k, v, 0, lane, true, ta);
+    for (int b = 0; b < D / 16; ++b) st.o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st.m = -INFINITY;
+    st.l = 0.f;
   }
-  for (int t = W - 1 - w; t * kT < u.own; t += W) {
-    load_own<D>(u, t * kT, u.own - 1, lane, tb);
-    compute_tile<D>(tb, u.own - t * kT, qf, st, lane, sc);
-  }
-  // (no branch around the loads: the compiler would wait for all of them where the paths meet)
-  for (int i = w; i < u.taken; i += W) {
-    load_tile<D>(k, v, 1, lane, n > kT, tb);
-    const int n0 = n;
-    compute_tile<D>(ta, n0, qf, st, lane, sc);
-    const bool more = i + W < u.taken;
-    if (more) block(i + W);
-    load_tile<D>(k, v, 0, lane, more, ta);
-    if (n0 > kT) compute_tile<D>(tb, n0 - kT, qf, st, lane, sc);
-  }
-  const float l = col_sum(st.l);
-  const int col = lane & 15, r4 = 4 * (lane >> 4);
-  __syncthreads();                      // the lists are done with
-  if (col < cols) {
-#pragma unroll
-    for (int b = 0; b < D / 16; ++b) *(f32x4 *)(o_out + col * D + 16 * b + r4) = st.o[b];
-    if (lane < 16) {
-      m_out[col] = partial_max(st.m, l);
-      l_out[col] = l;
+  __device__ __forceinline__ void own(const Unit &u, int w, int W, int lane, float sc, char *lds) {
+    for (int t = W - 1 - w; t * kT < u.own; t += W) {
+      Tile<D> x;
+      load_own<D>(u, t * kT, u.own - 1, lane, lds + (w % kWaves) * own_scratch<uint16_t, D>(), x);
+      compute_tile<D>(x, u.own - t * kT, qf, st, lane, sc);
     }
   }
-}
-
-// ---- fp32 attention on the vector ALU, up to 4 columns
-
-template <int D>
-__device__ __forceinline__ void attend(const Unit &u, const float *q, int cols, int w, int W, int lane, float sc,
-                                       char *extra, float *o_out, float *m_out, float *l_out) {
-  constexpr int C = 4, E = D / 64;
-  float *qs = (float *)extra;           // [4][D] (filled by the caller)
-  float *ps = qs + C * D + (w % kWaves) * C * 64;
-  float o[C][E], m[C], l[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    m[c] = -INFINITY;
-    l[c] = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[c][e] = 0.f;
+  __device__ __forceinline__ void blocks(const Unit &u, int w, int W, int lane, float sc) {
+    Tile<D> ta, tb;
+    const char *k = nullptr, *v = nullptr;
+    int n = 0;
+    auto block = [&](int i) {
+      k = uniform(u.k[i]);
+      v = uniform(u.v[i]);
+      n = __builtin_amdgcn_readfirstlane(u.n[i]);
+    };
+    if (w < u.taken) {
+      block(w);
+      load_tile<D>(k, v, 0, lane, true, ta);
+    }
+    // (no branch around the loads: the compiler would wait for all of them where the paths meet)
+    for (int i = w; i < u.taken; i += W) {
+      load_tile<D>(k, v, 1, lane, n > kT, tb);
+      const int n0 = n;
+      compute_tile<D>(ta, n0, qf, st, lane, sc);
+      const bool more = i + W < u.taken;
+      if (more) block(i + W);
+      load_tile<D>(k, v, 0, lane, more, ta);
+      if (n0 > kT) compute_tile<D>(tb, n0 - kT, qf, st, lane, sc);
+    }
   }
-  // scores of 64 keys, a lane one (its row at `row`), and their probabilities to LDS
-  auto scores = [&](const float *row, int n) {
+  __device__ __forceinline__ void store(int cols, int lane, float *o, float *m, float *l) {
+    const float sum = col_sum(st.l);
+    const int col = lane & 15, r4 = 4 * (lane >> 4);
+    if (col >= cols) return;
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) *(f32x4 *)(o + col * D + 16 * b + r4) = st.o[b];
+    if (lane < 16) {
+      m[col] = partial_max(st.m, sum);
+      l[col] = sum;
+    }
+  }
+};
+
+// fp32 on the vector ALU, up to 4 columns.
+template <int D>
+struct Attention<float, D> {
+  static constexpr int C = 4, E = D / 64;
+  const float *qs;                      // LDS: [4][D]
+  float *ps;                            // LDS: this wave's probabilities, [4][64]
+  float o[C][E], m[C], l[C];
+
+  __device__ __forceinline__ void start(const float *, int, int, char *extra) {
+    qs = (const float *)extra;
+    ps = (float *)extra + C * D + (threadIdx.x >> 6) * C * 64;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      m[c] = -INFINITY;
+      l[c] = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[c][e] = 0.f;
+    }
+  }
+  // scores of n keys, a lane one (its row at `row`), and their probabilities to LDS
+  __device__ __forceinline__ void scores(const float *row, int n, int lane, float sc) {
     float s[C] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kAhead = 8;           // 16-byte pieces of the row in flight
+#pragma unroll 1
+    for (int x0 = 0; x0 < D / 4; x0 += kAhead) {
+      float4 k4[kAhead];
 #pragma unroll
-    for (int x = 0; x < D / 4; ++x) {
-      const float4 k4 = ((const float4 *)row)[x];
+      for (int x = 0; x < kAhead; ++x) k4[x] = ((const float4 *)row)[x0 + x];
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const float4 q4 = ((const float4 *)(qs + c * D))[x];
-        s[c] = __builtin_fmaf(k4.x, q4.x, s[c]);
-        s[c] = __builtin_fmaf(k4.y, q4.y, s[c]);
-        s[c] = __builtin_fmaf(k4.z, q4.z, s[c]);
-        s[c] = __builtin_fmaf(k4.w, q4.w, s[c]);
-      }
+      for (int x = 0; x < kAhead; ++x)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const float4 q4 = ((const float4 *)(qs + c * D))[x0 + x];
+          s[c] = __builtin_fmaf(k4[x].x, q4.x, s[c]);
+          s[c] = __builtin_fmaf(k4[x].y, q4.y, s[c]);
+          s[c] = __builtin_fmaf(k4[x].z, q4.z, s[c]);
+          s[c] = __builtin_fmaf(k4[x].w, q4.w, s[c]);
+        }
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -327,60 +359,67 @@ __device__ __forceinline__ void attend(const Unit &u, const float *q, int cols, 
       ps[c * 64 + lane] = p;
     }
     __builtin_amdgcn_wave_barrier();
-  };
-  for (int i = w; i < u.taken; i += W) {
-    const char *k = uniform(u.k[i]), *v = uniform(u.v[i]);
-    const int n = __builtin_amdgcn_readfirstlane(u.n[i]);
-    scores((const float *)k + lane * D, n);        // (rows past the last are there, cleared)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {                  // panels of 32 tokens
-      if (h * kPanel >= n) break;
-#pragma unroll
-      for (int x = 0; x < kPanel / 4; ++x) {
-        float4 p4[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) p4[c] = ((const float4 *)(ps + c * 64 + h * kPanel))[x];
+  }
+  __device__ __forceinline__ void own(const Unit &u, int w, int W, int lane, float sc, char *) {
+    for (int t = W - 1 - w; t * 64 < u.own; t += W) {
+      const int n = min(64, u.own - t * 64);
+      scores((const float *)(u.k_own + (t * 64 + min(lane, n - 1)) * u.own_stride), n, lane, sc);
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) {
+        const float *v = (const float *)(u.v_own + (int64_t)(t * 64 + j) * u.own_stride);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float4 v4 = ((const float4 *)((const float *)v + (h * D + lane + 64 * e) * kPanel))[x];
+          const float x = v[lane + 64 * e];
 #pragma unroll
-          for (int c = 0; c < C; ++c) {
-            o[c][e] = __builtin_fmaf(p4[c].x, v4.x, o[c][e]);
-            o[c][e] = __builtin_fmaf(p4[c].y, v4.y, o[c][e]);
-            o[c][e] = __builtin_fmaf(p4[c].z, v4.z, o[c][e]);
-            o[c][e] = __builtin_fmaf(p4[c].w, v4.w, o[c][e]);
-          }
+          for (int c = 0; c < C; ++c) o[c][e] = __builtin_fmaf(ps[c * 64 + j], x, o[c][e]);
         }
       }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
   }
-  for (int t = W - 1 - w; t * 64 < u.own; t += W) {
-    const int n = min(64, u.own - t * 64);
-    scores((const float *)(u.k_own + (t * 64 + min(lane, n - 1)) * u.own_stride), n);
-    for (int j = 0; j < n; ++j) {
-      const float *v = (const float *)(u.v_own + (int64_t)(t * 64 + j) * u.own_stride);
+  __device__ __forceinline__ void blocks(const Unit &u, int w, int W, int lane, float sc) {
+    for (int i = w; i < u.taken; i += W) {
+      const char *k = uniform(u.k[i]), *v = uniform(u.v[i]);
+      const int n = __builtin_amdgcn_readfirstlane(u.n[i]);
+      scores((const float *)k + lane * D, n, lane, sc);      // (rows past the last are there, cleared)
+#pragma unroll 1
+      for (int h = 0; h * kPanel < n; ++h) {                 // panels of 32 tokens
+        const float4 *vh = (const float4 *)((const float *)v + (h * D + lane) * kPanel);
+        float4 v4[E][kPanel / 4];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float x = v[lane + 64 * e];
+        for (int e = 0; e < E; ++e)
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c][e] = __builtin_fmaf(ps[c * 64 + j], x, o[c][e]);
+          for (int x = 0; x < kPanel / 4; ++x) v4[e][x] = vh[e * 64 * (kPanel / 4) + x];
+#pragma unroll
+        for (int x = 0; x < kPanel / 4; ++x)
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const float4 p4 = ((const float4 *)(ps + c * 64 + h * kPanel))[x];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              o[c][e] = __builtin_fmaf(p4.x, v4[e][x].x, o[c][e]);
+              o[c][e] = __builtin_fmaf(p4.y, v4[e][x].y, o[c][e]);
+              o[c][e] = __builtin_fmaf(p4.z, v4[e][x].z, o[c][e]);
+              o[c][e] = __builtin_fmaf(p4.w, v4[e][x].w, o[c][e]);
+            }
+          }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  __device__ __forceinline__ void store(int cols, int lane, float *o_out, float *m_out, float *l_out) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (c >= cols) break;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o_out[c * D + lane + 64 * e] = o[c][e];
+      if (lane == 0) {
+        m_out[c] = partial_max(m[c], l[c]);
+        l_out[c] = l[c];
       }
     }
-    __builtin_amdgcn_wave_barrier();
   }
-  __syncthreads();
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if (c >= cols) break;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o_out[c * D + lane + 64 * e] = o[c][e];
-    if (lane == 0) {
-      m_out[c] = partial_max(m[c], l[c]);
-      l_out[c] = l[c];
-    }
-  }
-}
+};
 
 // ---- scores and selection
 
@@ -398,7 +437,7 @@ __device__ __forceinline__ void score_blocks(const SparseParams &p, const T *q, 
     for (int h = 0; h < 4; ++h)
 #pragma unroll
       for (int i = 0; i < 8; ++i) qd[h][i] = (double)to_float(q[min(h0 + h, p.group - 1) * D + sub * 8 + i]);
-    constexpr int kAhead = 4;                            // summaries in flight
+    constexpr int kAhead = 8;                            // summaries in flight
     for (int b0 = wave * kRows; b0 < n; b0 += kWaves * kRows * kAhead) {
       uint4 c[kAhead];
 #pragma unroll
@@ -406,6 +445,7 @@ __device__ __forceinline__ void score_blocks(const SparseParams &p, const T *q, 
         c[a] = *(const uint4 *)(base + (int64_t)page[min(b0 + a * kWaves * kRows + rr, n - 1)] * row_bytes);
 #pragma unroll
       for (int a = 0; a < kAhead; ++a) {
+        if (b0 + a * kWaves * kRows >= n) break;
         const int b = b0 + a * kWaves * kRows + rr;
         const double x[8] = {bf16_lo(c[a].x), bf16_hi(c[a].x), bf16_lo(c[a].y), bf16_hi(c[a].y),
                              bf16_lo(c[a].z), bf16_hi(c[a].z), bf16_lo(c[a].w), bf16_hi(c[a].w)};
@@ -520,12 +560,34 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   const int kvh = x % p.n_kv_heads, tok = p.token0 + x / p.n_kv_heads;
   const SparseToken R = tokens[tok];
   const int n = R.blocks, take = min(n, p.n_blocks);
-  const Layout at = layout_of<T, D>(p.most_blocks, p.n_blocks, p.cols);
+  const Layout at = layout_of<T, D>(p.most_blocks, p.n_blocks, p.cols, p.k_self != nullptr);
   int32_t *page = (int32_t *)(lds + at.page);
   uint16_t *link = (uint16_t *)(lds + at.link);
   uint64_t *sel_k = (uint64_t *)(lds + at.sel_k), *sel_v = (uint64_t *)(lds + at.sel_v);
   int32_t *sel_n = (int32_t *)(lds + at.sel_n);
   const T *q = (const T *)p.q + ((int64_t)tok * p.n_q_heads + kvh * p.group) * D;
+
+  const int col0 = cb * kCols, cols = min(kCols, p.group - col0);
+  const int w = split * kWaves + wave, W = p.splits * kWaves;
+  Unit u;
+  u.k = sel_k;
+  u.v = sel_v;
+  u.n = sel_n;
+  u.taken = take;
+  u.own_stride = (int64_t)p.n_kv_heads * D * (int)sizeof(T);
+  const int64_t own_at = R.s0 * u.own_stride + kvh * D * (int)sizeof(T);
+  u.k_own = (const char *)p.k_self + own_at;
+  u.v_own = (const char *)p.v_self + own_at;
+  u.own = R.own;
+  Attention<T, D> att;
+  att.start(q + col0 * D, cols, lane, lds + at.extra);
+  if (sizeof(T) == 4) {
+    for (int i = threadIdx.x; i < kCols * D; i += kThreads)
+      ((float *)(lds + at.extra))[i] = i < cols * D ? to_float(q[col0 * D + i]) : 0.f;
+    __syncthreads();
+  }
+  att.own(u, w, W, lane, p.scale_log2, lds);
+  if (sizeof(T) == 2 && u.own > 0) __syncthreads();
 
   // every block's page and link: a wave loads 64 links at once, then walks them
   links += R.link0;
@@ -562,26 +624,12 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   if (taken)
     for (int i = take + (int)threadIdx.x; i < p.n_blocks; i += kThreads) taken[i] = -1;
 
-  const int col0 = cb * kCols, cols = min(kCols, p.group - col0);
-  q += col0 * D;
-  if (sizeof(T) == 4)
-    for (int i = threadIdx.x; i < kCols * D; i += kThreads)
-      ((float *)(lds + at.extra))[i] = i < cols * D ? to_float(q[i]) : 0.f;
   __syncthreads();
-  Unit u;
-  u.k = sel_k;
-  u.v = sel_v;
-  u.n = sel_n;
-  u.taken = take;
-  u.own_stride = (int64_t)p.n_kv_heads * D * (int)sizeof(T);
-  const int64_t own_at = R.s0 * u.own_stride + kvh * D * (int)sizeof(T);
-  u.k_own = (const char *)p.k_self + own_at;
-  u.v_own = (const char *)p.v_self + own_at;
-  u.own = R.own;
+  att.blocks(u, w, W, lane, p.scale_log2);
+  __syncthreads();                      // the lists are done with
   const int stride = p.cols;            // columns of a wave's state
   float *o = (float *)lds, *m = o + kWaves * stride * D, *l = m + kWaves * stride;
-  attend<D>(u, q, cols, split * kWaves + wave, p.splits * kWaves, lane, p.scale_log2, lds + at.extra,
-            o + wave * stride * D, m + wave * stride, l + wave * stride);
+  att.store(cols, lane, o + wave * stride * D, m + wave * stride, l + wave * stride);
   __syncthreads();
 
   // the waves' states merged: a thread 4 dims of a column
@@ -641,7 +689,7 @@ hipError_t launch_sparse_t(SparseParams p, const SparseTabs *tabs, hipStream_t s
   constexpr int kCols = sizeof(T) == 4 ? 4 : 16;
   p.col_blocks = (p.group + kCols - 1) / kCols;
   p.cols = std::min(kCols, p.group);
-  const size_t lds = layout_of<T, D>(p.most_blocks, p.n_blocks, p.cols).bytes;
+  const size_t lds = layout_of<T, D>(p.most_blocks, p.n_blocks, p.cols, p.k_self != nullptr).bytes;
   const void *f = tabs ? (const void *)link_sparse_tabs_kernel<T, D> : (const void *)link_sparse_kernel<T, D>;
   hipError_t e = hipSuccess;
   if (lds > 64 * 1024) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

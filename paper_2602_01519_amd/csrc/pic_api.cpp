@@ -1793,9 +1793,12 @@ pic_status shared_link_call(pic_store *s, const pic_link_req *req, const pic_lin
 }
 
 // Workgroups that share a unit (query token x kv head) of `taken` blocks: as many as the CUs
-// have room for, where each wave of one would take more than two blocks.
+// have room for, down to a block a wave. Few CUs do not draw on all of HBM: one request of 24
+// blocks, 32/8 heads x 128, in 1 / 3 workgroups a unit 34 / 26 us, of 96 in 1 / 4 / 12 100 / 48 /
+// 37; 4 requests of 96 in 1 / 8 108 / 52. More than the CUs hold at once lose (12 requests of
+// 64 in 2 / 3 66 / 95), as each scores and selects for itself.
 int32_t sparse_splits(int32_t cus, int64_t units, int32_t taken) {
-  const int32_t most = taken / (2 * sparse_waves());
+  const int32_t most = (taken + sparse_waves() - 1) / sparse_waves();
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, cus / std::max<int64_t>(1, units)));
 }
 
@@ -3067,51 +3070,45 @@ pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_he
     if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
     const hipStream_t st = (hipStream_t)stream;
     const size_t off_t = round_up(sizeof(SparseLink) * links.size(), 256);
-    const size_t off_m = off_t + round_up(sizeof(SparseToken) * tq, 256);
-    const size_t bytes = off_m + (p.splits > 1 ? round_up(sizeof(MergeEntry) * B, 256) : 0);
-    const bool by_arg = p.splits == 1 && links.size() <= (size_t)kSparseTabLinks && tq <= kSparseTabTokens;
-    std::pair<hipEvent_t, hipEvent_t> ev{nullptr, nullptr};
-    if (by_arg) {
-      SparseTabs t{};
-      std::copy(links.begin(), links.end(), t.links);
-      std::copy(tokens.begin(), tokens.end(), t.tokens);
-      prof_start(st, &ev);
-      const hipError_t e = launch_link_sparse(p, &t, d.dtype, d.d_k, st);
-      prof_stop(st, &ev, "link_sparse_tabs_kernel");
-      HIP_TRY(e, "link_sparse_tabs_kernel");
-      return PIC_OK;
-    }
-    Stage *stage = nullptr;
+    const size_t bytes = off_t + round_up(sizeof(SparseToken) * tq, 256);
     const int64_t rows = (int64_t)tq * n_q_heads;
-    rc = stage_acquire(s, bytes, &stage);
-    if (rc == PIC_OK && p.splits > 1) rc = ensure_work(stage, (size_t)rows * p.splits * (d.d_v + 2) * sizeof(float));
-    if (rc != PIC_OK) return rc;
-    char *h = (char *)stage->host, *dev = (char *)stage->dev;
-    if (!links.empty()) memcpy(h, links.data(), sizeof(SparseLink) * links.size());
-    memcpy(h + off_t, tokens.data(), sizeof(SparseToken) * tq);
-    int32_t most_rows = 0;
-    for (int32_t r = 0; p.splits > 1 && r < B; ++r) {
-      const int32_t row0 = P.reqs[r].q0 * n_q_heads, n = P.reqs[r].lq * n_q_heads;
-      ((MergeEntry *)(h + off_m))[r] = MergeEntry{row0, n, {row0, 0}, {(int32_t)rows, 0}, {p.splits, 0}};
-      most_rows = std::max(most_rows, n);
+    const size_t part_bytes = p.splits > 1 ? (size_t)rows * p.splits * (d.d_v + 2) * sizeof(float) : 0;
+    const bool by_arg = links.size() <= (size_t)kSparseTabLinks && tq <= kSparseTabTokens;
+    // (a call in one piece whose tables are kernel arguments needs no memory of the store's)
+    Stage *stage = nullptr;
+    if (!by_arg || part_bytes > 0) {
+      rc = stage_acquire(s, by_arg ? 0 : bytes, &stage);
+      if (rc == PIC_OK && part_bytes > 0) rc = ensure_work(stage, part_bytes);
+      if (rc != PIC_OK) return rc;
+      if (p.splits > 1) p.part = place_partials((char *)stage->work, rows * p.splits, d.d_v);
     }
-    HIP_TRY(launch_table_copy(stage->host_dev, dev, (int64_t)bytes, st), "table_copy_kernel");
-    p.links = (const SparseLink *)dev;
-    p.tokens = (const SparseToken *)(dev + off_t);
-    if (p.splits > 1) p.part = place_partials((char *)stage->work, rows * p.splits, d.d_v);
+    SparseTabs tabs;
+    if (by_arg) {
+      std::copy(links.begin(), links.end(), tabs.links);
+      std::copy(tokens.begin(), tokens.end(), tabs.tokens);
+    } else {
+      char *h = (char *)stage->host, *dev = (char *)stage->dev;
+      if (!links.empty()) memcpy(h, links.data(), sizeof(SparseLink) * links.size());
+      memcpy(h + off_t, tokens.data(), sizeof(SparseToken) * tq);
+      HIP_TRY(launch_table_copy(stage->host_dev, dev, (int64_t)bytes, st), "table_copy_kernel");
+      p.links = (const SparseLink *)dev;
+      p.tokens = (const SparseToken *)(dev + off_t);
+    }
+    std::pair<hipEvent_t, hipEvent_t> ev{nullptr, nullptr};
     prof_start(st, &ev);
-    const hipError_t e = launch_link_sparse(p, nullptr, d.dtype, d.d_k, st);
+    const hipError_t e = launch_link_sparse(p, by_arg ? &tabs : nullptr, d.dtype, d.d_k, st);
     prof_stop(st, &ev, "link_sparse_kernel");
     HIP_TRY(e, "link_sparse_kernel");
     if (p.splits > 1) {
       MergeParams m{};
-      m.entries = (const MergeEntry *)(dev + off_m);
+      m.one = MergeEntry{0, (int32_t)rows, {0, 0}, {(int32_t)rows, 0}, {p.splits, 0}};
       m.src[0] = m.src[1] = p.part;
       m.out = out;
       m.lse = lse;
       m.d_v = d.d_v;
-      HIP_TRY(launch_merge(m, d.dtype, B, most_rows, p.splits, st), "merge_kernel");
+      HIP_TRY(launch_merge(m, d.dtype, 1, (int32_t)rows, p.splits, st), "merge_kernel");
     }
+    if (!stage) return PIC_OK;
     HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");
     stage->pending = true;
     return PIC_OK;

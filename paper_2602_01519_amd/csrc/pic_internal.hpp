@@ -578,7 +578,8 @@ struct Partials {
   float *o, *m, *l;           // [partial row][d_v], [partial row], [partial row]
 };
 struct MergeParams {
-  const MergeEntry *entries;
+  const MergeEntry *entries;  // by request; NULL: `one` alone
+  MergeEntry one;
   Partials src[2];
   void *out;
   float *lse;
