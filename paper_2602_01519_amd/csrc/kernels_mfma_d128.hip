@@ -42,6 +42,8 @@
 // magnitude, so almost every tile skips both the max and the rescale. Row
 // sums are kept per lane half (bf16 dot products of the rounded
 // probabilities, i.e. the weights the PV product uses) and added at the end.
+#include <type_traits>
+
 #include "pic_internal.hpp"
 
 namespace pic {
@@ -242,7 +244,7 @@ __device__ __forceinline__ bool mask_tile(const Ctx &c, f32x16 &s0, f32x16 &s1, 
 // the running max as it stands), O += V^T P^T from vt. In both matrix sections the LDS fragment
 // reads are issued a few MFMAs ahead of their use (scheduling groups), so an
 // MFMA does not wait on the read issued right before it.
-template <bool kLim, int kAux>
+template <bool kLim, int kAux, bool kFull>
 __device__ __forceinline__ void compute_tile(const Ctx &c, const uint4 *kt, const uint4 *vt,
                                              const bf16x8 (&qf)[8], Acc &a, const TileRef &ref,
                                              int lim, const DocLim &dlm, float sc,
@@ -286,6 +288,19 @@ __device__ __forceinline__ void compute_tile(const Ctx &c, const uint4 *kt, cons
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
   auto probs = [&]() {
     const float neg_m = a.m_used == -INFINITY ? 0.f : -a.m_used;
+    if constexpr (kFull) {        // the sums are of the fp32 probabilities
+      float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          const float s = ks == 0 ? s0[x] : ks == 1 ? s0[8 + x] : ks == 2 ? s1[x] : s1[8 + x];
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s, sc, neg_m));
+          pf[ks][x] = (__bf16)e;
+          t[ks] += e;
+        }
+      return (t[0] + t[1]) + (t[2] + t[3]);
+    }
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       pf[0][x] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s0[x], sc, neg_m));
@@ -340,8 +355,8 @@ __device__ __forceinline__ void compute_tile(const Ctx &c, const uint4 *kt, cons
   }
 }
 
-// kStages: tile buffer pairs, 2 or 3 (see the tile loops).
-template <bool kLim, int kStages>
+// kStages: tile buffer pairs, 2 or 3 (see the tile loops). kFull: see LinkParams::full_sums.
+template <bool kLim, int kStages, bool kFull>
 __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void link_mfma_d128_kernel(LinkParams p) {
   __shared__ uint4 sk0[kTile * 16], sk1[kTile * 16];
   __shared__ uint4 sv0[kD * 8], sv1[kD * 8];
@@ -472,7 +487,7 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void link_mfma_d128_kernel
     for (int t = t_begin; t < t_end; t += 3) {
       ref2 = t + 2 < t_end ? tile_ref(c, t + 2) : ref1;
       if (active)
-        compute_tile<kLim, kAux>(c, sk0, sv0, qf, a, ref0, lim, dlm, sc, ref2, sk2, sv2);
+        compute_tile<kLim, kAux, kFull>(c, sk0, sv0, qf, a, ref0, lim, dlm, sc, ref2, sk2, sv2);
       else
         issue_tile<kAux>(c, ref2, sk2, sv2);
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopySets) : "memory");
@@ -480,7 +495,7 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void link_mfma_d128_kernel
       if (t + 1 >= t_end) break;
       ref0 = t + 3 < t_end ? tile_ref(c, t + 3) : ref2;
       if (active)
-        compute_tile<kLim, kAux>(c, sk1, sv1, qf, a, ref1, lim, dlm, sc, ref0, sk0, sv0);
+        compute_tile<kLim, kAux, kFull>(c, sk1, sv1, qf, a, ref1, lim, dlm, sc, ref0, sk0, sv0);
       else
         issue_tile<kAux>(c, ref0, sk0, sv0);
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopySets) : "memory");
@@ -488,7 +503,7 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void link_mfma_d128_kernel
       if (t + 2 >= t_end) break;
       ref1 = t + 4 < t_end ? tile_ref(c, t + 4) : ref0;
       if (active)
-        compute_tile<kLim, kAux>(c, sk2, sv2, qf, a, ref2, lim, dlm, sc, ref1, sk1, sv1);
+        compute_tile<kLim, kAux, kFull>(c, sk2, sv2, qf, a, ref2, lim, dlm, sc, ref1, sk1, sv1);
       else
         issue_tile<kAux>(c, ref1, sk1, sv1);
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopySets) : "memory");
@@ -508,7 +523,7 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void link_mfma_d128_kernel
       // tile t in buffers 0; copy tile t+1 into buffers 1
       ref1 = t + 1 < t_end ? tile_ref(c, t + 1) : ref0;
       if (active)
-        compute_tile<kLim, kAux>(c, sk0, sv0, qf, a, ref0, lim, dlm, sc, ref1, sk1, sv1);
+        compute_tile<kLim, kAux, kFull>(c, sk0, sv0, qf, a, ref0, lim, dlm, sc, ref1, sk1, sv1);
       else
         issue_tile<kAux>(c, ref1, sk1, sv1);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -517,7 +532,7 @@ __global__ __launch_bounds__(kWaves * 64, 8 / kWaves) void link_mfma_d128_kernel
       // tile t+1 in buffers 1; copy tile t+2 into buffers 0
       ref0 = t + 2 < t_end ? tile_ref(c, t + 2) : ref1;
       if (active)
-        compute_tile<kLim, kAux>(c, sk1, sv1, qf, a, ref1, lim, dlm, sc, ref0, sk0, sv0);
+        compute_tile<kLim, kAux, kFull>(c, sk1, sv1, qf, a, ref1, lim, dlm, sc, ref0, sk0, sv0);
       else
         issue_tile<kAux>(c, ref0, sk0, sv0);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -566,17 +581,26 @@ hipError_t launch_link_mfma_d128(const LinkParams &p, hipStream_t st, const char
   // questions: few busy waves, short tiles) are bound by the latency of the
   // tile copies and get the three-stage loop; the others the two-stage one.
   const dim3 block(kWaves * 64);
-  if (p.max_rows < kRows) {
-    if (p.doc_lim)
-      hipLaunchKernelGGL((link_mfma_d128_kernel<true, 3>), grid, block, 0, st, p);
+  const auto go = [&](auto lim, auto stages, auto full) {
+    constexpr bool kLim = decltype(lim)::value, kFull = decltype(full)::value;
+    hipLaunchKernelGGL((link_mfma_d128_kernel<kLim, decltype(stages)::value, kFull>), grid, block, 0, st, p);
+  };
+  const auto by_sums = [&](auto lim, auto stages) {
+    if (p.full_sums)
+      go(lim, stages, std::true_type());
     else
-      hipLaunchKernelGGL((link_mfma_d128_kernel<false, 3>), grid, block, 0, st, p);
-  } else {
-    if (p.doc_lim)
-      hipLaunchKernelGGL((link_mfma_d128_kernel<true, 2>), grid, block, 0, st, p);
+      go(lim, stages, std::false_type());
+  };
+  const auto by_stages = [&](auto lim) {
+    if (p.max_rows < kRows)
+      by_sums(lim, std::integral_constant<int, 3>());
     else
-      hipLaunchKernelGGL((link_mfma_d128_kernel<false, 2>), grid, block, 0, st, p);
-  }
+      by_sums(lim, std::integral_constant<int, 2>());
+  };
+  if (p.doc_lim)
+    by_stages(std::true_type());
+  else
+    by_stages(std::false_type());
   return hipGetLastError();
 }
 

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeParams p) {
 }
 
 template <typename T, int kLanes, int kChunks>
-hipError_t launch_merge_t(MergeParams p, int32_t batch, int32_t max_rows, int32_t pieces, hipStream_t st) {
+hipError_t launch_merge_t(MergeParams p, int32_t batch, int32_t max_rows, int32_t rows, int32_t pieces, hipStream_t st) {
   auto go = [&](auto kg) {
     constexpr int kGpr = decltype(kg)::value;
     const int per = 256 / kLanes / kGpr;
@@ -176,26 +176,31 @@ hipError_t launch_merge_t(MergeParams p, int32_t batch, int32_t max_rows, int32_
     }
     return hipGetLastError();
   };
-  if (pieces <= 4) return go(std::integral_constant<int, 1>());
-  if (pieces <= 8) return go(std::integral_constant<int, 2>());
-  return go(std::integral_constant<int, 4>());
+  // One pass of each group over its pieces, as far as the rows leave room for it: about two
+  // thousand workgroups run at once.
+  const auto room = [&](int gpr) { return (int64_t)rows * kLanes * gpr <= (int64_t)256 * 2048; };
+  if constexpr (kLanes < 64)
+    if (pieces > 16 && room(8)) return go(std::integral_constant<int, 8>());
+  if (pieces > 8 && room(4)) return go(std::integral_constant<int, 4>());
+  if (pieces > 4 && room(2)) return go(std::integral_constant<int, 2>());
+  return go(std::integral_constant<int, 1>());
 }
 
 template <typename T>
-hipError_t launch_merge_w(const MergeParams &p, int32_t batch, int32_t max_rows, int32_t pieces, hipStream_t st) {
-  if (p.d_v <= 64) return launch_merge_t<T, 16, 1>(p, batch, max_rows, pieces, st);
-  if (p.d_v <= 128) return launch_merge_t<T, 32, 1>(p, batch, max_rows, pieces, st);
-  if (p.d_v <= 512) return launch_merge_t<T, 64, 2>(p, batch, max_rows, pieces, st);
-  return launch_merge_t<T, 64, 4>(p, batch, max_rows, pieces, st);
+hipError_t launch_merge_w(const MergeParams &p, int32_t batch, int32_t max_rows, int32_t rows, int32_t pieces, hipStream_t st) {
+  if (p.d_v <= 64) return launch_merge_t<T, 16, 1>(p, batch, max_rows, rows, pieces, st);
+  if (p.d_v <= 128) return launch_merge_t<T, 32, 1>(p, batch, max_rows, rows, pieces, st);
+  if (p.d_v <= 512) return launch_merge_t<T, 64, 2>(p, batch, max_rows, rows, pieces, st);
+  return launch_merge_t<T, 64, 4>(p, batch, max_rows, rows, pieces, st);
 }
 
 }  // namespace
 
-hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows, int32_t pieces,
-                        hipStream_t st) {
+hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows, int32_t rows,
+                        int32_t pieces, hipStream_t st) {
   if (batch <= 0 || max_rows <= 0) return hipSuccess;
-  return dtype == 0 ? launch_merge_w<float>(p, batch, max_rows, pieces, st)
-                    : launch_merge_w<uint16_t>(p, batch, max_rows, pieces, st);
+  return dtype == 0 ? launch_merge_w<float>(p, batch, max_rows, rows, pieces, st)
+                    : launch_merge_w<uint16_t>(p, batch, max_rows, rows, pieces, st);
 }
 
 }  // namespace pic

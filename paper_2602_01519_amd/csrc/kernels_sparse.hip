@@ -33,7 +33,6 @@ namespace pic {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
@@ -226,14 +225,16 @@ __device__ __forceinline__ void compute_tile(const Tile<D> &x, int nvalid, const
   }
   const float neg = st.m == -INFINITY ? 0.f : -st.m;
   bf16x8 pf;                            // rounded to bf16 for the value product, 2^-9 of each
+  float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    pf[i] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s0[i], sc, neg));
-    pf[4 + i] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s1[i], sc, neg));
+    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[i], sc, neg));
+    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s1[i], sc, neg));
+    pf[i] = (__bf16)p0;
+    pf[4 + i] = (__bf16)p1;
+    sum += p0 + p1;
   }
-  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-  for (int i = 0; i < 8; i += 2) st.l = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[i], pf[i + 1]}, ones, st.l, false);
+  st.l += sum;
 #pragma unroll
   for (int b = 0; b < D / 16; ++b)
     st.o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x.v[b]), pf, st.o[b], 0, 0, 0);

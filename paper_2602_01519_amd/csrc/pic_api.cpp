@@ -649,7 +649,7 @@ void prof_stop(hipStream_t st, std::pair<hipEvent_t, hipEvent_t> *ev, const char
 }
 
 enum class Mode { Prefill, Decode };
-enum class Kern { Valu, Mfma128, Decode128, Mla, Stream, Fp4, Fp4Prefill };
+enum class Kern { Valu, Mfma128, Decode128, Mla, Stream, Fp4, Fp4Prefill, Shared128 };
 
 // Everything about a call that does not depend on its tensors: the resolved
 // tables, the kernel, the split count and the workspace layout
@@ -665,6 +665,7 @@ struct Setup {
   // every row's softmax state goes to the partials, also of a request in one piece; the
   // caller sets lp.part_* and merges them
   bool partial = false;
+  bool shared = false;           // groups that share links, for the shared kernel
   bool lean = false;             // a small call the lean kernel runs
   bool small = false;            // tables as a kernel argument, own KV in place
   int32_t rows_per_block = 0;    // rows of a workgroup (decode kernel: wave)
@@ -1022,6 +1023,31 @@ bool fp4_few_rows(const Plan &P, const pic_store_desc &d, int group, int cus) {
   return tiles <= (int64_t)cus * (d.d_k == 128 ? 12 : 24);
 }
 
+// Times of a CU in the shared kernel: for a 64-key tile of a block of 256 rows (of 128: half of
+// it), for the start and end of a block, and for a 32-key tile of its waves' units (eight at a time).
+constexpr double kSharedTileUs = 2.3, kSharedBlockUs = 8, kSharedUnitTileUs = 0.6;
+
+// Work of the groups' blocks and of the requests' units in the shared kernel, in CU x us.
+struct SharedWork {
+  double groups, units;
+};
+SharedWork shared_work(const Plan &groups, const Plan &requests, const pic_store_desc &d, int group, int32_t cus) {
+  const int rows = shared_d128_rows_per_block(groups.max_rows);
+  SharedWork w{(double)cus * kSharedBlockUs, 0};     // (about a block a CU)
+  for (const ReqEntry &R : groups.reqs)
+    w.groups += d.n_kv_heads * kSharedTileUs * rows / 256 * R.tiles * (((int64_t)R.lq * group + rows - 1) / rows);
+  for (const ReqEntry &R : requests.reqs)
+    if (R.lq > 0) w.units += d.n_kv_heads * kSharedUnitTileUs * 2 * R.tiles;
+  return w;
+}
+
+// Calls that the shared kernel takes: those of up to this time on the whole GPU. One launch
+// starts and ends once and mixes the two parts, but each has to do with its share of the CUs: 8
+// requests over 6 links of 200..900 15 us, in a launch each 20; 64 over 16 links of 1024 46, 54;
+// four groups of 4 over 10 links 41, 47; but 8 groups of 8 over 12 links 108, 78; two of 100 over 16
+// links 104, 98; four of 30..60 over 40..64 links 350, 323.
+constexpr double kSharedMostUs = 40;
+
 // Costs of a kernel's pieces in its tiles (see choose_splits). Tile times on
 // a full GPU: d128 1.75 us per workgroup (64 keys), MLA 2.0 us (64 keys),
 // decode 5 us per wave (32 keys, eight waves per CU on the HBM stream),
@@ -1030,7 +1056,7 @@ bool fp4_few_rows(const Plan &P, const pic_store_desc &d, int group, int cus) {
 // uneven_rows: some request has fewer row blocks than another. units: the call's
 // workgroups before any split.
 SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t max_rows,
-                     const StreamShape &ss, bool uneven_rows, int64_t units) {
+                     int32_t rows_per_block, const StreamShape &ss, bool uneven_rows, int64_t units) {
   const double part_us = (d.d_v + 2) * 8.0 / 4e6;
   SplitCost c{};
   c.max_splits = 256;
@@ -1044,6 +1070,11 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     const int64_t part = 2 * (int64_t)std::min(max_rows, mfma_d128_rows_per_block()) * (d.d_v + 2) * 4;
     const int64_t tile = (int64_t)kTile * (d.d_k + d.d_v) * 2;
     c.min_piece = (int32_t)std::max<int64_t>(1, std::min<int64_t>(8, part / tile));
+  } else if (kern == Kern::Shared128) {
+    us = kSharedTileUs * rows_per_block / 256;
+    c.slots = cus;
+    c.over = kSharedBlockUs / us;
+    c.min_piece = 2;
   } else if (kern == Kern::Mla) {
     us = 2.0;
     c.slots = cus;
@@ -1101,7 +1132,8 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
   // some of them: an eighth stays free (12 fp32 requests of 20..130 tokens:
   // 77 us with a twentieth free, 64 us with a tenth or more; 8 bf16 requests
   // of 30..300 tokens, 64-wide heads: 168 us full, 147 us).
-  c.fit = uneven_rows ? c.slots * 7 / 8 : c.slots;
+  // (The blocks of groups that share links are listed one by one: none is empty.)
+  c.fit = uneven_rows && kern != Kern::Shared128 ? c.slots * 7 / 8 : c.slots;
   c.part = part_us / us;
   c.fixed = 4.5 / us;
   return c;
@@ -1245,30 +1277,81 @@ size_t noalloc_charge(const pic_store *s, const Setup &C, int32_t num_splits) {
          round_up(sizeof(int32_t) * P.doc_lim.size(), 256) + round_up(P.own_bytes, 256) + part;
 }
 
-pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, float scale,
-                      int32_t layer, int32_t num_splits, Mode mode, Setup &C) {
-  if (mode == Mode::Decode && (num_splits < 0 || num_splits > 256))
-    return fail(PIC_ERR_INVALID, "num_splits must be 0..256");
+// Cuts the requests of a call of work items into pieces (given: num_splits each), for a GPU of
+// `cus` compute units.
+pic_status split_items(pic_store *s, int32_t n_q_heads, int32_t num_splits, Mode mode, const StreamShape &ss,
+                       int32_t cus, Setup &C) {
   Plan &P = C.P;
-  pic_status rc = plan_call(s, req, n_q_heads, scale, layer,
-                            mode == Mode::Decode ? 16 : INT32_MAX, P);
-  if (rc != PIC_OK) return rc;
+  LinkParams &lp = C.lp;
+  const pic_store_desc &d = s->desc;
+  const Kern kern = C.kern;
+  const int rows_per_block = C.rows_per_block, B = (int)P.reqs.size();
+  C.tile_keys = kern == Kern::Decode128 || kern == Kern::Stream ? 32 : kTile;
+  std::vector<int32_t> tiles(B), blocks(B);
+  std::vector<int64_t> rows(B);
+  std::vector<double> share(B, 1.0);
+  bool uneven_rows = false;
+  for (int r = 0; r < B; ++r) {
+    const ReqEntry &R = P.reqs[r];
+    tiles[r] = R.tiles * (kTile / C.tile_keys);
+    blocks[r] = d.n_kv_heads * ((R.lq * lp.group + rows_per_block - 1) / rows_per_block);
+    rows[r] = (int64_t)R.lq * n_q_heads;
+    uneven_rows |= blocks[r] != d.n_kv_heads * lp.nrb;
+    // d128 row blocks end at the farthest limit of their rows: count the
+    // part of the tiles they walk. (The few-row 4-bit kernel's end there, too, but
+    // its pieces are cheaper than the more of them that this gives: one request of 30
+    // tokens over 110 tiles 16 us, counted 22; 8 of them over 66 36, 39.)
+    if ((kern == Kern::Mfma128 || kern == Kern::Fp4Prefill) && !P.doc_lim.empty() && R.ls == 0 &&
+        R.nlinks > 0) {
+      const LinkEntry &last = P.links[R.link0 + R.nlinks - 1];
+      share[r] = limit_share(P, R, lp.group, rows_per_block, last.tok0 + last.len);
+    }
+  }
+  // (the combine of 64-wide rows reads every partial)
+  lp.skip_empty = (kern == Kern::Mfma128 || (kern == Kern::Fp4Prefill && d.d_v == 128)) &&
+                  !P.doc_lim.empty();
+  const bool given = mode == Mode::Decode && num_splits > 0;
+  if (given)
+    C.req_splits.assign(B, num_splits);
+  else
+    C.req_splits = choose_splits(tiles, blocks, rows, share,
+                                 split_cost(kern, cus, d, P.max_rows, rows_per_block, ss, uneven_rows,
+                                            std::accumulate(blocks.begin(), blocks.end(), int64_t{0})));
+  apply_splits(s, n_q_heads, rows_per_block, C);
+  while (!given && C.part_bytes > kMostPartBytes && C.splits > 1) fewer_pieces(s, n_q_heads, C);
+  // A decode call that the no-alloc entry takes (by its charge) fits its
+  // scratch, also where uneven requests are cut into more pieces than the
+  // charge counts or the work items need more than its slack. Cut here, for
+  // both entries, so that their results are the same.
+  if (mode == Mode::Decode && !C.partial && noalloc_charge(s, C, num_splits) <= kStaticScratchBytes)
+    while (table_layout(C).bytes + C.work_bytes() > kStaticScratchBytes + kStaticScratchSlack &&
+           C.splits > 1)
+      fewer_pieces(s, n_q_heads, C);
+  if (launch_items(C) < 1) return fail(PIC_ERR_UNSUPPORTED, "too many query rows for one launch");
+  return PIC_OK;
+}
+
+// Kernel, pieces and workspace of a planned call (C.P).
+pic_status setup_planned(pic_store *s, int32_t n_q_heads, int32_t num_splits, Mode mode, Setup &C) {
+  Plan &P = C.P;
   const pic_store_desc &d = s->desc;
   const bool mla = d.kind == PIC_MLA;
   const bool fp4 = is_fp4(d);
   LinkParams &lp = C.lp;
-  lp.batch = req->batch;
+  const int32_t batch = (int32_t)P.reqs.size();
+  lp.batch = batch;
   lp.n_q_heads = n_q_heads;
   lp.n_kv_heads = d.n_kv_heads;
   lp.group = n_q_heads / d.n_kv_heads;
   lp.d_k = d.d_k;
   lp.d_v = d.d_v;
   lp.total_q = P.total_q;
-  if (req->batch == 0 || P.total_q == 0) return PIC_OK;
-  if (P.max_own_lp > 0 && req->batch <= kOwnArgs) {
-    C.own_args.assign(req->batch, OwnArg{0, 0, 0});
+  lp.full_sums = C.partial;
+  if (batch == 0 || P.total_q == 0) return PIC_OK;
+  if (P.max_own_lp > 0 && batch <= kOwnArgs) {
+    C.own_args.assign(batch, OwnArg{0, 0, 0});
     size_t k = 0;
-    for (int32_t r = 0; r < req->batch; ++r) {
+    for (int32_t r = 0; r < batch; ++r) {
       const ReqEntry &R = P.reqs[r];
       if (R.ls == 0) continue;
       C.own_args[r] = OwnArg{R.s0, R.ls, P.own[k++].second};
@@ -1290,6 +1373,7 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   // rows of one request that see different numbers of linked rows need the
   // per-row masks of the flash kernel
   if (kern == Kern::Decode128 && !P.doc_lim.empty()) kern = Kern::Mfma128;
+  if (C.shared) kern = Kern::Shared128;
   if (d.dtype == PIC_BF16 && mla && d.d_k == 576 && d.d_v == 512) kern = Kern::Mla;
   if (fp4) kern = fp4_few_rows(P, d, lp.group, s->shape.cus) ? Kern::Fp4 : Kern::Fp4Prefill;
   // A small generic call of a shape the lean kernel is built for (tables as
@@ -1322,63 +1406,18 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
                              : kern == Kern::Mla   ? mla_rows_per_block()
                              : kern == Kern::Fp4   ? fp4_rows_per_block(P.max_rows)
                              : kern == Kern::Fp4Prefill ? fp4_prefill_rows_per_block()
+                             : kern == Kern::Shared128 ? shared_d128_rows_per_block(P.max_rows)
                                                    : decode_d128_max_rows();
   C.rows_per_block = rows_per_block;
   lp.nrb = std::max(1, (P.max_rows + rows_per_block - 1) / rows_per_block);
   lp.max_rows = P.max_rows;
-  lp.n_groups = req->batch * d.n_kv_heads;
+  lp.n_groups = batch * d.n_kv_heads;
   lp.n_xcd = s->shape.xcds;
 
-  const bool by_items = kern != Kern::Valu && !C.small;
-  if (by_items) {
-    C.tile_keys = kern == Kern::Decode128 || kern == Kern::Stream ? 32 : kTile;
-    const int B = req->batch;
-    std::vector<int32_t> tiles(B), blocks(B);
-    std::vector<int64_t> rows(B);
-    std::vector<double> share(B, 1.0);
-    bool uneven_rows = false;
-    for (int r = 0; r < B; ++r) {
-      const ReqEntry &R = P.reqs[r];
-      tiles[r] = R.tiles * (kTile / C.tile_keys);
-      blocks[r] = d.n_kv_heads * ((R.lq * lp.group + rows_per_block - 1) / rows_per_block);
-      rows[r] = (int64_t)R.lq * n_q_heads;
-      uneven_rows |= blocks[r] != d.n_kv_heads * lp.nrb;
-      // d128 row blocks end at the farthest limit of their rows: count the
-      // part of the tiles they walk. (The few-row 4-bit kernel's end there, too, but
-      // its pieces are cheaper than the more of them that this gives: one request of 30
-      // tokens over 110 tiles 16 us, counted 22; 8 of them over 66 36, 39.)
-      if ((kern == Kern::Mfma128 || kern == Kern::Fp4Prefill) && !P.doc_lim.empty() && R.ls == 0 &&
-          R.nlinks > 0) {
-        const LinkEntry &last = P.links[R.link0 + R.nlinks - 1];
-        share[r] = limit_share(P, R, lp.group, rows_per_block, last.tok0 + last.len);
-      }
-    }
-    // (the combine of 64-wide rows reads every partial)
-    lp.skip_empty = (kern == Kern::Mfma128 || (kern == Kern::Fp4Prefill && d.d_v == 128)) &&
-                    !P.doc_lim.empty();
-    const bool given = mode == Mode::Decode && num_splits > 0;
-    if (given)
-      C.req_splits.assign(B, num_splits);
-    else
-      C.req_splits = choose_splits(tiles, blocks, rows, share,
-                                   split_cost(kern, s->shape.cus, d, P.max_rows, ss, uneven_rows,
-                                              std::accumulate(blocks.begin(), blocks.end(), int64_t{0})));
-    apply_splits(s, n_q_heads, rows_per_block, C);
-    while (!given && C.part_bytes > kMostPartBytes && C.splits > 1) fewer_pieces(s, n_q_heads, C);
-    // A decode call that the no-alloc entry takes (by its charge) fits its
-    // scratch, also where uneven requests are cut into more pieces than the
-    // charge counts or the work items need more than its slack. Cut here, for
-    // both entries, so that their results are the same.
-    if (mode == Mode::Decode && !C.partial && noalloc_charge(s, C, num_splits) <= kStaticScratchBytes)
-      while (table_layout(C).bytes + C.work_bytes() > kStaticScratchBytes + kStaticScratchSlack &&
-             C.splits > 1)
-        fewer_pieces(s, n_q_heads, C);
-    if (launch_items(C) < 1) return fail(PIC_ERR_UNSUPPORTED, "too many query rows for one launch");
-    return PIC_OK;
-  }
+  if (kern != Kern::Valu && !C.small) return split_items(s, n_q_heads, num_splits, mode, ss, s->shape.cus, C);
 
   int32_t splits = 1;
-  const int64_t blocks = (int64_t)req->batch * d.n_kv_heads * lp.nrb;
+  const int64_t blocks = (int64_t)batch * d.n_kv_heads * lp.nrb;
   if (mode == Mode::Decode) {
     if (num_splits > 0) {
       splits = num_splits;
@@ -1417,9 +1456,18 @@ pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, 
   C.part_off = round_up(P.own_bytes, 256);
   C.part_bytes = (size_t)C.part_rows * (d.d_v + 2) * sizeof(float);
   // (a small call is one launch; the pieces of the vector-ALU kernel are its second dimension)
-  if (launch_items(C) < (!C.small ? 1 : (int64_t)req->batch * (kern == Kern::Stream ? splits : 1)))
+  if (launch_items(C) < (!C.small ? 1 : (int64_t)batch * (kern == Kern::Stream ? splits : 1)))
     return fail(PIC_ERR_UNSUPPORTED, "too many query rows for one launch");
   return PIC_OK;
+}
+
+pic_status setup_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, float scale,
+                      int32_t layer, int32_t num_splits, Mode mode, Setup &C) {
+  if (mode == Mode::Decode && (num_splits < 0 || num_splits > 256))
+    return fail(PIC_ERR_INVALID, "num_splits must be 0..256");
+  const pic_status rc = plan_call(s, req, n_q_heads, scale, layer,
+                                  mode == Mode::Decode ? 16 : INT32_MAX, C.P);
+  return rc != PIC_OK ? rc : setup_planned(s, n_q_heads, num_splits, mode, C);
 }
 
 // Whether a 4-bit call's tables go as a kernel argument: few items and links, no limits,
@@ -1635,13 +1683,59 @@ pic_status link_call(pic_store *s, const pic_link_req *req, int32_t n_q_heads, c
 // of their partials. Tables: [groups' tables][requests' tables][merge entries]; workspace: the
 // requests' own KV laid out, then the partials of both.
 struct SharedCall {
-  Setup pre, own;
+  Setup pre, own;                              // joined: own holds both, the groups first
+  bool joined = false;
+  int32_t most_rows = 0;                       // most output rows of a request
   std::vector<MergeEntry> merge;
   bool has_pre = false, has_own = false;       // some request sees a key there
   TableLayout t_pre{}, t_own{};
-  size_t off_own = 0, off_merge = 0, table_bytes = 0, work_bytes = 0;
+  std::vector<std::pair<int32_t, int32_t>> blocks;   // kernels_shared_d128.hip: pre's item, row block
+  size_t off_own = 0, off_merge = 0, off_blocks = 0, table_bytes = 0, work_bytes = 0;
   int32_t pieces = 1;                          // most pieces of a row
+  int32_t unit_wgs = 0;                        // workgroups for own's units
+
+  // pre and own in one launch of the shared kernel
+  bool one_launch() const { return has_pre && pre.shared; }
 };
+
+// Whether both calls run one kernel in one shape, which takes items of either.
+bool joinable(const Setup &a, const Setup &b) {
+  return a.kern == b.kern && a.kern != Kern::Valu && a.kern != Kern::Shared128 &&
+         a.rows_per_block == b.rows_per_block && a.lp.kpar == b.lp.kpar && a.P.doc_lim.empty() && b.P.doc_lim.empty();
+}
+
+// Puts the requests of `pre` (no own KV) before those of `own`, in one call: one launch, cut for the
+// GPU as a whole (3 groups of 3..9 questions of 5..60 tokens, 24/6 heads x 64, 68.7 -> 57.3 us).
+pic_status join_calls(pic_store *s, int32_t n_q_heads, Setup &pre, Setup &own) {
+  Plan P = std::move(pre.P);
+  const Plan &Q = own.P;
+  const int32_t links = (int32_t)P.links.size(), reqs = (int32_t)P.reqs.size();
+  P.links.insert(P.links.end(), Q.links.begin(), Q.links.end());
+  for (ReqEntry R : Q.reqs) {
+    R.link0 += links;
+    P.reqs.push_back(R);
+  }
+  for (const auto &o : Q.own) {
+    P.own.emplace_back(o.first + links, o.second);
+    P.max_own_lp = std::max(P.max_own_lp, Q.links[o.first].lp);
+  }
+  for (int32_t r : Q.order) P.order.push_back(r + reqs);
+  std::stable_sort(P.order.begin(), P.order.end(), [&](int32_t a, int32_t b) {
+    return (int64_t)P.reqs[a].tiles * P.reqs[a].lq > (int64_t)P.reqs[b].tiles * P.reqs[b].lq;
+  });
+  P.ids.insert(P.ids.end(), Q.ids.begin(), Q.ids.end());
+  P.own_bytes = Q.own_bytes;
+  P.max_rows = std::max(P.max_rows, Q.max_rows);
+  P.max_tiles = std::max(P.max_tiles, Q.max_tiles);
+  P.self = Q.self;
+  P.total_self = Q.total_self;
+  const Mode mode = own.kern == Kern::Decode128 ? Mode::Decode : Mode::Prefill;
+  pre = Setup{};
+  own = Setup{};
+  own.partial = true;
+  own.P = std::move(P);
+  return setup_planned(s, n_q_heads, 0, mode, own);
+}
 
 pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_groups *groups,
                         int32_t n_q_heads, float scale, int32_t layer, SharedCall &S) {
@@ -1668,10 +1762,36 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
   S.pre.partial = S.own.partial = true;
   pic_status rc = setup_call(s, req, n_q_heads, scale, layer, 0, most_q <= 16 ? Mode::Decode : Mode::Prefill, S.own);
   if (rc != PIC_OK) return rc;
-  rc = setup_call(s, &pr, n_q_heads, scale, layer, 0, most_group_q <= 16 ? Mode::Decode : Mode::Prefill, S.pre);
+  rc = plan_call(s, &pr, n_q_heads, scale, layer, INT32_MAX, S.pre.P);
+  if (rc != PIC_OK) return rc;
+  const int32_t cus = s->shape.cus;
+  const int group = n_q_heads / s->desc.n_kv_heads;
+  SharedWork work{0, 0};
+  if (S.own.kern == Kern::Decode128 && S.own.P.max_tiles > 0 && S.pre.P.max_rows > decode_d128_max_rows()) {
+    work = shared_work(S.pre.P, S.own.P, s->desc, group, cus);
+    S.pre.shared = work.groups + work.units <= cus * kSharedMostUs;
+  }
+  rc = setup_planned(s, n_q_heads, 0, most_group_q <= 16 ? Mode::Decode : Mode::Prefill, S.pre);
   if (rc != PIC_OK) return rc;
   S.has_pre = S.pre.P.max_tiles > 0;
   S.has_own = S.own.P.max_tiles > 0;
+  S.most_rows = S.own.P.max_rows * s->desc.n_kv_heads;
+  if (S.has_pre && S.has_own && joinable(S.pre, S.own)) {
+    rc = join_calls(s, n_q_heads, S.pre, S.own);
+    if (rc != PIC_OK) return rc;
+    S.joined = true;
+    S.has_pre = false;
+  }
+  if (S.one_launch()) {
+    // each part gets CUs by its share of the work, and is cut for those
+    const double share = work.units / (work.groups + work.units);
+    S.unit_wgs = std::max(1, std::min(cus - 1, (int32_t)std::lround(cus * share)));
+    const StreamShape none{0, 1, 4};
+    rc = split_items(s, n_q_heads, 0, Mode::Decode, none, S.unit_wgs, S.own);
+    if (rc == PIC_OK) rc = split_items(s, n_q_heads, 0, Mode::Prefill, none, cus - S.unit_wgs, S.pre);
+    if (rc != PIC_OK) return rc;
+    S.unit_wgs = std::min(S.unit_wgs, (S.own.n_items * s->desc.n_kv_heads + shared_d128_waves() - 1) / shared_d128_waves());
+  }
   S.merge.resize(B);
   const auto source = [](const Setup &C, int32_t r, int32_t row, MergeEntry &m, int x) {
     if (C.kern == Kern::Valu) {                  // pieces of all rows one after another
@@ -1688,19 +1808,35 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
     for (int32_t r = groups->request_offsets[g]; r < groups->request_offsets[g + 1]; ++r) {
       MergeEntry &m = S.merge[r];
       m = MergeEntry{};
-      const ReqEntry &R = S.own.P.reqs[r];
+      const ReqEntry &R = S.own.P.reqs[S.joined ? G + r : r];
       m.row0 = R.q0 * n_q_heads;
       m.rows = R.lq * n_q_heads;
       if (R.lq == 0) continue;
+      if (S.joined) {
+        source(S.own, g, (R.q0 - group_q[g]) * n_q_heads, m, 0);
+        source(S.own, G + r, 0, m, 1);
+      }
       if (S.has_pre && S.pre.P.reqs[g].tiles > 0) source(S.pre, g, (R.q0 - group_q[g]) * n_q_heads, m, 0);
-      if (S.has_own && R.tiles > 0) source(S.own, r, 0, m, 1);
+      if (!S.joined && S.has_own && R.tiles > 0) source(S.own, r, 0, m, 1);
       S.pieces = std::max(S.pieces, m.splits[0] + m.splits[1]);
     }
+  if (S.one_launch()) {
+    // (in the items' order; a row block's other heads follow it)
+    int32_t item = 0;
+    for (int32_t g : S.pre.P.order) {
+      const int32_t rows = S.pre.P.reqs[g].lq * S.pre.lp.group;
+      for (int32_t i = 0; i < S.pre.req_splits[g]; ++i, ++item)
+        for (int32_t rb = 0; rb * S.pre.rows_per_block < rows; ++rb) S.blocks.emplace_back(item, rb);
+    }
+    if ((int64_t)S.blocks.size() * S.pre.lp.n_kv_heads > kMostBlocks)
+      return fail(PIC_ERR_UNSUPPORTED, "too many query rows for one launch");
+  }
   S.t_pre = table_layout(S.pre);
   S.t_own = table_layout(S.own);
   S.off_own = S.t_pre.bytes;
   S.off_merge = S.off_own + S.t_own.bytes;
-  S.table_bytes = S.off_merge + round_up(sizeof(MergeEntry) * B, 256);
+  S.off_blocks = S.off_merge + round_up(sizeof(MergeEntry) * B, 256);
+  S.table_bytes = S.off_blocks + round_up(sizeof(SharedBlock) * S.blocks.size(), 256);
   S.work_bytes = S.own.part_off + round_up(S.own.part_bytes, 256) + S.pre.part_bytes;
   return PIC_OK;
 }
@@ -1709,6 +1845,8 @@ void write_shared_tables(const SharedCall &S, const LinkEntry *pre_links, const 
   write_tables(S.pre, S.t_pre, pre_links, h);
   write_tables(S.own, S.t_own, own_links, h + S.off_own);
   memcpy(h + S.off_merge, S.merge.data(), sizeof(MergeEntry) * S.merge.size());
+  SharedBlock *b = (SharedBlock *)(h + S.off_blocks);
+  for (const auto &x : S.blocks) *b++ = SharedBlock{((const WorkItem *)(h + S.t_pre.off_i))[x.first], x.second};
 }
 
 Partials place_partials(char *at, int64_t rows, int32_t d_v) {
@@ -1728,21 +1866,23 @@ pic_status launch_shared(const pic_store *s, const SharedCall &S, char *dev, con
   m.entries = (const MergeEntry *)(dev + S.off_merge);
   char *parts = work + S.own.part_off;
   m.src[1] = place_partials(parts, S.own.part_rows, d_v);
-  m.src[0] = place_partials(parts + round_up(S.own.part_bytes, 256), S.pre.part_rows, d_v);
+  m.src[0] = S.joined ? m.src[1]
+                      : place_partials(parts + round_up(S.own.part_bytes, 256), S.pre.part_rows, d_v);
   m.out = out;
   m.lse = lse;
   m.d_v = d_v;
   m.sparse = S.own.lp.skip_empty;
-  const auto run = [&](const Setup &C, const TableLayout &t, size_t off, const Partials &to, const Prologue &pro,
-                       const void *ks, const void *vs) {
+  const auto params = [&](const Setup &C, const TableLayout &t, size_t off, const Partials &to) {
     LinkParams lp = C.lp;
     point_tables(C, t, dev + off, lp);
     lp.part_o = to.o;
     lp.part_m = to.m;
     lp.part_l = to.l;
-    return launch_call(s, C, lp, work, pro, q, ks, vs, scale, out, lse, st);
+    return lp;
   };
-  if (S.has_own) {
+  const LinkParams lp_pre = params(S.pre, S.t_pre, 0, m.src[0]);
+  const LinkParams lp_own = params(S.own, S.t_own, S.off_own, m.src[1]);
+  if (S.has_own && !S.one_launch()) {
     Prologue pro;
     const char *tables = host_dev ? host_dev : dev;
     pro.links = (const LinkEntry *)(tables + S.off_own);
@@ -1752,17 +1892,36 @@ pic_status launch_shared(const pic_store *s, const SharedCall &S, char *dev, con
       pro.copy_dst = dev;
       pro.copy_bytes = (int64_t)S.table_bytes;
     }
-    const pic_status rc = run(S.own, S.t_own, S.off_own, m.src[1], pro, k_self, v_self);
+    const pic_status rc = launch_call(s, S.own, lp_own, work, pro, q, k_self, v_self, scale, out, lse, st);
     if (rc != PIC_OK) return rc;
   } else if (host_dev) {
     HIP_TRY(launch_table_copy(host_dev, dev, (int64_t)S.table_bytes, st), "table_copy_kernel");
   }
-  if (S.has_pre) {
-    const pic_status rc = run(S.pre, S.t_pre, 0, m.src[0], Prologue{}, nullptr, nullptr);
+  if (S.one_launch()) {
+    SharedParams sp{};
+    sp.pre = lp_pre;
+    sp.own = lp_own;
+    for (LinkParams *lp : {&sp.pre, &sp.own}) {
+      lp->q = q;
+      lp->k_self = k_self;
+      lp->v_self = v_self;
+      lp->scale_log2 = scale * 1.4426950408889634f;
+    }
+    sp.blocks = (const SharedBlock *)(dev + S.off_blocks);
+    sp.n_blocks = (int32_t)S.blocks.size();
+    sp.n_units = S.own.n_items * s->desc.n_kv_heads;
+    sp.unit_wgs = S.unit_wgs;
+    std::pair<hipEvent_t, hipEvent_t> ev{nullptr, nullptr};
+    prof_start(st, &ev);
+    const hipError_t e = launch_link_shared_d128(sp, st);
+    prof_stop(st, &ev, "link_shared_d128_kernel");
+    HIP_TRY(e, "link_shared_d128_kernel");
+  } else if (S.has_pre) {
+    const pic_status rc = launch_call(s, S.pre, lp_pre, work, Prologue{}, q, nullptr, nullptr, scale, out, lse, st);
     if (rc != PIC_OK) return rc;
   }
-  HIP_TRY(launch_merge(m, io_dtype(s->desc), (int32_t)S.merge.size(),
-                       S.own.P.max_rows * s->desc.n_kv_heads, S.pieces, st), "merge_kernel");
+  HIP_TRY(launch_merge(m, io_dtype(s->desc), (int32_t)S.merge.size(), S.most_rows,
+                       S.own.P.total_q * S.own.lp.n_q_heads, S.pieces, st), "merge_kernel");
   return PIC_OK;
 }
 
@@ -3106,7 +3265,7 @@ pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_he
       m.out = out;
       m.lse = lse;
       m.d_v = d.d_v;
-      HIP_TRY(launch_merge(m, d.dtype, 1, (int32_t)rows, p.splits, st), "merge_kernel");
+      HIP_TRY(launch_merge(m, d.dtype, 1, (int32_t)rows, (int32_t)rows, p.splits, st), "merge_kernel");
     }
     if (!stage) return PIC_OK;
     HIP_TRY(hipEventRecord(stage->done, st), "hipEventRecord(stage)");

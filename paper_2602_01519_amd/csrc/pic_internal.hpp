@@ -126,6 +126,9 @@ struct LinkParams {
   int32_t even;           // all requests have as many tiles, rows and pieces
   int32_t gang;           // MLA kernel: consecutive row blocks on one XCD (planned: its CUs)
   int32_t kpar;           // stream kernel: key parts within a workgroup (1, 2 or 4)
+  // bf16 128-wide kernels: row sums of the fp32 probabilities, for a log-sum-exp as exact as
+  // fp32 (else of their bf16 roundings, which the value products take)
+  int32_t full_sums;
   float scale_log2;       // softmax_scale * log2(e)
 };
 
@@ -587,9 +590,27 @@ struct MergeParams {
   int32_t sparse;             // values of pieces that hold no key may be unwritten
   int32_t blocks;             // workgroups of a request (set by launch_merge)
 };
-// max_rows, pieces: most rows and pieces of an entry
+// max_rows, pieces: most rows and pieces of an entry; rows: of all
 hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows,
-                        int32_t pieces, hipStream_t st);
+                        int32_t rows, int32_t pieces, hipStream_t st);
+
+// bf16 GQA link attention of requests that share links, d_k = d_v = 128, to partials: row blocks
+// of the groups' pieces (pre), and units (item x kv head, at most 16 rows) of the requests' own
+// links and KV (own; n_units 0: none).
+struct alignas(16) SharedBlock {
+  WorkItem item;              // one of pre's (here too: a read less before the first key)
+  int32_t rb;                 // row block
+};
+struct SharedParams {
+  LinkParams pre, own;        // items, links, tensors and part_* set
+  const SharedBlock *blocks;
+  int32_t n_blocks, n_units;
+  int32_t unit_wgs;           // workgroups for the units (0 if none)
+};
+static_assert(sizeof(SharedParams) <= 4064, "kernel arguments");
+int shared_d128_waves();
+int shared_d128_rows_per_block(int max_rows);
+hipError_t launch_link_shared_d128(const SharedParams &p, hipStream_t st);
 
 // Link attention over selected blocks (kernels_sparse.hip). A request's blocks are the 64-token
 // tiles of its links, in order.
