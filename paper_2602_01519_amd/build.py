@@ -31,7 +31,7 @@ SOURCES = [
     "kernels_rope.hip",
     "kernels_append.hip",
     "kernels_shared.hip",
-    "kernels_shared_d128.hip",
+    "kernels_shared_mfma.hip",
     "kernels_sparse.hip",
     "static_scratch.hip",
 ]

@@ -1,27 +1,28 @@
-// bf16 GQA link attention of requests that share links, head dim 128: the shared rows of every
-// group, and the requests' own, in one launch of partials (merge_kernel joins them).
+// bf16 GQA link attention of requests that share links, head dim 128 or 64, on the matrix cores:
+// row blocks of pieces of keys, to partials (merge_kernel joins them).
 //
-// The first walk has hundreds of query rows per key (a group's query tokens x the heads of a kv
-// head) and is bound by the matrix cores, the second a few rows per key and is bound by HBM. The
-// planner divides the CUs between them: some workgroups' waves take the requests' pieces one
-// after another, the others a block of a group's rows and keys each.
-//
-// Block: 256 or 128 rows of one (group's piece of keys, kv head). 256: 8 waves of 32 rows, each over
-// whole 64-key tiles; 128: 4 groups of 32 rows x 2 halves of each tile, whose (m, l, O) merge
-// through LDS at the end.
-//   S^T[64 (32) keys][32 rows] = K . Q^T    16 (8) x v_mfma_f32_32x32x16_bf16
-//   O^T[128][32 rows]         += V^T . P^T  16 (8) x v_mfma_f32_32x32x16_bf16
-// A tile takes a CU 2.1 us at 256 rows (1000 TFLOP/s on all of them, the rate of
+// Block: 256 or 128 rows (query token x head of the group) of one (item, kv head), an item a piece of
+// the keys of a group of requests, of 64-wide heads also of one request with its own KV. 256: 8
+// waves of 32 rows, each over whole 64-key tiles; 128: 4 groups of 32 rows x 2 halves of each tile,
+// whose (m, l, O) merge through LDS at the end.
+//   S^T[64 (32) keys][32 rows] = K . Q^T    D / 8 (D / 16) x v_mfma_f32_32x32x16_bf16
+//   O^T[D][32 rows]           += V^T . P^T  the same
+// The tiles' LDS layout, the key order of the scores and the softmax are link_mfma_d128_kernel's:
+// probabilities against the running max as it stands, a tile done again against its own max where
+// a sum passes 2^64 or the row has no max yet. The row sums are of the fp32 probabilities.
+// 128 wide, a tile takes a CU 2.1 us at 256 rows (1000 TFLOP/s on all of them, the rate of
 // link_mfma_d128_kernel) and 1.05 at 128, which groups of no more rows take. Larger groups in blocks
 // of 128 would be cut into half as many pieces, with half the partials, but read each key once
-// more: 64 requests x 32/8 heads over 16 links of 1024 50.8 us, in blocks of 256 45.9. The tiles'
-// LDS layout, the key order of the scores and the softmax are link_mfma_d128_kernel's:
-// probabilities against the running max as it stands, a tile done again against its own max where
-// a sum passes 2^64 or the row has no max yet.
+// more: 64 requests x 32/8 heads over 16 links of 1024 50.8 us, in blocks of 256 45.9. 64-wide heads
+// have half the products beside the same exponentials: 1.2 us a tile of 256 rows (895 TFLOP/s).
 //
-// Tiles are copied global -> LDS three ahead of their use (four buffers of 32 KB): keys that come
-// from HBM arrive 2 us after their copies are issued, four tiles' products. The own rows of a
-// request, read in place, turn through LDS (decode_d128.hpp).
+// Tiles are copied global -> LDS three ahead of their use (four buffers): keys that come from HBM
+// arrive 2 us after their copies are issued, four tiles' products.
+//
+// 128-wide heads, single tokens: the requests' own links and KV have a few rows per key and are
+// bound by HBM where the groups' blocks are bound by the matrix cores. Both go in one launch: the
+// planner divides the CUs, some workgroups' waves take the requests' pieces one after another
+// (decode_d128.hpp; own rows are read in place and turn through LDS), the others a block each.
 #include "decode_d128.hpp"
 
 namespace pic {
@@ -31,23 +32,31 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void *lds_ptr;
 
-constexpr int kD = 128;
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kRowsPerWave = 32;
 template <bool kWide>
 constexpr int kRows = kWide ? 256 : 128;        // of a block
 constexpr int kBuffers = 4;                     // tiles in LDS
-constexpr int kUnits = 1024;                    // 16-byte units of a K (or V) tile
+template <int D>
+constexpr int kUnits = kTile * D / 8;           // 16-byte units of a K (or V) tile
+template <int D>
+constexpr int kSets = D / 64;                   // copies a lane of each
 constexpr float kJumpSum = 18446744073709551616.0f;   // 2^64
-static_assert(kWaves * decode_d128::kOwnScratch <= kBuffers * 2 * kUnits * 16, "LDS");
+static_assert(kWaves * decode_d128::kOwnScratch <= kBuffers * 2 * kUnits<128> * 16, "LDS");
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8, u); }
 
-// LDS tiles in 16-byte units, swizzled within each row (see link_mfma_d128_kernel): K [key][16
-// units of 8 dims], V^T [dv][8 units of 8 keys].
+// LDS tiles in 16-byte units, swizzled within each row (see link_mfma_d128_kernel): K [key][D / 8
+// units of 8 dims], V^T [dv][8 units of 8 keys]. Rows of 8 units lie two to a 256-byte bank row: the
+// 16 rows that a group of lanes reads, {0-3, 8-11, 4-7, 12-15}, take every unit of both.
 __device__ __forceinline__ int hk(int key) { return (key & 3) | ((key & 8) >> 1) | ((key & 4) << 1); }
 __device__ __forceinline__ int hv(int x) { return (x ^ (x >> 3)) & 7; }
-__device__ __forceinline__ int k_slot(int key, int c) { return key * 16 + (c ^ hk(key & 15)); }
+template <int D>
+__device__ __forceinline__ int k_unit(int key, int c) {      // c ^ the row's swizzle
+  return D == 128 ? c ^ hk(key & 15) : c ^ hv(key & 31);
+}
+template <int D>
+__device__ __forceinline__ int k_slot(int key, int c) { return key * (D / 8) + k_unit<D>(key, c); }
 __device__ __forceinline__ int v_slot(int dv, int c) { return dv * 8 + (c ^ hv(dv & 31)); }
 // Key row that feeds M index m: a lane's scores are then 8 consecutive keys, twice.
 __device__ __forceinline__ int key_of_m(int m) {
@@ -66,10 +75,11 @@ __device__ __forceinline__ float half_sum(float x) {
 struct TileRef {
   const char *k, *v;
   int nvalid;
+  int own;                      // 0, or 1 + the first key's index among the own ones
 };
 struct Cursor {
   const_links links;            // from the item's first link on
-  int li, kvh;
+  int li, kvh, doc_tiles;
   const char *k, *v;
   int len, lp, tile0, end;
 };
@@ -81,14 +91,16 @@ __device__ __forceinline__ void cursor_set(Cursor &c, const void *k, const void 
   c.tile0 = tile0;
   c.end = tile0 + (len + kTile - 1) / kTile;
 }
+template <int D>
 __device__ __forceinline__ TileRef tile_ref(Cursor &c, int t) {   // (t only grows)
   while (t >= c.end) {
     ++c.li;
     cursor_set(c, c.links[c.li].k, c.links[c.li].v, c.links[c.li].len, c.links[c.li].lp, c.links[c.li].tile0);
   }
   const int tt = t - c.tile0;
-  return TileRef{c.k + ((int64_t)c.kvh * c.lp + tt * kTile) * kD * 2,
-                 c.v + ((int64_t)c.kvh * kD * c.lp + tt * kTile * kD) * 2, min(kTile, c.len - tt * kTile)};
+  return TileRef{c.k + ((int64_t)c.kvh * c.lp + tt * kTile) * D * 2,
+                 c.v + ((int64_t)c.kvh * D * c.lp + tt * kTile * D) * 2, min(kTile, c.len - tt * kTile),
+                 t >= c.doc_tiles ? 1 + tt * kTile : 0};
 }
 
 template <int kAux>
@@ -98,60 +110,66 @@ __device__ __forceinline__ void copy16(const void *base, uint32_t off, uint4 *ds
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)dst, 16, off, 0, 0, kAux);
 }
 
+template <int D>
 struct Lane {
   int lane, wave, n, g;         // n: row of the wave's 32, g: lane / 32
   int half;                     // (blocks of 128 rows) the wave's half of a tile's keys
-  uint32_t koff[2], voff[2];    // byte offsets of the lane's two K and V units within a tile
+  uint32_t koff[kSets<D>], voff[kSets<D>];      // byte offsets of the lane's K and V units within a tile
 };
 
-// Copy i (0..3) of a tile into a buffer (its K units, then its V units): two of K, two of V.
-template <int kAux>
-__device__ __forceinline__ void tile_copy(const Lane &c, int i, const TileRef &r, uint4 *to) {
-  if (i < 2)
+// Copy i of a tile into a buffer (its K units, then its V units).
+template <int D, int kAux>
+__device__ __forceinline__ void tile_copy(const Lane<D> &c, int i, const TileRef &r, uint4 *to) {
+  constexpr int n = kSets<D>;
+  if (i < n)
     copy16<kAux>(r.k, c.koff[i], to + (i * kWaves + c.wave) * 64);
   else
-    copy16<kAux>(r.v, c.voff[i - 2], to + kUnits + ((i - 2) * kWaves + c.wave) * 64);
+    copy16<kAux>(r.v, c.voff[i - n], to + kUnits<D> + ((i - n) * kWaves + c.wave) * 64);
 }
+
+template <int D>
 struct State {
-  f32x16 o[4];
+  f32x16 o[D / 32];
   float m, l;
 };
 
 // One tile, the copies of a later one spread over its score products. The wave takes kN halves of
-// the tile's keys, from c.half on.
-template <int kN, int kAux>
-__device__ __forceinline__ void compute_tile(const Lane &c, const uint4 *kt, const bf16x8 (&qf)[8], State &a,
-                                             int nvalid, float sc, const TileRef &next, uint4 *to) {
-  const uint4 *vt = kt + kUnits;
-  constexpr int kAhead = 5;                     // K reads run ahead of their products
+// the tile's keys, from c.half on. lim: the last own key that this lane's row sees.
+template <int D, int kN, int kAux>
+__device__ __forceinline__ void compute_tile(const Lane<D> &c, const uint4 *kt, const bf16x8 (&qf)[D / 16], State<D> &a,
+                                             const TileRef &r, int lim, float sc, const TileRef &next, uint4 *to) {
+  const uint4 *vt = kt + kUnits<D>;
+  constexpr int kSteps = D / 16, kAhead = D == 64 ? 4 : 5;   // K reads run ahead of their products
   const int row = 32 * c.half + key_of_m(c.n);
   f32x16 s[kN];
 #pragma unroll
   for (int h = 0; h < kN; ++h)
 #pragma unroll
     for (int x = 0; x < 16; ++x) s[h][x] = 0.f;
-  bf16x8 kf[kN][8];
+  bf16x8 kf[kN][kSteps];
 #pragma unroll
   for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-    for (int h = 0; h < kN; ++h) kf[h][i] = as_bf16x8(kt[k_slot(32 * h + row, i * 2 + c.g)]);
+    for (int h = 0; h < kN; ++h) kf[h][i] = as_bf16x8(kt[k_slot<D>(32 * h + row, i * 2 + c.g)]);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i + kAhead < 8) {
+  for (int i = 0; i < kSteps; ++i) {
+    if (i + kAhead < kSteps) {
 #pragma unroll
       for (int h = 0; h < kN; ++h)
-        kf[h][i + kAhead] = as_bf16x8(kt[k_slot(32 * h + row, (i + kAhead) * 2 + c.g)]);
+        kf[h][i + kAhead] = as_bf16x8(kt[k_slot<D>(32 * h + row, (i + kAhead) * 2 + c.g)]);
     }
-    if (i % 2 == 0) tile_copy<kAux>(c, i / 2, next, to);
+    if (i % 2 == 0) tile_copy<D, kAux>(c, i / 2, next, to);
 #pragma unroll
     for (int h = 0; h < kN; ++h) s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][i], qf[i], s[h], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   }
   // s[h][x]: key 32 (half + h) + (x >> 3) * 16 + g * 8 + (x & 7)
+  constexpr bool kOwn = D == 64;                // (128-wide items are of shared rows alone)
   bool seen = true;
-  if (__builtin_expect(nvalid < kTile, 0)) {
+  if (__builtin_expect(r.nvalid < kTile || (kOwn && r.own), 0)) {
     asm volatile("");             // (a branch: as selects, the masks of whole tiles cost 45 instructions)
-    const int kl = nvalid - 1 - 32 * c.half - 8 * c.g;
+    const int last = kOwn && r.own ? min(lim + 1 - r.own, r.nvalid - 1) : r.nvalid - 1;
+    const int kl = last - 32 * c.half - 8 * c.g;
 #pragma unroll
     for (int h = 0; h < kN; ++h)
 #pragma unroll
@@ -189,7 +207,7 @@ __device__ __forceinline__ void compute_tile(const Lane &c, const uint4 *kt, con
     a.m = mnew;
     a.l *= f;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int x = 0; x < 16; ++x) a.o[d][x] *= f;
     t = probs();
@@ -198,31 +216,32 @@ __device__ __forceinline__ void compute_tile(const Lane &c, const uint4 *kt, con
 #pragma unroll
   for (int k = 0; k < 2 * kN; ++k)
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
+    for (int d = 0; d < D / 32; ++d) {
       const bf16x8 vf = as_bf16x8(vt[v_slot(d * 32 + c.n, (2 * c.half + k) * 2 + c.g)]);
       a.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], a.o[d], 0, 0, 0);
     }
-  constexpr int kLead = 4 * kN;                 // V reads run ahead of their products
+  constexpr int kPv = kN * D / 16, kLead = kPv / 2;   // V reads run ahead of their products
   __builtin_amdgcn_sched_group_barrier(0x100, kLead, 0);
 #pragma unroll
-  for (int i = 0; i < 8 * kN; ++i) {
+  for (int i = 0; i < kPv; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if (i + kLead < 8 * kN) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    if (i + kLead < kPv) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
 }
 
-// After a tile: the next one's copies have landed (those of the two behind it, 4 each, may be in
-// flight), the LDS reads are done, and no access moves across.
+// After a tile: the next one's copies have landed (those of the two behind it may be in flight),
+// the LDS reads are done, and no access moves across.
+template <int D>
 __device__ __forceinline__ void tile_barrier() {
-  asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kSets<D>) : "memory");
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-template <bool kWide, int kAux>
+template <int D, bool kWide, int kAux>
 __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkItem &it, int rb, int kvh, uint4 *lds) {
-  Lane c;
+  Lane<D> c;
   c.lane = threadIdx.x & 63;
   c.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   c.n = c.lane & 31;
@@ -236,44 +255,49 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
   const int qi = rvalid ? row / group : 0, qh = kvh * group + (rvalid ? row % group : 0);
   const int64_t orow = (int64_t)(it.q0 + qi) * p.n_q_heads + qh;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {                 // (load-to-LDS: lane i lands at unit base + i)
+  for (int u = 0; u < kSets<D>; ++u) {          // (load-to-LDS: lane i lands at unit base + i)
     const int s = (u * kWaves + c.wave) * 64 + c.lane;
-    const int key = s >> 4, kc = (s & 15) ^ hk(key & 15);
-    c.koff[u] = (uint32_t)((key * kD + kc * 8) * 2);
+    const int key = s / (D / 8), kc = k_unit<D>(key, s % (D / 8));
+    c.koff[u] = (uint32_t)((key * D + kc * 8) * 2);
     const int dv = s >> 3, cc = (s & 7) ^ hv(dv & 31);
-    c.voff[u] = (uint32_t)((cc >> 2) * kD * kPanel * 2 + dv * kPanel * 2 + (cc & 3) * 16);
+    c.voff[u] = (uint32_t)((cc >> 2) * D * kPanel * 2 + dv * kPanel * 2 + (cc & 3) * 16);
   }
   Cursor cur;
   cur.links = (const_links)p.links + it.link;
   cur.li = 0;
   cur.kvh = kvh;
+  cur.doc_tiles = it.doc_tiles;
   cursor_set(cur, it.k, it.v, it.len, it.lp, it.tile0);
-  const int t0 = it.t_begin, t1 = it.t_end;
+  const int lim = rvalid ? qi + it.ls - it.lq : -1;
+  // own tiles past the causal limit of the block's last row hold no key that it sees
+  const int t0 = it.t_begin;
+  const int t1 = D == 128 ? it.t_end
+                          : min(it.t_end, visible_tiles(item_request(it), (min(nrows, row0 + kRows<kWide>) - 1) / group));
   // (past the last tile the copies repeat it into buffers nobody reads again, which keeps the
   // counts of the waits)
   TileRef r0{}, r1{}, r2{}, r3{};
-  auto tile = [&](int t) { return tile_ref(cur, min(t, t1 - 1)); };
+  auto tile = [&](int t) { return tile_ref<D>(cur, min(t, t1 - 1)); };
   auto issue = [&](const TileRef &r, int i) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tile_copy<kAux>(c, k, r, lds + 2 * kUnits * i);
+    for (int k = 0; k < 2 * kSets<D>; ++k) tile_copy<D, kAux>(c, k, r, lds + 2 * kUnits<D> * i);
   };
   if (t0 < t1) {
     r0 = tile(t0);
     issue(r0, 0);
   }
-  bf16x8 qf[8];
+  bf16x8 qf[D / 16];
   {
-    const uint4 *q = (const uint4 *)((const uint16_t *)p.q + orow * kD);
+    const uint4 *q = (const uint4 *)((const uint16_t *)p.q + orow * D);
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
+    for (int s = 0; s < D / 16; ++s) {
       uint4 v = make_uint4(0, 0, 0, 0);
       if (rvalid) v = q[s * 2 + c.g];
       qf[s] = as_bf16x8(v);
     }
   }
-  State a;
+  State<D> a;
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < D / 32; ++d)
 #pragma unroll
     for (int x = 0; x < 16; ++x) a.o[d][x] = 0.f;
   a.m = -INFINITY;
@@ -290,10 +314,11 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
     // Tile t from buffer i, the copies of tile t + 3 into the one that tile t - 1 left.
     auto step = [&](const TileRef &r, int i, const TileRef &next) {
       if (active)
-        compute_tile<kWide ? 2 : 1, kAux>(c, lds + 2 * kUnits * i, qf, a, r.nvalid, sc, next, lds + 2 * kUnits * ((i + 3) & 3));
+        compute_tile<D, kWide ? 2 : 1, kAux>(c, lds + 2 * kUnits<D> * i, qf, a, r, lim, sc, next,
+                                             lds + 2 * kUnits<D> * ((i + 3) & 3));
       else
         issue(next, (i + 3) & 3);
-      tile_barrier();
+      tile_barrier<D>();
     };
     for (int t = t0; t < t1; t += 4) {
       r3 = tile(t + 3);
@@ -314,11 +339,29 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
 
   const int nvalid = min(kRowsPerWave, nrows - (row0 + rg * kRowsPerWave));
   const int64_t prow = it.part + (orow - (int64_t)it.q0 * p.n_q_heads);
+  // 64 dims of the wave's rows (O^T[dv][row], dv = d * 32 + (x >> 2) * 8 + g * 4 + (x & 3)) leave
+  // through 8 KB of LDS as whole 256-byte pieces
+  auto store = [&](const f32x16 &o0, const f32x16 &o1, float *lds8k, int dim0) {
+    const lds_units units = (lds_units)(uintptr_t)(uint32_t)(uintptr_t)(lds_ptr)lds8k;
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const f32x16 &o = d ? o1 : o0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        units[c.n * 16 + ((8 * d + 2 * j + c.g) ^ (c.n & 15))] = __builtin_bit_cast(
+            u32x4v, (f32x4v){o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]});
+    }
+    store_block_units(units, c.lane, nvalid, (int)prow, (char *)(p.part_o + dim0), D * 4);
+  };
+  float *xo = (float *)lds, *mine = xo + c.wave * 2048;
   if constexpr (kWide) {
     if (!active) return;
     const float sum = half_sum(a.l);
-    const lds_units units = (lds_units)(uintptr_t)(uint32_t)(uintptr_t)(lds_ptr)(lds + c.wave * 512);
-    store_block_f32(a.o[0], a.o[1], a.o[2], a.o[3], units, c.lane, nvalid, (int)prow, p.part_o, kD);
+    if constexpr (D == 128)
+      store_block_f32(a.o[0], a.o[1], a.o[2], a.o[3], (lds_units)(uintptr_t)(uint32_t)(uintptr_t)(lds_ptr)mine, c.lane,
+                      nvalid, (int)prow, p.part_o, D);
+    else
+      store(a.o[0], a.o[1], mine, 0);
     if (rvalid && c.g == 0) {
       p.part_m[prow] = partial_max(a.m, sum);
       p.part_l[prow] = sum;
@@ -327,16 +370,20 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
   }
 
   // The halves of a row group merge: each wave hands over the two 32-dim blocks that the other
-  // writes out (8 KB a wave, same lanes on both sides), and its max and sum behind them.
-  float *xo = (float *)lds, *xm = xo + kWaves * 2048;
+  // writes out (64 wide: the second half all it has; 8 KB a wave, same lanes on both sides), and
+  // its max and sum behind them.
+  float *xm = xo + kWaves * 2048;
   const int other = c.wave ^ 1;
-  float *mine = xo + c.wave * 2048, *theirs = xo + other * 2048;
-  if (active) {
+  const float *theirs = xo + other * 2048;
+  constexpr bool kBoth = D == 128;              // both halves write out
+  const int give = kBoth && !c.half ? 2 : 0, keep = kBoth && c.half ? 2 : 0;
+  const bool gives = active && (kBoth || c.half), keeps = active && (kBoth || !c.half);
+  if (gives) {
 #pragma unroll
     for (int d = 0; d < 2; ++d)
 #pragma unroll
       for (int x = 0; x < 16; x += 4) {
-        const f32x16 &o = c.half ? a.o[d] : a.o[2 + d];
+        const f32x16 &o = kBoth && give ? a.o[(D / 32 - 2) + d] : a.o[d];
         *(float4 *)(mine + ((d * 4 + x / 4) * 64 + c.lane) * 4) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
       }
     xm[c.wave * 128 + c.lane] = a.m;
@@ -345,7 +392,7 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
   __syncthreads();
   f32x16 s0, s1;                                // the wave's 64 dims, merged
   float m = -INFINITY, l = 0.f;
-  if (active) {
+  if (keeps) {
     const float m1 = xm[other * 128 + c.lane], l1 = xm[other * 128 + 64 + c.lane];
     m = fmaxf(a.m, m1);
     const float f0 = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.m - m);
@@ -354,7 +401,7 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
     l = (a.m == -INFINITY ? a.l : a.l * f0) + (m1 == -INFINITY ? l1 : l1 * f1);
 #pragma unroll
     for (int d = 0; d < 2; ++d) {
-      const f32x16 &o = c.half ? a.o[2 + d] : a.o[d];
+      const f32x16 &o = kBoth && keep ? a.o[(D / 32 - 2) + d] : a.o[d];
       f32x16 &to = d ? s1 : s0;
 #pragma unroll
       for (int x = 0; x < 16; x += 4) {
@@ -367,19 +414,8 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
     }
   }
   __syncthreads();                              // the exchange is over: 8 KB of it for each wave
-  if (active) {
-    // O^T[dv][row], dv = d * 32 + (x >> 2) * 8 + g * 4 + (x & 3): 64 dims of 32 rows leave as
-    // whole 256-byte pieces
-    const lds_units units = (lds_units)(uintptr_t)(uint32_t)(uintptr_t)(lds_ptr)mine;
-#pragma unroll
-    for (int d = 0; d < 2; ++d) {
-      const f32x16 &o = d ? s1 : s0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        units[c.n * 16 + ((8 * d + 2 * j + c.g) ^ (c.n & 15))] = __builtin_bit_cast(
-            u32x4v, (f32x4v){o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]});
-    }
-    store_block_units(units, c.lane, nvalid, (int)prow, (char *)(p.part_o + 64 * c.half), kD * 4);
+  if (keeps) {
+    store(s0, s1, mine, 32 * keep);
     const float sum = half_sum(l);
     if (rvalid && c.g == 0 && c.half == 0) {
       p.part_m[prow] = partial_max(m, sum);
@@ -389,10 +425,10 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
 }
 
 // The first unit_wgs workgroups take the wave units, the others a block each.
-template <bool kWide, int kAux>
-__global__ __launch_bounds__(kThreads, 1) void link_shared_d128_kernel(SharedParams p) {
-  __shared__ uint4 lds[kBuffers * 2 * kUnits];
-  if ((int)blockIdx.x < p.unit_wgs) {
+template <int D, bool kWide, int kAux>
+__global__ __launch_bounds__(kThreads, 1) void link_shared_kernel(SharedParams p) {
+  __shared__ uint4 lds[kBuffers * 2 * kUnits<D> + (D == 64 ? 512 : 0)];   // (64 wide: the exchange is larger)
+  if (D == 128 && (int)blockIdx.x < p.unit_wgs) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int u = blockIdx.x + p.unit_wgs * wave; u < p.n_units; u += p.unit_wgs * kWaves)
       decode_d128::wave_unit<true, true>(p.own, u, lane, (char *)lds + wave * decode_d128::kOwnScratch);
@@ -401,24 +437,32 @@ __global__ __launch_bounds__(kThreads, 1) void link_shared_d128_kernel(SharedPar
   const int x = blockIdx.x - p.unit_wgs, b = x / p.pre.n_kv_heads;
   typedef __attribute__((address_space(4))) const SharedBlock *const_blocks;
   const int rb = ((const_blocks)p.blocks + b)->rb;
-  block_partial<kWide, kAux>(p.pre, load_item(&p.blocks[b].item, 0), rb, x - b * p.pre.n_kv_heads, lds);
+  block_partial<D, kWide, kAux>(p.pre, load_item(&p.blocks[b].item, 0), rb, x - b * p.pre.n_kv_heads, lds);
+}
+
+template <int D>
+void launch_shared_t(const SharedParams &p, hipStream_t st) {
+  const dim3 grid((unsigned)(p.unit_wgs + (int64_t)p.n_blocks * p.pre.n_kv_heads)), block(kThreads);
+  // K and V of a block that no other reads need not stay in the caches
+  if (p.pre.max_rows <= kRows<false>)
+    hipLaunchKernelGGL((link_shared_kernel<D, false, 2>), grid, block, 0, st, p);
+  else if (p.pre.nrb == 1)
+    hipLaunchKernelGGL((link_shared_kernel<D, true, 2>), grid, block, 0, st, p);
+  else
+    hipLaunchKernelGGL((link_shared_kernel<D, true, 0>), grid, block, 0, st, p);
 }
 
 }  // namespace
 
-int shared_d128_rows_per_block(int max_rows) { return max_rows > kRows<false> ? kRows<true> : kRows<false>; }
-int shared_d128_waves() { return kWaves; }
+int shared_rows_per_block(int max_rows) { return max_rows > kRows<false> ? kRows<true> : kRows<false>; }
+int shared_waves() { return kWaves; }
 
-hipError_t launch_link_shared_d128(const SharedParams &p, hipStream_t st) {
-  const dim3 grid((unsigned)(p.unit_wgs + (int64_t)p.n_blocks * p.pre.n_kv_heads)), block(kThreads);
-  if (grid.x == 0) return hipSuccess;
-  // K and V of a block that no other reads need not stay in the caches
-  if (p.pre.max_rows <= kRows<false>)
-    hipLaunchKernelGGL((link_shared_d128_kernel<false, 2>), grid, block, 0, st, p);
-  else if (p.pre.nrb == 1)
-    hipLaunchKernelGGL((link_shared_d128_kernel<true, 2>), grid, block, 0, st, p);
+hipError_t launch_link_shared(const SharedParams &p, hipStream_t st) {
+  if (p.unit_wgs + p.n_blocks == 0) return hipSuccess;
+  if (p.pre.d_k == 128)
+    launch_shared_t<128>(p, st);
   else
-    hipLaunchKernelGGL((link_shared_d128_kernel<true, 0>), grid, block, 0, st, p);
+    launch_shared_t<64>(p, st);
   return hipGetLastError();
 }
 

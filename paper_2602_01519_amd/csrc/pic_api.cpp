@@ -109,6 +109,7 @@ struct Slot {
   bool grows = false;
   int64_t max_tokens = 0;
   std::vector<int32_t> layer_len;
+  uint64_t append = 0;           // the last append call that named it
 
   int64_t tokens(int32_t layer) const { return grows ? layer_len[layer] : len; }
   // Tokens of a run that are there, of a chunk's n.
@@ -201,6 +202,7 @@ struct pic_store {
   int64_t layer_bytes = 0;       // bytes of one layer's pool; layer l of a slot is l * layer_bytes on
   int64_t live_plans = 0, live_indexes = 0;
   uint64_t versions = 0;         // Slot::version of the newest content
+  uint64_t appends = 0;          // append calls
   int64_t k_tok_elems = 0;       // K elements per padded token (all heads)
   int64_t v_tok_elems = 0;       // V elements per padded token (GQA)
   int64_t page_bytes = 0;        // bytes of a 64-token page in one layer
@@ -649,7 +651,7 @@ void prof_stop(hipStream_t st, std::pair<hipEvent_t, hipEvent_t> *ev, const char
 }
 
 enum class Mode { Prefill, Decode };
-enum class Kern { Valu, Mfma128, Decode128, Mla, Stream, Fp4, Fp4Prefill, Shared128 };
+enum class Kern { Valu, Mfma128, Decode128, Mla, Stream, Fp4, Fp4Prefill, Shared };
 
 // Everything about a call that does not depend on its tensors: the resolved
 // tables, the kernel, the split count and the workspace layout
@@ -665,7 +667,7 @@ struct Setup {
   // every row's softmax state goes to the partials, also of a request in one piece; the
   // caller sets lp.part_* and merges them
   bool partial = false;
-  bool shared = false;           // groups that share links, for the shared kernel
+  bool shared = false;           // for the shared kernel (bf16 GQA, 64 or 128 wide; no limits)
   bool lean = false;             // a small call the lean kernel runs
   bool small = false;            // tables as a kernel argument, own KV in place
   int32_t rows_per_block = 0;    // rows of a workgroup (decode kernel: wave)
@@ -1025,14 +1027,14 @@ bool fp4_few_rows(const Plan &P, const pic_store_desc &d, int group, int cus) {
 
 // Times of a CU in the shared kernel: for a 64-key tile of a block of 256 rows (of 128: half of
 // it), for the start and end of a block, and for a 32-key tile of its waves' units (eight at a time).
-constexpr double kSharedTileUs = 2.3, kSharedBlockUs = 8, kSharedUnitTileUs = 0.6;
+constexpr double kSharedTileUs = 2.3, kSharedTileUs64 = 1.2, kSharedBlockUs = 8, kSharedUnitTileUs = 0.6;
 
 // Work of the groups' blocks and of the requests' units in the shared kernel, in CU x us.
 struct SharedWork {
   double groups, units;
 };
 SharedWork shared_work(const Plan &groups, const Plan &requests, const pic_store_desc &d, int group, int32_t cus) {
-  const int rows = shared_d128_rows_per_block(groups.max_rows);
+  const int rows = shared_rows_per_block(groups.max_rows);
   SharedWork w{(double)cus * kSharedBlockUs, 0};     // (about a block a CU)
   for (const ReqEntry &R : groups.reqs)
     w.groups += d.n_kv_heads * kSharedTileUs * rows / 256 * R.tiles * (((int64_t)R.lq * group + rows - 1) / rows);
@@ -1070,8 +1072,8 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
     const int64_t part = 2 * (int64_t)std::min(max_rows, mfma_d128_rows_per_block()) * (d.d_v + 2) * 4;
     const int64_t tile = (int64_t)kTile * (d.d_k + d.d_v) * 2;
     c.min_piece = (int32_t)std::max<int64_t>(1, std::min<int64_t>(8, part / tile));
-  } else if (kern == Kern::Shared128) {
-    us = kSharedTileUs * rows_per_block / 256;
+  } else if (kern == Kern::Shared) {
+    us = (d.d_k == 128 ? kSharedTileUs : kSharedTileUs64) * rows_per_block / 256;
     c.slots = cus;
     c.over = kSharedBlockUs / us;
     c.min_piece = 2;
@@ -1133,7 +1135,7 @@ SplitCost split_cost(Kern kern, int32_t cus, const pic_store_desc &d, int32_t ma
   // 77 us with a twentieth free, 64 us with a tenth or more; 8 bf16 requests
   // of 30..300 tokens, 64-wide heads: 168 us full, 147 us).
   // (The blocks of groups that share links are listed one by one: none is empty.)
-  c.fit = uneven_rows && kern != Kern::Shared128 ? c.slots * 7 / 8 : c.slots;
+  c.fit = uneven_rows && kern != Kern::Shared ? c.slots * 7 / 8 : c.slots;
   c.part = part_us / us;
   c.fixed = 4.5 / us;
   return c;
@@ -1373,7 +1375,7 @@ pic_status setup_planned(pic_store *s, int32_t n_q_heads, int32_t num_splits, Mo
   // rows of one request that see different numbers of linked rows need the
   // per-row masks of the flash kernel
   if (kern == Kern::Decode128 && !P.doc_lim.empty()) kern = Kern::Mfma128;
-  if (C.shared) kern = Kern::Shared128;
+  if (C.shared) kern = Kern::Shared;
   if (d.dtype == PIC_BF16 && mla && d.d_k == 576 && d.d_v == 512) kern = Kern::Mla;
   if (fp4) kern = fp4_few_rows(P, d, lp.group, s->shape.cus) ? Kern::Fp4 : Kern::Fp4Prefill;
   // A small generic call of a shape the lean kernel is built for (tables as
@@ -1406,7 +1408,7 @@ pic_status setup_planned(pic_store *s, int32_t n_q_heads, int32_t num_splits, Mo
                              : kern == Kern::Mla   ? mla_rows_per_block()
                              : kern == Kern::Fp4   ? fp4_rows_per_block(P.max_rows)
                              : kern == Kern::Fp4Prefill ? fp4_prefill_rows_per_block()
-                             : kern == Kern::Shared128 ? shared_d128_rows_per_block(P.max_rows)
+                             : kern == Kern::Shared ? shared_rows_per_block(P.max_rows)
                                                    : decode_d128_max_rows();
   C.rows_per_block = rows_per_block;
   lp.nrb = std::max(1, (P.max_rows + rows_per_block - 1) / rows_per_block);
@@ -1689,19 +1691,20 @@ struct SharedCall {
   std::vector<MergeEntry> merge;
   bool has_pre = false, has_own = false;       // some request sees a key there
   TableLayout t_pre{}, t_own{};
-  std::vector<std::pair<int32_t, int32_t>> blocks;   // kernels_shared_d128.hip: pre's item, row block
+  std::vector<std::pair<int32_t, int32_t>> blocks;   // kernels_shared_mfma.hip: pre's item, row block
   size_t off_own = 0, off_merge = 0, off_blocks = 0, table_bytes = 0, work_bytes = 0;
   int32_t pieces = 1;                          // most pieces of a row
   int32_t unit_wgs = 0;                        // workgroups for own's units
 
-  // pre and own in one launch of the shared kernel
-  bool one_launch() const { return has_pre && pre.shared; }
+  // the call that the shared kernel takes in blocks, if one; own's pieces beside it as units
+  const Setup *blocked() const { return has_own && own.shared ? &own : has_pre && pre.shared ? &pre : nullptr; }
+  bool units() const { return has_pre && pre.shared && has_own && own.kern == Kern::Decode128; }
 };
 
 // Whether both calls run one kernel in one shape, which takes items of either.
 bool joinable(const Setup &a, const Setup &b) {
-  return a.kern == b.kern && a.kern != Kern::Valu && a.kern != Kern::Shared128 &&
-         a.rows_per_block == b.rows_per_block && a.lp.kpar == b.lp.kpar && a.P.doc_lim.empty() && b.P.doc_lim.empty();
+  if (a.kern != b.kern || a.kern == Kern::Valu || !a.P.doc_lim.empty() || !b.P.doc_lim.empty()) return false;
+  return a.kern == Kern::Shared || (a.rows_per_block == b.rows_per_block && a.lp.kpar == b.lp.kpar);
 }
 
 // Puts the requests of `pre` (no own KV) before those of `own`, in one call: one launch, cut for the
@@ -1730,9 +1733,11 @@ pic_status join_calls(pic_store *s, int32_t n_q_heads, Setup &pre, Setup &own) {
   P.self = Q.self;
   P.total_self = Q.total_self;
   const Mode mode = own.kern == Kern::Decode128 ? Mode::Decode : Mode::Prefill;
+  const bool shared = own.shared;
   pre = Setup{};
   own = Setup{};
   own.partial = true;
+  own.shared = shared;
   own.P = std::move(P);
   return setup_planned(s, n_q_heads, 0, mode, own);
 }
@@ -1760,6 +1765,14 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
   pr.chunk_starts = groups->chunk_starts;
   pr.q_offsets = group_q.data();
   S.pre.partial = S.own.partial = true;
+  // 64-wide bf16 heads: requests of more than 16 rows run the shared kernel joined with their groups
+  // (3 x 3..9 questions of 5..60 tokens, 24/6 heads, 45 us, by the streaming kernel 56; 3 x 9 of
+  // 60..100 212, 278; 2 x 3 of 6..20 25, 34), and so do groups alone, but those of few rows, which
+  // leave a block's matrix rows empty (128 rows of 60 links of 1024 34 us, 45; 48 of 10 links 36, 32).
+  // Single tokens stay joined in the streaming kernel (4 x 12, 32/8 heads, 41 us, apart 43; 4 x 5 33, 39).
+  const pic_store_desc &d = s->desc;
+  const bool narrow = d.kind == PIC_GQA && d.dtype == PIC_BF16 && d.d_k == 64 && d.d_v == 64;
+  S.own.shared = narrow && !req->q_doc_limits && (int64_t)most_q * n_q_heads > 16 * (int64_t)d.n_kv_heads;
   pic_status rc = setup_call(s, req, n_q_heads, scale, layer, 0, most_q <= 16 ? Mode::Decode : Mode::Prefill, S.own);
   if (rc != PIC_OK) return rc;
   rc = plan_call(s, &pr, n_q_heads, scale, layer, INT32_MAX, S.pre.P);
@@ -1767,6 +1780,8 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
   const int32_t cus = s->shape.cus;
   const int group = n_q_heads / s->desc.n_kv_heads;
   SharedWork work{0, 0};
+  S.pre.shared = narrow && S.pre.P.max_rows > 16 &&
+                 (S.own.shared || (S.own.P.max_tiles == 0 && S.pre.P.max_rows > 64));
   if (S.own.kern == Kern::Decode128 && S.own.P.max_tiles > 0 && S.pre.P.max_rows > decode_d128_max_rows()) {
     work = shared_work(S.pre.P, S.own.P, s->desc, group, cus);
     S.pre.shared = work.groups + work.units <= cus * kSharedMostUs;
@@ -1782,7 +1797,7 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
     S.joined = true;
     S.has_pre = false;
   }
-  if (S.one_launch()) {
+  if (S.units()) {
     // each part gets CUs by its share of the work, and is cut for those
     const double share = work.units / (work.groups + work.units);
     S.unit_wgs = std::max(1, std::min(cus - 1, (int32_t)std::lround(cus * share)));
@@ -1790,7 +1805,7 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
     rc = split_items(s, n_q_heads, 0, Mode::Decode, none, S.unit_wgs, S.own);
     if (rc == PIC_OK) rc = split_items(s, n_q_heads, 0, Mode::Prefill, none, cus - S.unit_wgs, S.pre);
     if (rc != PIC_OK) return rc;
-    S.unit_wgs = std::min(S.unit_wgs, (S.own.n_items * s->desc.n_kv_heads + shared_d128_waves() - 1) / shared_d128_waves());
+    S.unit_wgs = std::min(S.unit_wgs, (S.own.n_items * s->desc.n_kv_heads + shared_waves() - 1) / shared_waves());
   }
   S.merge.resize(B);
   const auto source = [](const Setup &C, int32_t r, int32_t row, MergeEntry &m, int x) {
@@ -1820,15 +1835,15 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
       if (!S.joined && S.has_own && R.tiles > 0) source(S.own, r, 0, m, 1);
       S.pieces = std::max(S.pieces, m.splits[0] + m.splits[1]);
     }
-  if (S.one_launch()) {
+  if (const Setup *C = S.blocked()) {
     // (in the items' order; a row block's other heads follow it)
     int32_t item = 0;
-    for (int32_t g : S.pre.P.order) {
-      const int32_t rows = S.pre.P.reqs[g].lq * S.pre.lp.group;
-      for (int32_t i = 0; i < S.pre.req_splits[g]; ++i, ++item)
-        for (int32_t rb = 0; rb * S.pre.rows_per_block < rows; ++rb) S.blocks.emplace_back(item, rb);
+    for (int32_t r : C->P.order) {
+      const int32_t rows = C->P.reqs[r].lq * C->lp.group;
+      for (int32_t i = 0; i < C->req_splits[r]; ++i, ++item)
+        for (int32_t rb = 0; rb * C->rows_per_block < rows; ++rb) S.blocks.emplace_back(item, rb);
     }
-    if ((int64_t)S.blocks.size() * S.pre.lp.n_kv_heads > kMostBlocks)
+    if ((int64_t)S.blocks.size() * C->lp.n_kv_heads > kMostBlocks - s->shape.cus)
       return fail(PIC_ERR_UNSUPPORTED, "too many query rows for one launch");
   }
   S.t_pre = table_layout(S.pre);
@@ -1846,7 +1861,8 @@ void write_shared_tables(const SharedCall &S, const LinkEntry *pre_links, const 
   write_tables(S.own, S.t_own, own_links, h + S.off_own);
   memcpy(h + S.off_merge, S.merge.data(), sizeof(MergeEntry) * S.merge.size());
   SharedBlock *b = (SharedBlock *)(h + S.off_blocks);
-  for (const auto &x : S.blocks) *b++ = SharedBlock{((const WorkItem *)(h + S.t_pre.off_i))[x.first], x.second};
+  const char *items = h + (S.blocked() == &S.own ? S.off_own + S.t_own.off_i : S.t_pre.off_i);
+  for (const auto &x : S.blocks) *b++ = SharedBlock{((const WorkItem *)items)[x.first], x.second};
 }
 
 Partials place_partials(char *at, int64_t rows, int32_t d_v) {
@@ -1881,41 +1897,47 @@ pic_status launch_shared(const pic_store *s, const SharedCall &S, char *dev, con
     return lp;
   };
   const LinkParams lp_pre = params(S.pre, S.t_pre, 0, m.src[0]);
-  const LinkParams lp_own = params(S.own, S.t_own, S.off_own, m.src[1]);
-  if (S.has_own && !S.one_launch()) {
-    Prologue pro;
-    const char *tables = host_dev ? host_dev : dev;
-    pro.links = (const LinkEntry *)(tables + S.off_own);
-    pro.reqs = (const ReqEntry *)(tables + S.off_own + S.t_own.off_r);
-    if (host_dev) {
-      pro.copy_src = host_dev;
-      pro.copy_dst = dev;
-      pro.copy_bytes = (int64_t)S.table_bytes;
-    }
+  LinkParams lp_own = params(S.own, S.t_own, S.off_own, m.src[1]);
+  lp_own.q = q;
+  lp_own.k_self = k_self;
+  lp_own.v_self = v_self;
+  lp_own.scale_log2 = scale * 1.4426950408889634f;
+  const Setup *blocks = S.blocked();
+  Prologue pro;
+  const char *tables = host_dev ? host_dev : dev;
+  pro.links = (const LinkEntry *)(tables + S.off_own);
+  pro.reqs = (const ReqEntry *)(tables + S.off_own + S.t_own.off_r);
+  if (host_dev) {
+    pro.copy_src = host_dev;
+    pro.copy_dst = dev;
+    pro.copy_bytes = (int64_t)S.table_bytes;
+  }
+  if (S.has_own && blocks == &S.own) {
+    if (S.own.P.max_own_lp > 0 || pro.copy_bytes > 0)
+      HIP_TRY(launch_prologue(lp_own, pro.links, pro.reqs, false, s->esz, S.own.P.max_own_lp,
+                              S.own.own_args.empty() ? nullptr : S.own.own_args.data(), work, pro.copy_src,
+                              pro.copy_dst, pro.copy_bytes, st), "prep_own_kernel");
+  } else if (S.has_own && !S.units()) {
     const pic_status rc = launch_call(s, S.own, lp_own, work, pro, q, k_self, v_self, scale, out, lse, st);
     if (rc != PIC_OK) return rc;
   } else if (host_dev) {
     HIP_TRY(launch_table_copy(host_dev, dev, (int64_t)S.table_bytes, st), "table_copy_kernel");
   }
-  if (S.one_launch()) {
+  if (blocks) {
     SharedParams sp{};
-    sp.pre = lp_pre;
     sp.own = lp_own;
-    for (LinkParams *lp : {&sp.pre, &sp.own}) {
-      lp->q = q;
-      lp->k_self = k_self;
-      lp->v_self = v_self;
-      lp->scale_log2 = scale * 1.4426950408889634f;
-    }
+    sp.pre = blocks == &S.own ? lp_own : lp_pre;
+    sp.pre.q = q;
+    sp.pre.scale_log2 = lp_own.scale_log2;
     sp.blocks = (const SharedBlock *)(dev + S.off_blocks);
     sp.n_blocks = (int32_t)S.blocks.size();
-    sp.n_units = S.own.n_items * s->desc.n_kv_heads;
+    sp.n_units = S.units() ? S.own.n_items * s->desc.n_kv_heads : 0;
     sp.unit_wgs = S.unit_wgs;
     std::pair<hipEvent_t, hipEvent_t> ev{nullptr, nullptr};
     prof_start(st, &ev);
-    const hipError_t e = launch_link_shared_d128(sp, st);
-    prof_stop(st, &ev, "link_shared_d128_kernel");
-    HIP_TRY(e, "link_shared_d128_kernel");
+    const hipError_t e = launch_link_shared(sp, st);
+    prof_stop(st, &ev, "link_shared_kernel");
+    HIP_TRY(e, "link_shared_kernel");
   } else if (S.has_pre) {
     const pic_status rc = launch_call(s, S.pre, lp_pre, work, Prologue{}, q, nullptr, nullptr, scale, out, lse, st);
     if (rc != PIC_OK) return rc;
@@ -2422,10 +2444,7 @@ pic_status pic_store_append(pic_store *s, const pic_append *a, void *stream) {
   p.positions = a->positions;
   return guarded([&] {
     std::vector<Slot *> slots(n);
-    std::vector<uint64_t> seen(a->chunk_ids, a->chunk_ids + n);
-    std::sort(seen.begin(), seen.end());
-    if (std::adjacent_find(seen.begin(), seen.end()) != seen.end())
-      return fail(PIC_ERR_INVALID, "a chunk is named twice");
+    const uint64_t call = ++s->appends;
     for (int32_t i = 0; i < n; ++i) {
       const uint64_t id = a->chunk_ids[i];
       auto it = s->map.find(id);
@@ -2434,6 +2453,8 @@ pic_status pic_store_append(pic_store *s, const pic_append *a, void *stream) {
       Slot &sl = it->second;
       if (!sl.grows)
         return fail(PIC_ERR_INVALID, "chunk id 0x%llx was not made by pic_store_open", (unsigned long long)id);
+      if (sl.append == call) return fail(PIC_ERR_INVALID, "chunk id 0x%llx is named twice", (unsigned long long)id);
+      sl.append = call;
       if (sl.plan_refs > 0)
         return fail(PIC_ERR_INVALID, "chunk id 0x%llx is linked by %lld live link plans",
                     (unsigned long long)id, (long long)sl.plan_refs);

@@ -594,23 +594,23 @@ struct MergeParams {
 hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows,
                         int32_t rows, int32_t pieces, hipStream_t st);
 
-// bf16 GQA link attention of requests that share links, d_k = d_v = 128, to partials: row blocks
-// of the groups' pieces (pre), and units (item x kv head, at most 16 rows) of the requests' own
-// links and KV (own; n_units 0: none).
+// bf16 GQA link attention of requests that share links, d_k = d_v in {64, 128}, to partials: row
+// blocks of pre's items (64: with own KV laid out like a chunk), and of 128-wide heads units (item
+// x kv head, at most 16 rows) of own's items.
 struct alignas(16) SharedBlock {
   WorkItem item;              // one of pre's (here too: a read less before the first key)
   int32_t rb;                 // row block
 };
 struct SharedParams {
-  LinkParams pre, own;        // items, links, tensors and part_* set
+  LinkParams pre, own;        // links, tensors and part_* set, own's items too
   const SharedBlock *blocks;
   int32_t n_blocks, n_units;
   int32_t unit_wgs;           // workgroups for the units (0 if none)
 };
 static_assert(sizeof(SharedParams) <= 4064, "kernel arguments");
-int shared_d128_waves();
-int shared_d128_rows_per_block(int max_rows);
-hipError_t launch_link_shared_d128(const SharedParams &p, hipStream_t st);
+int shared_rows_per_block(int max_rows);
+int shared_waves();           // of a workgroup
+hipError_t launch_link_shared(const SharedParams &p, hipStream_t st);
 
 // Link attention over selected blocks (kernels_sparse.hip). A request's blocks are the 64-token
 // tiles of its links, in order.

@@ -177,11 +177,12 @@ def _ptr(x):
 def _token_stride(x) -> int:
     """Elements from token to token of a torch tensor [tokens][heads][width] whose tokens are dense
     rows (0: leave it to the call)."""
-    if not hasattr(x, "stride"):
+    if x is None or not hasattr(x, "stride"):
         return 0
-    if x.dim() != 3 or (x.numel() and (x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]))):
+    strides, shape = x.stride(), x.shape
+    if len(shape) != 3 or (shape[0] and shape[1] and (strides[2] != 1 or (shape[1] > 1 and strides[1] != shape[2]))):
         raise PicError(ERR_INVALID, "a tensor must be [tokens][heads][width] with dense rows")
-    return x.stride(0) if x.shape[0] > 1 else 0
+    return strides[0] if shape[0] > 1 else 0
 
 
 def _host_i32(a):

@@ -149,13 +149,50 @@ def test_ragged_questions(shape, limits, starts):
 
 
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[4], SHAPES[6]], ids=lambda s: s[0])
-@pytest.mark.parametrize("n", [2, 4, 5, 17, 70])
+@pytest.mark.parametrize("n", [2, 4, 5, 17, 40, 70])
 def test_sizes_of_a_group(shape, n):
     """Rows of a group from one workgroup's to several, over few and many keys."""
     rng = np.random.default_rng(n)
     for shared in ([1], [64], [2500, 33]):
         b = Batch(rng, *shape[1:], [n], [shared], [[]] * n, [1] * n, own=[int(x) for x in rng.integers(0, 40, n)])
         b.check(*b.call(), label=str(shared))
+
+
+@pytest.mark.parametrize("shape,q_len", [(SHAPES[0], 1), (SHAPES[0], 6), (SHAPES[1], 1), (SHAPES[3], 1), (SHAPES[4], 9)],
+                         ids=lambda x: x[0] if isinstance(x, tuple) else str(x))
+def test_log_sums_are_of_unrounded_probabilities(shape, q_len):
+    """Few keys, where a probability rounded to bf16 would show in the log-sum-exp. Products of bf16
+    elements are exact in fp32, so a logit is off by at most d_k roundings of the sum of its products'
+    sizes; the sums of n probabilities, their exponents, maxima and joins by at most n + 32 more of
+    numbers up to the logits' size."""
+    rng = np.random.default_rng(11)
+    n = 5
+    b = Batch(rng, *shape[1:], [n], [[3]], [[2]] * n, [q_len] * n, own=[2] * n)
+    out, lse = b.call()
+    b.check(out, lse)
+    d, hkv = shape[4], shape[3]
+    size = 0.0
+    for r in range(n):
+        kk = torch.empty(5, hkv, d, dtype=torch.bfloat16, device="cuda")
+        pic.debug_gather(b.store, b.shared[0] + b.mine[r], kk, torch.empty_like(kk), L.stream())
+        q = b.q[r * q_len:(r + 1) * q_len].double().abs()
+        k = torch.cat([kk, b.ko[r * (q_len + 2):(r + 1) * (q_len + 2)]]).double().abs()
+        for h in range(b.hq):
+            size = max(size, b.scale * float((q[:, h] @ k[:, h // (b.hq // hkv)].T.contiguous()).max()))
+    bound = 2.0 ** -24 * (d * size + (7 + q_len + 32) * (1 + size))
+    assert bound < 3e-4     # (a probability rounded to bf16 is off by up to 2 ** -8 = 4e-3 of it)
+    assert float((lse.double() - b.refs[0][1]).abs().max()) <= bound
+
+
+def test_long_calls():
+    """More work than one launch takes: the groups' blocks and the requests' units in a launch each."""
+    rng = np.random.default_rng(12)
+    n = 160
+    b = Batch(rng, pic.GQA, pic.BF16, 2, 128, 128, 8, [n], [[25001]], [[70]] + [[]] * (n - 1), [1] * n,
+              own=[int(x) for x in rng.integers(0, 90, n)])
+    b.check(*b.call())
+    with b.plan() as plan:
+        b.check(*b.run(plan), label="plan")
 
 
 def test_rows_that_see_nothing():

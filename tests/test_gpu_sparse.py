@@ -148,6 +148,32 @@ def test_a_batch_larger_than_the_gpu():
     c.check(c.call(9, 1, 1), 9, 1, 1)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_log_sums_are_of_unrounded_probabilities(d):
+    """Few keys, where a probability rounded to bf16 would show in the log-sum-exp. A logit is off by
+    at most d roundings of the sum of its products' sizes, the sums of the probabilities, their
+    exponents, maxima and joins by at most n + 32 more of numbers up to the logits' size."""
+    rng = np.random.default_rng(12)
+    c = Case(rng, pic.BF16, 2, d, 4, [3, 2, 4], [[0], [1, 0], [2]], [1, 1, 2], own=[0, 2, 1])
+    got = c.call(2)
+    c.check(got, 2)
+    size = 0.0
+    at = 0
+    for r, l in enumerate(c.links):
+        for i in range(c.q_len[r]):
+            s0 = sum(c.own[:r])
+            k = torch.empty(sum(c.store.lookup(j) for j in l), 2, d, dtype=torch.bfloat16, device="cuda")
+            pic.debug_gather(c.store, l, k, torch.empty_like(k), L.stream())
+            k = torch.cat([k, c.ko[s0:s0 + c.own[r] - c.q_len[r] + i + 1]]).double()
+            for h in range(c.hq):
+                s = c.scale * (c.q[at, h].double() * k[:, h // 4])
+                size = max(size, float(s.abs().sum(1).max()))
+                bound = 2.0 ** -24 * (d * size + 45 * (1 + size))
+                assert bound < 3e-4
+                assert abs(float(got[1][at, h]) - float(torch.logsumexp(s.sum(1), 0))) <= bound
+            at += 1
+
+
 def test_equal_scores_go_to_the_lower_block():
     rng = np.random.default_rng(4)
     c = Case(rng, pic.BF16, 2, 64, 3, [64, 128, 64], [[0, 0, 1, 0, 2, 0, 1, 0], [0] * 40], [1, 1])
