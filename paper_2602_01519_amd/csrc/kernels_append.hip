@@ -60,21 +60,11 @@ __device__ __forceinline__ void append_rows(const AppendParams &p, int block, fl
   const int64_t src0 = P.src0 + tok0;
   const int row0 = P.row0 + tok0;
 
-  for (int i = threadIdx.x; i < ntok * half; i += kThreads) {
-    const int t = div_small(i, p.inv_half), j = i - t * half;
-    const double rev = (double)p.positions[src0 + t] * p.rev[j];
-    float s, c;
-    sincospif(2.f * (float)(rev - rint(rev)), &s, &c);
-    trig[t * 2 * part + j] = c * p.magnitude;
-    trig[t * 2 * part + part + j] = s * p.magnitude;
-  }
-  __syncthreads();
-
-  for (int r0 = slot; r0 < rows; r0 += kBatch * p.slots) {
-    uint4 a[kBatch], b[kBatch];
-    const T *src[kBatch];
-    T *dst[kBatch];
-    int tok[kBatch];
+  uint4 a[kBatch], b[kBatch];
+  const T *src[kBatch];
+  T *dst[kBatch];
+  int tok[kBatch];
+  const auto load = [&](int r0) {
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int r = r0 + k * p.slots;
@@ -95,6 +85,23 @@ __device__ __forceinline__ void append_rows(const AppendParams &p, int block, fl
         if (kHalf && pc.rot) b[k] = load_nt(src[k] + half);
       }
     }
+  };
+  // On their way while the angles are formed: 2000 tokens of 16 query heads and a latent row of 576,
+  // one wave of workgroups, 19.8 -> 17.3 us.
+  load(slot);
+
+  for (int i = threadIdx.x; i < ntok * half; i += kThreads) {
+    const int t = div_small(i, p.inv_half), j = i - t * half;
+    const double rev = (double)p.positions[src0 + t] * p.rev[j];
+    float s, c;
+    sincospif(2.f * (float)(rev - rint(rev)), &s, &c);
+    trig[t * 2 * part + j] = c * p.magnitude;
+    trig[t * 2 * part + part + j] = s * p.magnitude;
+  }
+  __syncthreads();
+
+  for (int r0 = slot; r0 < rows; r0 += kBatch * p.slots) {
+    if (r0 != slot) load(r0);
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       if (!src[k]) continue;
