@@ -41,22 +41,22 @@ __device__ __forceinline__ const E *value_at(const LinkEntry &e, int head, int d
 // 16 bytes at any address that is aligned to its elements
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 
-// The listed links back to token-major rows. A unit is a page (64 tokens) of one head: its K
-// rows, or 64 dims of its V panels, transposed through LDS (links' tile0: their first page in
-// the list). 16-byte pieces; one element a thread, with a search for each element's link, took
+// The listed links back to token-major rows. A unit is of a page (64 tokens) of one head: 16 KB
+// of its K rows, or 64 dims of its V panels, transposed through LDS (links' tile0: their first
+// page in the list). 16-byte pieces; one element a thread, with a search for each element's link, took
 // 48 chunks of 128
 // tokens, 8 heads x 128 bf16, in 72 us a call, now 10.9.
 template <typename E>
 __device__ __forceinline__ void gather_pages(const LinkEntry *__restrict__ links, int32_t n_links,
                                              int64_t units, int32_t heads, int32_t d_k, int32_t d_v,
-                                             int32_t v_parts, E *__restrict__ k_out,
+                                             int32_t v_parts, int32_t k_parts, E *__restrict__ k_out,
                                              E *__restrict__ v_out) {
   constexpr int N = 16 / sizeof(E);
   constexpr int ROW = 64 + N;                // padded LDS row (elements)
   __shared__ __attribute__((aligned(16))) E tile[64 * ROW];
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int part = (int)(unit % (v_parts + 1));
-    const int64_t x = unit / (v_parts + 1);
+    const int part = (int)(unit % (v_parts + k_parts));
+    const int64_t x = unit / (v_parts + k_parts);
     const int h = (int)(x % heads);
     const int64_t pg = x / heads;
     int lo = 0, hi = n_links - 1;
@@ -67,10 +67,10 @@ __device__ __forceinline__ void gather_pages(const LinkEntry *__restrict__ links
     const LinkEntry e = links[lo];
     const int row0 = (int)(pg - e.tile0) * kTile, n = min(kTile, e.len - row0);
     const int64_t tok = (int64_t)e.tok0 + row0;
-    if (part == v_parts) {
+    if (part >= v_parts) {
       const E *src = key_row<E>(e, h, row0, d_k);
-      const int per = d_k / N;
-      for (int i = threadIdx.x; i < n * per; i += 256) {
+      const int per = d_k / N, rows = (kTile + k_parts - 1) / k_parts, r0 = (part - v_parts) * rows;
+      for (int i = r0 * per + threadIdx.x; i < min(n, r0 + rows) * per; i += 256) {
         const int r = i / per, c = (i - r * per) * N;
         const uint4 v = *(const uint4 *)(src + (int64_t)r * d_k + c);
         *(u32x4u *)(k_out + ((tok + r) * heads + h) * d_k + c) = u32x4u{v.x, v.y, v.z, v.w};
@@ -102,8 +102,9 @@ __device__ __forceinline__ void gather_pages(const LinkEntry *__restrict__ links
 template <typename E>
 __global__ __launch_bounds__(256) void gather_kernel(const LinkEntry *links, int32_t n_links,
                                                      int64_t units, int32_t heads, int32_t d_k,
-                                                     int32_t d_v, int32_t v_parts, E *k_out, E *v_out) {
-  gather_pages<E>(links, n_links, units, heads, d_k, d_v, v_parts, k_out, v_out);
+                                                     int32_t d_v, int32_t v_parts, int32_t k_parts,
+                                                     E *k_out, E *v_out) {
+  gather_pages<E>(links, n_links, units, heads, d_k, d_v, v_parts, k_parts, k_out, v_out);
 }
 struct GatherLinks {
   LinkEntry link[kGatherArgs];
@@ -112,9 +113,9 @@ static_assert(sizeof(GatherLinks) <= 3960, "kernel arguments");
 template <typename E>
 __global__ __launch_bounds__(256) void gather_args_kernel(GatherLinks links, int32_t n_links,
                                                           int64_t units, int32_t heads, int32_t d_k,
-                                                          int32_t d_v, int32_t v_parts, E *k_out,
-                                                          E *v_out) {
-  gather_pages<E>(links.link, n_links, units, heads, d_k, d_v, v_parts, k_out, v_out);
+                                                          int32_t d_v, int32_t v_parts, int32_t k_parts,
+                                                          E *k_out, E *v_out) {
+  gather_pages<E>(links.link, n_links, units, heads, d_k, d_v, v_parts, k_parts, k_out, v_out);
 }
 
 // Rows written into chunk slots (rows recomputed at link time): row i of the
@@ -1497,8 +1498,9 @@ hipError_t launch_write_rows(const RowView *views, int32_t n_views, const int32_
 hipError_t launch_gather(const LinkEntry *links, int32_t n_links, int64_t pages,
                          int32_t heads, int32_t d_k, int32_t d_v, int32_t mla, int32_t esz,
                          bool host, void *k_out, void *v_out, hipStream_t st) {
-  const int32_t v_parts = mla ? 0 : (d_v + 63) / 64;
-  const int64_t units = pages * heads * (v_parts + 1);
+  // (pages of 24 chunks of 4..450 latent rows of 576, a workgroup a page 9.5 us, a part of one 5.5)
+  const int32_t v_parts = mla ? 0 : (d_v + 63) / 64, k_parts = (d_k * esz + 255) / 256;
+  const int64_t units = pages * heads * (v_parts + k_parts);
   if (units == 0) return hipSuccess;
   const dim3 grid((unsigned)std::min<int64_t>(units, 65536));
   const auto go = [&](auto e) {
@@ -1507,10 +1509,10 @@ hipError_t launch_gather(const LinkEntry *links, int32_t n_links, int64_t pages,
       GatherLinks args;
       std::copy(links, links + n_links, args.link);
       hipLaunchKernelGGL(gather_args_kernel<E>, grid, dim3(256), 0, st, args, n_links, units, heads, d_k,
-                         d_v, v_parts, (E *)k_out, (E *)v_out);
+                         d_v, v_parts, k_parts, (E *)k_out, (E *)v_out);
     } else {
       hipLaunchKernelGGL(gather_kernel<E>, grid, dim3(256), 0, st, links, n_links, units, heads, d_k, d_v,
-                         v_parts, (E *)k_out, (E *)v_out);
+                         v_parts, k_parts, (E *)k_out, (E *)v_out);
     }
     return hipGetLastError();
   };
