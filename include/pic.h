@@ -412,9 +412,14 @@ pic_status pic_link_plan_destroy(pic_link_plan *plan);
  *     the batch. A group may be empty or share nothing.
  * Tensors, scale and lse as for pic_link_attn. Workspace: fp32 partials of every query row,
  * about 2 Tq * H_q * (d_v + 2) * 4 bytes or more where keys are split.
+ * The range of the values and the rounding of lse are those of the store's link calls; over bf16
+ * GQA stores with d_k = d_v = 128, or 64 and more than 16 query rows per kv head, the sums are of
+ * fp32 probabilities.
  * pic_link_shared_plan_create: the same, resolved once (req->layer must be 0), run and
- *   destroyed by pic_link_plan_run and pic_link_plan_destroy: a run enqueues kernels only.
- * Errors: as pic_link_attn; the plan's also OOM. */
+ *   destroyed by pic_link_plan_run and pic_link_plan_destroy: a run enqueues kernels only, and may
+ *   be captured.
+ * Errors: as pic_link_attn; UNSUPPORTED also for pic_link_shared in a graph capture (its
+ * workspace serves later calls); the plan's also OOM. */
 typedef struct pic_link_groups {
   int32_t n_groups;
   const int32_t *request_offsets;
@@ -447,13 +452,16 @@ pic_status pic_link_shared_plan_create(pic_store *store, const pic_link_req *req
  * pic_index_update: forms the summaries of the listed chunks (host, an id may repeat) in
  *   one layer, or in all of them for layer -1, as the chunks stand; ordered on `stream`. To be
  *   called again when a chunk has been written to, has grown (only blocks that grew are
- *   formed again) or has been put anew. Errors: INVALID, NOT_FOUND, HIP.
+ *   formed again) or has been put anew. A captured call forms the same blocks again when it
+ *   is replayed. Errors: INVALID, NOT_FOUND, HIP.
  * pic_index_destroy: waits for the device and frees the index; NULL is ignored.
  * pic_link_sparse: tensors, scale and lse as for pic_link_attn; req->q_doc_limits must be
  *   NULL. blocks: device int32 [Tq][n_kv_heads][n_blocks] or NULL: receives the taken blocks,
  *   ascending, -1 behind them. n_blocks 1 .. 1024, a request's blocks at most 8192 (else
  *   UNSUPPORTED). One token a request is the ordinary use (a decode step); several are
- *   computed one by one. Errors: INVALID (also a linked chunk whose summaries in the layer are
+ *   computed one by one. A graph capture takes calls of up to 88 links and 32 query tokens in
+ *   all (else UNSUPPORTED); a replay reads the rows that those links had, so their chunks have
+ *   to stay. Errors: INVALID (also a linked chunk whose summaries in the layer are
  *   not those of its present content), NOT_FOUND, UNSUPPORTED, OOM, HIP. */
 typedef struct pic_index pic_index;
 pic_status pic_index_create(pic_store *store, pic_index **out);

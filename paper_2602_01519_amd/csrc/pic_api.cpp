@@ -261,6 +261,17 @@ pic_status ensure_work(Stage *st, size_t bytes) {
   return PIC_OK;
 }
 
+// Whether work enqueued on a stream now becomes part of a graph. Such work may not use the ring's
+// slots: later calls take them while the graph lives.
+bool capturing(hipStream_t st) {
+  hipStreamCaptureStatus x = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(st, &x) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return x != hipStreamCaptureStatusNone;
+}
+
 // Returns a run of pages to the free map, merging it with free neighbours.
 void free_run(pic_store *s, int64_t page0, int64_t pages) {
   auto next = s->free_runs.lower_bound(page0);
@@ -1959,6 +1970,7 @@ pic_status shared_link_call(pic_store *s, const pic_link_req *req, const pic_lin
   if (S.own.P.total_q == 0) return PIC_OK;
   DeviceGuard dg(s->device);
   if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
+  if (capturing(st)) return fail(PIC_ERR_UNSUPPORTED, "in a graph capture run a plan (pic_link_shared_plan_create)");
   Stage *stage = nullptr;
   rc = stage_acquire(s, S.table_bytes, &stage);
   if (rc == PIC_OK) rc = ensure_work(stage, S.work_bytes);
@@ -3245,15 +3257,21 @@ pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_he
     p.first = keep_first;
     p.last = keep_last;
     p.scale_log2 = softmax_scale * 1.4426950408889634f;
-    p.splits = sparse_splits(s->shape.cus, (int64_t)tq * d.n_kv_heads, std::min(n_blocks, p.most_blocks));
     DeviceGuard dg(s->device);
     if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
     const hipStream_t st = (hipStream_t)stream;
+    const bool by_arg = links.size() <= (size_t)kSparseTabLinks && tq <= kSparseTabTokens;
+    p.splits = sparse_splits(s->shape.cus, (int64_t)tq * d.n_kv_heads, std::min(n_blocks, p.most_blocks));
+    if (capturing(st)) {
+      if (!by_arg)
+        return fail(PIC_ERR_UNSUPPORTED, "in a graph capture a call has at most %d links and %d query tokens",
+                    kSparseTabLinks, kSparseTabTokens);
+      p.splits = 1;
+    }
     const size_t off_t = round_up(sizeof(SparseLink) * links.size(), 256);
     const size_t bytes = off_t + round_up(sizeof(SparseToken) * tq, 256);
     const int64_t rows = (int64_t)tq * n_q_heads;
     const size_t part_bytes = p.splits > 1 ? (size_t)rows * p.splits * (d.d_v + 2) * sizeof(float) : 0;
-    const bool by_arg = links.size() <= (size_t)kSparseTabLinks && tq <= kSparseTabTokens;
     // (a call in one piece whose tables are kernel arguments needs no memory of the store's)
     Stage *stage = nullptr;
     if (!by_arg || part_bytes > 0) {

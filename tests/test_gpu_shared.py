@@ -269,6 +269,20 @@ def test_layers_streams_and_graphs():
     b.store.remove(b.mine[0][0], L.stream())
 
 
+def test_a_capture_takes_plans_alone():
+    rng = np.random.default_rng(13)
+    b = Batch(rng, pic.GQA, pic.BF16, 2, 128, 128, 4, [6], [[300]], [[]] * 6, [1] * 6, own=[9] * 6)
+    out, lse = b.buffers()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(pic.PicError) as e:
+            b.call(out=out, lse=lse)
+        assert e.value.status == pic.ERR_UNSUPPORTED
+        b.q.add_(0)
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())
+    b.check(*b.call())
+
+
 def test_growing_chunks_behind_shared_documents():
     """Decode steps whose own tokens live in growing chunks, behind the group's documents."""
     rng = np.random.default_rng(8)

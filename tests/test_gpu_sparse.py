@@ -342,6 +342,33 @@ def test_streams_layers_and_graphs():
         c.check(c.call(4), 4)
 
 
+def test_captured_calls():
+    """A capture takes no memory of the store's: a unit that eager calls share out is one workgroup's."""
+    rng = np.random.default_rng(13)
+    c = Case(rng, pic.BF16, 2, 128, 4, [700, 300, 64, 900], [[0, 1, 2, 3, 0, 3]], [1], own=[40])
+    bufs, g = c.buffers(24), torch.cuda.CUDAGraph()
+    c.check(c.call(24, 1, 1), 24, 1, 1)
+    with torch.cuda.graph(g):
+        c.call(24, 1, 1, bufs=bufs)
+    for _ in range(3):
+        c.q.copy_(L.draw(rng, pic.BF16, *c.q.shape))
+        eager = [c.call(24, 1, 1) for _ in range(9)]        # (every workspace of the store)
+        g.replay()
+        c.check(bufs, 24, 1, 1)
+        for x in eager:
+            c.check(x, 24, 1, 1)
+    c.links, c.starts = [[0] * 89], [[0] * 89]
+    out = c.buffers(24)
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(pic.PicError) as e:
+            c.call(24, bufs=out)
+        assert e.value.status == pic.ERR_UNSUPPORTED
+        c.q.add_(0)
+    torch.cuda.synchronize()
+    assert bool((out[0] == 7).all())
+    c.check(c.call(24), 24)
+
+
 def test_refusals_write_nothing():
     rng = np.random.default_rng(10)
     c = Case(rng, pic.BF16, 2, 64, 2, [200, 300], [[0, 1]], [1], own=[4])
