@@ -27,6 +27,8 @@ __device__ __forceinline__ void add_scaled(float4 &a, float w, const float4 &v) 
   a = make_float4(a.x + w * v.x, a.y + w * v.y, a.z + w * v.z, a.w + w * v.w);
 }
 
+constexpr int kMostBlocks = (1 << 24) - 1;     // (a launch's threads are counted in 32 bits)
+
 template <typename T, int kLanes, int kChunks, int kGpr>
 __global__ __launch_bounds__(256) void merge_kernel(MergeParams p) {
   constexpr int kB = 4;
@@ -166,8 +168,7 @@ hipError_t launch_merge_t(MergeParams p, int32_t batch, int32_t max_rows, int32_
     constexpr int kGpr = decltype(kg)::value;
     const int per = 256 / kLanes / kGpr;
     p.blocks = (max_rows + per - 1) / per;
-    // (a launch's threads are counted in 32 bits)
-    const int most = std::max(1, ((1 << 24) - 1) / p.blocks);
+    const int most = std::max(1, kMostBlocks / p.blocks);
     const MergeEntry *all = p.entries;
     for (int32_t at = 0; at < batch; at += most) {
       p.entries = all ? all + at : nullptr;
@@ -195,6 +196,8 @@ hipError_t launch_merge_w(const MergeParams &p, int32_t batch, int32_t max_rows,
 }
 
 }  // namespace
+
+int merge_most_rows() { return kMostBlocks * (256 / 64); }
 
 hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows, int32_t rows,
                         int32_t pieces, hipStream_t st) {

@@ -1786,6 +1786,8 @@ pic_status setup_shared(pic_store *s, const pic_link_req *req, const pic_link_gr
   S.own.shared = narrow && !req->q_doc_limits && (int64_t)most_q * n_q_heads > 16 * (int64_t)d.n_kv_heads;
   pic_status rc = setup_call(s, req, n_q_heads, scale, layer, 0, most_q <= 16 ? Mode::Decode : Mode::Prefill, S.own);
   if (rc != PIC_OK) return rc;
+  if ((int64_t)most_q * n_q_heads > merge_most_rows())
+    return fail(PIC_ERR_UNSUPPORTED, "a request has more than %d output rows", merge_most_rows());
   rc = plan_call(s, &pr, n_q_heads, scale, layer, INT32_MAX, S.pre.P);
   if (rc != PIC_OK) return rc;
   const int32_t cus = s->shape.cus;

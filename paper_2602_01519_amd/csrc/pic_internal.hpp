@@ -591,6 +591,7 @@ struct MergeParams {
   int32_t blocks;             // workgroups of a request (set by launch_merge)
 };
 // max_rows, pieces: most rows and pieces of an entry; rows: of all
+int merge_most_rows();            // of a request
 hipError_t launch_merge(const MergeParams &p, int dtype, int32_t batch, int32_t max_rows,
                         int32_t rows, int32_t pieces, hipStream_t st);
 

@@ -344,6 +344,9 @@ def test_refusals_write_nothing():
     bad(INV, q_doc_limits=[6, 0, 0])
     with pytest.raises(pic.PicError):
         pic.SharedLinkPlan(b.store, [0, 2], [0, 1], ids[:1], *a)
+    with pytest.raises(pic.PicError) as e:       # more output rows of a request than a launch merges
+        pic.SharedLinkPlan(b.store, [0, 1], [0, 1], ids[:1], [0, 0], [], [0, 2 ** 25], None, 2)
+    assert e.value.status == pic.ERR_UNSUPPORTED
     torch.cuda.synchronize()
     assert bool((out == 7).all()) and bool((lse == 3).all())
     # nothing to do
