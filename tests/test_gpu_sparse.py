@@ -282,6 +282,13 @@ def test_blocks_of_scattered_runs():
         c.check(c.call(n, 0, 1), n, 0, 1)
 
 
+def test_many_heads():
+    """The most kv heads, and more chunks than one launch of summaries takes."""
+    rng = np.random.default_rng(14)
+    c = Case(rng, pic.BF16, 256, 64, 1, [70, 1, 130] + [5] * 100, [[0, 1], [2, 102]], [1, 1], own=[3, 0])
+    c.check(c.call(2, 0, 1), 2, 0, 1)
+
+
 @pytest.mark.parametrize("blocks,ok", [(8192, True), (8193, False)])
 def test_longest_requests(blocks, ok):
     rng = np.random.default_rng(8)
