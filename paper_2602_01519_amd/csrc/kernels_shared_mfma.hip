@@ -23,6 +23,8 @@
 // bound by HBM where the groups' blocks are bound by the matrix cores. Both go in one launch: the
 // planner divides the CUs, some workgroups' waves take the requests' pieces one after another
 // (decode_d128.hpp; own rows are read in place and turn through LDS), the others a block each.
+#include <cfloat>
+
 #include "decode_d128.hpp"
 
 namespace pic {
@@ -133,11 +135,18 @@ struct State {
   float m, l;
 };
 
+// When a tile is done again against its own max, and what that max is raised by (64 wide, where the
+// sums of a block left the fp32 range: every tile, and the logarithm of the block's keys).
+struct Steps {
+  float jump, raise;
+};
+
 // One tile, the copies of a later one spread over its score products. The wave takes kN halves of
 // the tile's keys, from c.half on. lim: the last own key that this lane's row sees.
 template <int D, int kN, int kAux>
 __device__ __forceinline__ void compute_tile(const Lane<D> &c, const uint4 *kt, const bf16x8 (&qf)[D / 16], State<D> &a,
-                                             const TileRef &r, int lim, float sc, const TileRef &next, uint4 *to) {
+                                             const TileRef &r, int lim, float sc, Steps steps, const TileRef &next,
+                                             uint4 *to) {
   const uint4 *vt = kt + kUnits<D>;
   constexpr int kSteps = D / 16, kAhead = D == 64 ? 4 : 5;   // K reads run ahead of their products
   const int row = 32 * c.half + key_of_m(c.n);
@@ -195,14 +204,14 @@ __device__ __forceinline__ void compute_tile(const Lane<D> &c, const uint4 *kt, 
     return t[0] + t[1];
   };
   float t = probs();
-  if (__builtin_expect(__any(!(t <= kJumpSum) || (a.m == -INFINITY && seen)), 0)) {
+  if (__builtin_expect(__any(!(t <= (D == 64 ? steps.jump : kJumpSum)) || (a.m == -INFINITY && seen)), 0)) {
     float top = -INFINITY;
 #pragma unroll
     for (int h = 0; h < kN; ++h)
 #pragma unroll
       for (int x = 0; x < 16; x += 2) top = fmaxf(fmaxf(top, s[h][x]), s[h][x + 1]);
     top = half_max(top);
-    const float mnew = fmaxf(a.m, top * sc);
+    const float mnew = fmaxf(a.m, D == 64 ? top * sc + steps.raise : top * sc);
     const float f = mnew == a.m ? 1.f : __builtin_amdgcn_exp2f(a.m - mnew);
     a.m = mnew;
     a.l *= f;
@@ -275,6 +284,7 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
                           : min(it.t_end, visible_tiles(item_request(it), (min(nrows, row0 + kRows<kWide>) - 1) / group));
   // (past the last tile the copies repeat it into buffers nobody reads again, which keeps the
   // counts of the waits)
+  Steps steps{kJumpSum, 0.f};
   TileRef r0{}, r1{}, r2{}, r3{};
   auto tile = [&](int t) { return tile_ref<D>(cur, min(t, t1 - 1)); };
   auto issue = [&](const TileRef &r, int i) {
@@ -296,14 +306,24 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
     }
   }
   State<D> a;
+  const auto clear = [&]() {
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
+    for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-    for (int x = 0; x < 16; ++x) a.o[d][x] = 0.f;
-  a.m = -INFINITY;
-  a.l = 0.f;
+      for (int x = 0; x < 16; ++x) a.o[d][x] = 0.f;
+    a.m = -INFINITY;
+    a.l = 0.f;
+  };
+  clear();
+  const auto restart = [&]() {
+    clear();
+    cur.li = 0;
+    cursor_set(cur, it.k, it.v, it.len, it.lp, it.tile0);
+    r0 = tile(t0);
+    issue(r0, 0);
+  };
   const float sc = p.scale_log2;
-  if (t0 < t1) {
+  const auto walk = [&]() {                     // the first tile's copies are on their way
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     // (behind the first tile's arrival, which they would delay)
@@ -314,7 +334,7 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
     // Tile t from buffer i, the copies of tile t + 3 into the one that tile t - 1 left.
     auto step = [&](const TileRef &r, int i, const TileRef &next) {
       if (active)
-        compute_tile<D, kWide ? 2 : 1, kAux>(c, lds + 2 * kUnits<D> * i, qf, a, r, lim, sc, next,
+        compute_tile<D, kWide ? 2 : 1, kAux>(c, lds + 2 * kUnits<D> * i, qf, a, r, lim, sc, steps, next,
                                              lds + 2 * kUnits<D> * ((i + 3) & 3));
       else
         issue(next, (i + 3) & 3);
@@ -333,9 +353,26 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
       r2 = tile(t + 6);
       step(r3, 3, r2);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                            // every copy has landed, every tile is done with
+  };
+  if (t0 < t1) {
+#pragma unroll 1
+    for (;;) {
+      walk();
+      if constexpr (D == 128) break;
+      // Probabilities against a max that lags reach 2^64: the sums of large values may leave the
+      // fp32 range. Then once more, against a max that keeps them below the largest value.
+      float most = 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) most = __builtin_elementwise_maximum(most, fabsf(a.o[d][x]));   // (NaN if one is)
+      if (steps.raise > 0.f || !__syncthreads_or(!(most <= FLT_MAX))) break;
+      steps = Steps{0.f, log2f((float)(t1 - t0)) + 6.f};
+      restart();
+    }
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();                              // every copy has landed, every tile is done with
 
   const int nvalid = min(kRowsPerWave, nrows - (row0 + rg * kRowsPerWave));
   const int64_t prow = it.part + (orow - (int64_t)it.q0 * p.n_q_heads);

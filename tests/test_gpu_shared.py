@@ -231,6 +231,49 @@ def test_far_logits_and_large_values():
             assert bool(torch.isfinite(out[r]).all()) and near.any()
 
 
+@pytest.mark.parametrize("q_len,per", [(9, 2), (3, 2), (40, 3), (1, 3)])
+def test_values_near_the_largest(q_len, per):
+    """64-wide heads: values up to 2^126 under logits that rise by 40 along the keys, so that unnormalised
+    sums would leave the fp32 range. (Up to 16 rows run the streaming kernel, whose probabilities go up to
+    one: some 13 of them here, which takes 2^126 out of the range in it as in every link call of
+    64-wide heads. There the values go up to 2^101.) A probability is off by half a bf16 step, 2^-8 of it, the
+    logits (exact products of 8 and at most 40) and fp32 sums by less than 2^-12, the output by half a step."""
+    rng = np.random.default_rng(15)
+    n = per
+    b = Batch(rng, pic.GQA, pic.BF16, 2, 64, 64, 4, [n], [[]], [[]] * n, [q_len] * n, own=[30] * n)
+    store = pic.Store(pic.GQA, pic.BF16, 2, 64, 64, 64 * 30)
+    big = lambda *s: (L.draw(rng, pic.F32, *s).clamp(-2, 2) * 2.0 ** (125 if q_len > 4 else 100)).bfloat16()  # noqa: E731
+    lens = [700, 130]
+
+    def rising(m, lo, hi):
+        k = torch.zeros(m, 2, 64, dtype=torch.bfloat16, device="cuda")
+        k[:, :, 0] = torch.linspace(lo, hi, m, device="cuda").bfloat16()[:, None]
+        return k
+
+    ks, vs = [rising(700, 0, 30), rising(130, 30, 40)], [big(m, 2, 64) for m in lens]
+    for i, m in enumerate(lens):
+        store.put(1 + i, m, ks[i], vs[i], L.stream())
+    own = q_len + 30
+    q = torch.zeros(n * q_len, 8, 64, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 8.0                            # (the scale is 1 / 8)
+    ko, vo = torch.cat([rising(own, 0, 40) for _ in range(n)]), big(n * own, 2, 64)
+    out, lse = torch.empty_like(q), torch.empty(n * q_len, 8, dtype=torch.float32, device="cuda")
+    pic.link_shared(store, [0, n], [0, 2], [1, 2], [0] * (n + 1), [], L.offsets([q_len] * n), L.offsets([own] * n), 8, q, ko,
+                    vo, b.scale, out, lse, stream=L.stream())
+    torch.cuda.synchronize()
+    for r in range(n):
+        at, rows = slice(r * q_len, (r + 1) * q_len), slice(r * own, (r + 1) * own)
+        k, v = torch.cat(ks + [ko[rows]]), torch.cat(vs + [vo[rows]])
+        seen = L.causal(q_len, own, 830)
+        ref, ref_lse = L.attend(q[at], k, v, b.scale, seen)
+        size, _ = L.attend(q[at], k, v.abs(), b.scale, seen)
+        # (single tokens: sums of rounded probabilities, off by as much again)
+        bound = size * ((2.0 if q_len == 1 else 1.0) * 2.0 ** -8 + 2.0 ** -11) + ref.abs() * 2.0 ** -8
+        assert bool(torch.isfinite(out[at]).all())
+        assert bool(((out[at].double() - ref).abs() <= bound).all())
+        assert float((lse[at].double() - ref_lse).abs().max()) <= 2.0 ** -8 + 2.0 ** -11
+
+
 def test_layers_streams_and_graphs():
     rng = np.random.default_rng(7)
     b = Batch(rng, pic.GQA, pic.BF16, 2, 128, 128, 4, [6, 3], [[300, 65], [130]], [[20]] + [[]] * 8, [1] * 9,
