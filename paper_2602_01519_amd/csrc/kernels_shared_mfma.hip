@@ -186,7 +186,7 @@ __device__ __forceinline__ void compute_tile(const Lane<D> &c, const uint4 *kt, 
         if (32 * h + (x >> 3) * 16 + (x & 7) > kl) s[h][x] = -INFINITY;
     seen = kl >= 0;
   }
-  bf16x8 pf[2 * kN];                            // rounded to bf16, 2^-9 of each; the sums are not
+  bf16x8 pf[2 * kN];                            // rounded to bf16, 2^-8 of each; the sums are not
   auto probs = [&]() {
     const float neg = a.m == -INFINITY ? 0.f : -a.m;
     float t[2] = {0.f, 0.f};

@@ -123,6 +123,9 @@ struct Unit {
   const char *k_own, *v_own;            // the request's first own row, kv head applied
   int64_t own_stride;                   // bytes from own token to own token
   int own;                              // own keys that the token sees
+  // log2 of all these keys: the running maxima lie that far above the scores', so that a sum of
+  // probabilities is at most one and a sum of values no larger than the largest
+  float raise;
 };
 
 // ---- bf16 attention: columns of a 16x16x32 product
@@ -197,7 +200,7 @@ __device__ __forceinline__ void load_own(const Unit &u, int j0, int last, int la
 // nvalid: keys of the tile that count (may be 0 or less).
 template <int D>
 __device__ __forceinline__ void compute_tile(const Tile<D> &x, int nvalid, const bf16x8 (&qf)[D / 32],
-                                             State<D> &st, int lane, float sc) {
+                                             State<D> &st, int lane, float sc, float raise) {
   f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) {
@@ -214,7 +217,7 @@ __device__ __forceinline__ void compute_tile(const Tile<D> &x, int nvalid, const
   }
   float top = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
   top = col_max(top);
-  const float mnew = fmaxf(st.m, top * sc);
+  const float mnew = fmaxf(st.m, top * sc + raise);
   if (mnew > st.m) {
     const float alpha = __builtin_amdgcn_exp2f(st.m - mnew);   // 0 when st.m = -inf
     st.l *= alpha;
@@ -223,7 +226,7 @@ __device__ __forceinline__ void compute_tile(const Tile<D> &x, int nvalid, const
     st.m = mnew;
   }
   const float neg = st.m == -INFINITY ? 0.f : -st.m;
-  bf16x8 pf;                            // rounded to bf16 for the value product, 2^-9 of each
+  bf16x8 pf;                            // rounded to bf16 for the value product, 2^-8 of each
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -267,7 +270,7 @@ struct Attention<uint16_t, D> {
     for (int t = W - 1 - w; t * kT < u.own; t += W) {
       Tile<D> x;
       load_own<D>(u, t * kT, u.own - 1, lane, lds + (w % kWaves) * own_scratch<uint16_t, D>(), x);
-      compute_tile<D>(x, u.own - t * kT, qf, st, lane, sc);
+      compute_tile<D>(x, u.own - t * kT, qf, st, lane, sc, u.raise);
     }
   }
   __device__ __forceinline__ void blocks(const Unit &u, int w, int W, int lane, float sc) {
@@ -287,11 +290,11 @@ struct Attention<uint16_t, D> {
     for (int i = w; i < u.taken; i += W) {
       load_tile<D>(k, v, 1, lane, n > kT, tb);
       const int n0 = n;
-      compute_tile<D>(ta, n0, qf, st, lane, sc);
+      compute_tile<D>(ta, n0, qf, st, lane, sc, u.raise);
       const bool more = i + W < u.taken;
       if (more) block(i + W);
       load_tile<D>(k, v, 0, lane, more, ta);
-      if (n0 > kT) compute_tile<D>(tb, n0 - kT, qf, st, lane, sc);
+      if (n0 > kT) compute_tile<D>(tb, n0 - kT, qf, st, lane, sc, u.raise);
     }
   }
   __device__ __forceinline__ void store(int cols, int lane, float *o, float *m, float *l) {
@@ -327,7 +330,7 @@ struct Attention<float, D> {
     }
   }
   // scores of n keys, a lane one (its row at `row`), and their probabilities to LDS
-  __device__ __forceinline__ void scores(const float *row, int n, int lane, float sc) {
+  __device__ __forceinline__ void scores(const float *row, int n, int lane, float sc, float raise) {
     float s[C] = {0.f, 0.f, 0.f, 0.f};
     constexpr int kAhead = 8;           // 16-byte pieces of the row in flight
 #pragma unroll 1
@@ -349,7 +352,7 @@ struct Attention<float, D> {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const float x = lane < n ? s[c] * sc : -INFINITY;
-      const float mnew = fmaxf(m[c], wave_max(x));
+      const float mnew = fmaxf(m[c], wave_max(x) + raise);
       const float alpha = mnew == m[c] ? 1.f : __builtin_amdgcn_exp2f(m[c] - mnew);
       const float p = mnew == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - mnew);
       m[c] = mnew;
@@ -363,7 +366,7 @@ struct Attention<float, D> {
   __device__ __forceinline__ void own(const Unit &u, int w, int W, int lane, float sc, char *) {
     for (int t = W - 1 - w; t * 64 < u.own; t += W) {
       const int n = min(64, u.own - t * 64);
-      scores((const float *)(u.k_own + (t * 64 + min(lane, n - 1)) * u.own_stride), n, lane, sc);
+      scores((const float *)(u.k_own + (t * 64 + min(lane, n - 1)) * u.own_stride), n, lane, sc, u.raise);
 #pragma unroll 8
       for (int j = 0; j < n; ++j) {
         const float *v = (const float *)(u.v_own + (int64_t)(t * 64 + j) * u.own_stride);
@@ -381,7 +384,7 @@ struct Attention<float, D> {
     for (int i = w; i < u.taken; i += W) {
       const char *k = uniform(u.k[i]), *v = uniform(u.v[i]);
       const int n = __builtin_amdgcn_readfirstlane(u.n[i]);
-      scores((const float *)k + lane * D, n, lane, sc);      // (rows past the last are there, cleared)
+      scores((const float *)k + lane * D, n, lane, sc, u.raise);      // (rows past the last are there, cleared)
 #pragma unroll 1
       for (int h = 0; h * kPanel < n; ++h) {                 // panels of 32 tokens
         const float4 *vh = (const float4 *)((const float *)v + (h * D + lane) * kPanel);
@@ -589,6 +592,7 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   u.k_own = (const char *)p.k_self + own_at;
   u.v_own = (const char *)p.v_self + own_at;
   u.own = R.own;
+  u.raise = log2f((float)(take * kTile + R.own + 1));
   Attention<T, D> att;
   att.start(q + col0 * D, cols, lane, lds + at.extra);
   if (sizeof(T) == 4) {

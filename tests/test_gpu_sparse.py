@@ -174,6 +174,32 @@ def test_log_sums_are_of_unrounded_probabilities(d):
             at += 1
 
 
+@pytest.mark.parametrize("dtype,d", [(pic.BF16, 128), (pic.BF16, 64), (pic.F32, 128), (pic.F32, 64)])
+def test_values_near_the_largest(dtype, d):
+    """Values up to 2^126 under some 900 keys of like scores: their means stay finite. A probability is off
+    by half a bf16 step, 2^-8 of it, logits and fp32 sums (128 products, 900 values) by less than 2^-11 of
+    what they make, the output by half a step."""
+    rng = np.random.default_rng(15)
+    c = Case(rng, dtype, 2, d, 4, [70], [[0], [0]], [1, 1], own=[60, 0], capacity=64 * 40)
+    k = L.draw(rng, dtype, 1, 830, 2, d) * 0.25
+    big = lambda *s: (L.draw(rng, pic.F32, *s).clamp(-2, 2) * 2.0 ** 125).to(k.dtype)  # noqa: E731
+    v = big(1, 830, 2, d)
+    c.store.put(50, 830, k, v, L.stream())
+    c.index.update([50], stream=L.stream())
+    c.links = [[50], [50]]
+    c.vo = big(*c.vo.shape)
+    out, lse, _ = c.call(20)
+    torch.cuda.synchronize()
+    step = 2.0 ** -8 if dtype == pic.BF16 else 0.0
+    for t, own in ((0, slice(0, 61)), (1, slice(61, 62))):
+        kk, vv = torch.cat([k[0], c.ko[own]]), torch.cat([v[0], c.vo[own]])
+        ref, ref_lse = L.attend(c.q[t:t + 1], kk, vv, c.scale)
+        size, _ = L.attend(c.q[t:t + 1], kk, vv.abs(), c.scale)
+        assert bool(torch.isfinite(out[t]).all())
+        assert bool(((out[t].double() - ref[0]).abs() <= size[0] * (step + 2.0 ** -11) + ref[0].abs() * step).all())
+        assert float((lse[t].double() - ref_lse[0]).abs().max()) <= 2.0 ** -11
+
+
 def test_equal_scores_go_to_the_lower_block():
     rng = np.random.default_rng(4)
     c = Case(rng, pic.BF16, 2, 64, 3, [64, 128, 64], [[0, 0, 1, 0, 2, 0, 1, 0], [0] * 40], [1, 1])
