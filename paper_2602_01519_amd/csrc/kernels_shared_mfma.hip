@@ -369,7 +369,7 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
 #pragma unroll
         for (int x = 0; x < 16; ++x) most = __builtin_elementwise_maximum(most, fabsf(a.o[d][x]));   // (NaN if one is)
       if (steps.raise > 0.f || !__syncthreads_or(!(most <= FLT_MAX))) break;
-      steps = Steps{0.f, log2f((float)(t1 - t0)) + 6.f};
+      steps = Steps{0.f, ceilf(log2f((float)(t1 - t0))) + 6.f};
       restart();
     }
   }

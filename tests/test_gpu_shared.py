@@ -312,6 +312,31 @@ def test_layers_streams_and_graphs():
     b.store.remove(b.mine[0][0], L.stream())
 
 
+@pytest.mark.parametrize("own", [True, False])
+def test_narrow_heads_by_layer_captured(own):
+    """64-wide heads, several tokens: groups' and requests' blocks in one launch, own KV laid out before it."""
+    rng = np.random.default_rng(16)
+    q_len = [9, 1, 40, 0, 5]
+    b = Batch(rng, pic.GQA, pic.BF16, 2, 64, 64, 4, [3, 2], [[300, 65], [130]], [[20], [], [70, 1], [], []], q_len,
+              own=[3, 0, 64, 2, 0] if own else None, layers=2)
+    with b.plan() as plan, b.plan() as other:
+        graphs = []
+        for p, layer in ((plan, 0), (other, 1), (plan, 1)):
+            out, lse = b.buffers()
+            b.run(p, layer, out, lse)
+            b.check(out, lse, layer, "run")
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                b.run(p, layer, out, lse)
+            graphs.append((g, out, lse, layer))
+        for _ in range(3):
+            for g, out, lse, layer in graphs:
+                out.fill_(2.0)
+                g.replay()
+                b.check(out, lse, layer, "graph")
+            b.check(*b.call(1), 1, "between replays")
+
+
 def test_a_capture_takes_plans_alone():
     rng = np.random.default_rng(13)
     b = Batch(rng, pic.GQA, pic.BF16, 2, 128, 128, 4, [6], [[300]], [[]] * 6, [1] * 6, own=[9] * 6)
