@@ -49,6 +49,7 @@ __device__ __forceinline__ uint4 load_nt(const char *p) {
   const u32x4 w = __builtin_nontemporal_load((global_u32x4)p);
   return make_uint4(w.x, w.y, w.z, w.w);
 }
+__device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 template <typename P>
 __device__ __forceinline__ const char *uniform(P x) {     // a wave-uniform address
   const uint64_t a = (uint64_t)x;
@@ -269,7 +270,7 @@ struct Attention<uint16_t, D> {
   __device__ __forceinline__ void own(const Unit &u, int w, int W, int lane, float sc, char *lds) {
     for (int t = W - 1 - w; t * kT < u.own; t += W) {
       Tile<D> x;
-      load_own<D>(u, t * kT, u.own - 1, lane, lds + (w % kWaves) * own_scratch<uint16_t, D>(), x);
+      load_own<D>(u, t * kT, u.own - 1, lane, lds + uniform_wave() * own_scratch<uint16_t, D>(), x);
       compute_tile<D>(x, u.own - t * kT, qf, st, lane, sc, u.raise);
     }
   }
@@ -564,7 +565,7 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
                                             const SparseToken *tokens) {
   constexpr int kCols = sizeof(T) == 4 ? 4 : 16;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = uniform_wave();
   int x = blockIdx.x;
   const int split = x % p.splits;
   x /= p.splits;
@@ -581,7 +582,8 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   const T *q = (const T *)p.q + ((int64_t)tok * p.n_q_heads + kvh * p.group) * D;
 
   const int col0 = cb * kCols, cols = min(kCols, p.group - col0);
-  const int w = split * kWaves + wave, W = p.splits * kWaves;
+  // (the first blocks go to the first wave of every split, which has a SIMD to itself)
+  const int w = wave * p.splits + split, W = p.splits * kWaves;
   Unit u;
   u.k = sel_k;
   u.v = sel_v;
@@ -765,8 +767,6 @@ __global__ __launch_bounds__(256) void block_means_kernel(MeansParams p) {
 bool sparse_supported(int dtype, int mla, int d_k, int d_v) {
   return !mla && d_k == d_v && (d_k == 64 || d_k == 128) && (dtype == 0 || dtype == 1);
 }
-
-int sparse_waves() { return kWaves; }
 
 hipError_t launch_link_sparse(const SparseParams &p, const SparseTabs *tabs, int dtype, int d, hipStream_t st) {
   if (dtype == 0)

@@ -1988,12 +1988,14 @@ pic_status shared_link_call(pic_store *s, const pic_link_req *req, const pic_lin
 }
 
 // Workgroups that share a unit (query token x kv head) of `taken` blocks: as many as the CUs
-// have room for, down to a block a wave. Few CUs do not draw on all of HBM: one request of 24
-// blocks, 32/8 heads x 128, in 1 / 3 workgroups a unit 34 / 26 us, of 96 in 1 / 4 / 12 100 / 48 /
-// 37; 4 requests of 96 in 1 / 8 108 / 52. More than the CUs hold at once lose (12 requests of
+// have room for, down to two blocks each and up to 32 partials to merge. Few CUs do not draw on
+// all of HBM, and one keeps some 50 GB/s of it in flight: one request of 24 blocks, 32/8
+// heads x 128, in 3 / 6 / 12 / 24 workgroups a unit 22.9 / 20.9 / 19.1 / 18.9 us, of 96 in 12 / 32 27.8 /
+// 24.5, 4 requests of 96 in 1 / 8 108 / 52; one of 64, 16/2 heads, in 8 / 32 / 64 38.1 / 33.2 / 35.0, of 300,
+// 64-wide, in 38 / 75 / 128 32.3 / 33.4 / 35.4. More than the CUs hold at once lose (12 requests of
 // 64 in 2 / 3 66 / 95), as each scores and selects for itself.
 int32_t sparse_splits(int32_t cus, int64_t units, int32_t taken) {
-  const int32_t most = (taken + sparse_waves() - 1) / sparse_waves();
+  const int32_t most = std::min(32, (taken + 1) / 2);
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, cus / std::max<int64_t>(1, units)));
 }
 

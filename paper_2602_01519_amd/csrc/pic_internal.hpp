@@ -648,7 +648,6 @@ struct SparseTabs {
 };
 static_assert(sizeof(SparseParams) + sizeof(SparseTabs) <= 4064, "kernel arguments");
 bool sparse_supported(int dtype, int mla, int d_k, int d_v);
-int sparse_waves();           // of a workgroup, which share a unit's blocks
 // tabs: used in place of the tables when not NULL
 hipError_t launch_link_sparse(const SparseParams &p, const SparseTabs *tabs, int dtype, int d, hipStream_t st);
 
