@@ -176,13 +176,18 @@ def _ptr(x):
 
 def _token_stride(x) -> int:
     """Elements from token to token of a torch tensor [tokens][heads][width] whose tokens are dense
-    rows (0: leave it to the call)."""
+    rows, each of its own (0: dense, for one token or none)."""
     if x is None or not hasattr(x, "stride"):
         return 0
     strides, shape = x.stride(), x.shape
     if len(shape) != 3 or (shape[0] and shape[1] and (strides[2] != 1 or (shape[1] > 1 and strides[1] != shape[2]))):
         raise PicError(ERR_INVALID, "a tensor must be [tokens][heads][width] with dense rows")
-    return strides[0] if shape[0] > 1 else 0
+    if shape[0] <= 1:
+        return 0
+    # (tokens expanded from one have stride 0, which the library takes for dense rows)
+    if strides[0] < shape[1] * shape[2]:
+        raise PicError(ERR_INVALID, "a tensor's tokens must not share memory")
+    return strides[0]
 
 
 def _host_i32(a):
