@@ -362,13 +362,15 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
       walk();
       if constexpr (D == 128) break;
       // Probabilities against a max that lags reach 2^64: the sums of large values may leave the
-      // fp32 range. Then once more, against a max that keeps them below the largest value.
+      // fp32 range, of 128 rows also only where the two halves of the keys are joined. Then once
+      // more, against a max that keeps them below the largest value.
+      constexpr float kMost = kWide ? FLT_MAX : FLT_MAX / 2;
       float most = 0.f;
 #pragma unroll
       for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int x = 0; x < 16; ++x) most = __builtin_elementwise_maximum(most, fabsf(a.o[d][x]));   // (NaN if one is)
-      if (steps.raise > 0.f || !__syncthreads_or(!(most <= FLT_MAX))) break;
+      if (steps.raise > 0.f || !__syncthreads_or(!(most <= kMost))) break;
       steps = Steps{0.f, ceilf(log2f((float)(t1 - t0))) + 6.f};
       restart();
     }

@@ -1,0 +1,44 @@
+"""Shared links: the range of the values, and outputs where the parts of a row lie far apart."""
+import numpy as np
+import pytest
+import torch
+
+import link_model as L
+from paper_2602_01519_amd import pic
+
+pytestmark = pytest.mark.gpu
+
+
+def group_over(k, v, n, q_len, q, hq, scale, **kw):
+    """out, lse of n requests of q_len tokens that share one chunk and have no keys of their own."""
+    hkv, d = k.shape[1:]
+    with pic.Store(pic.GQA, pic.BF16, hkv, d, d, (len(k) + 63) // 64 * 64) as store:
+        store.put(1, len(k), k, v, L.stream())
+        out, lse = torch.full_like(q, 7.0), torch.zeros(len(q), hq, dtype=torch.float32, device="cuda")
+        pic.link_shared(store, [0, n], [0, 1], [1], [0] * (n + 1), [], L.offsets([q_len] * n), None, hq, q, None, None,
+                        scale, out, lse, stream=L.stream(), **kw)
+        torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("q_len,n", [(5, 3), (8, 4), (20, 1)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_halves_of_a_block_that_pass_the_range_only_together(q_len, n, sign):
+    """64-wide heads, groups of 60..128 rows, whose two halves of each tile's keys are summed apart. Over a
+    first tile of logits 0 the next one's are 41 (2^59.15): a half is 32 x 2^59.15 x 1.375 x 2^63 =
+    2^127.61, within fp32's range, both are not; the output is 1.375 x 2^63 but for the first tile's share, 2^-59 of
+    that. A probability is off by half a bf16 step, 2^-8 of it, exponents and fp32 sums by less than 2^-11, the output by
+    half a step."""
+    k = torch.zeros(128, 2, 64, dtype=torch.bfloat16, device="cuda")
+    k[64:, :, 0] = 41.0
+    v = torch.ones_like(k)
+    v[64:] = sign * 1.375 * 2.0 ** 63
+    v[64:, :, 1::2] *= -1
+    q = torch.zeros(n * q_len, 8, 64, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 8.0
+    out, lse = group_over(k, v, n, q_len, q, 8, 0.125)
+    ref, ref_lse = L.attend(q, k, v, 0.125)
+    over = float(((out.double() - ref).abs() - ref.abs() * (2.0 ** -7 + 2.0 ** -11)).max())
+    assert over <= 0
+    off = float((lse.double() - ref_lse).abs().max())
+    assert off <= 2.0 ** -11
