@@ -478,7 +478,7 @@ pic_status pic_link_sparse(pic_index *index, const pic_link_req *req, int32_t n_
  * address resolution the attention kernels use. k_out: device token-major
  * [sum len][H_kv][d_k]; v_out: device [sum len][H_kv][d_v] (GQA) or NULL
  * (MLA). Bit-exact copies.
- * Errors: INVALID, NOT_FOUND, HIP. */
+ * Errors: INVALID (also more than 2^31 - 1 tokens in all), NOT_FOUND, HIP. */
 pic_status pic_debug_gather(pic_store *store, const uint64_t *ids, int32_t n, int32_t layer,
                             void *k_out, void *v_out, void *stream);
 

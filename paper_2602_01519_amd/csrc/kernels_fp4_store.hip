@@ -216,14 +216,16 @@ hipError_t launch_fp4_gather(const LinkEntry *links, int32_t n_links, int32_t he
                              void *k, void *v, hipStream_t st) {
   GatherLinks g{};
   g.n = n_links;
-  int32_t tiles = 0;
+  int64_t tiles = 0;
   for (int32_t i = 0; i < n_links; ++i) {
-    g.tile0[i] = tiles;
+    g.tile0[i] = (int32_t)tiles;
     g.page[i] = (const char *)links[i].k;
     g.len[i] = links[i].len;
     g.tok0[i] = links[i].tok0;
     tiles += (links[i].len + 63) / 64;
   }
+  // (a launch's threads are counted in 32 bits: 2^30 tokens, 256 GB and more of output)
+  if (tiles >= 1 << 24) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)tiles, (unsigned)heads);
   if (d == 128)
     hipLaunchKernelGGL(fp4_gather_kernel<128>, grid, dim3(256), 0, st, g, heads, (uint16_t *)k,

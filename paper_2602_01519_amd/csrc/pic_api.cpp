@@ -3342,7 +3342,7 @@ pic_status pic_debug_gather(pic_store *s, const uint64_t *ids, int32_t n, int32_
       toks += r.ntok;
       pages += (r.ntok + kTile - 1) / kTile;
     }
-    if (toks > INT32_MAX / 2) return fail(PIC_ERR_INVALID, "too many tokens");
+    if (toks > INT32_MAX) return fail(PIC_ERR_INVALID, "the listed chunks hold more than 2^31 - 1 tokens");
   }
   n = (int32_t)links.size();
   if (toks == 0) return PIC_OK;
