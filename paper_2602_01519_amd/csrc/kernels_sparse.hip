@@ -38,6 +38,10 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kT = 32;                  // keys per tile (bf16)
+template <typename T>
+constexpr int kCols = sizeof(T) == 4 ? 4 : 16;   // query heads of a workgroup
+template <typename T>
+int col_blocks(int group) { return (group + kCols<T> - 1) / kCols<T>; }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -100,7 +104,6 @@ __host__ __device__ constexpr uint32_t own_scratch() {
 }
 template <typename T, int D>
 __host__ __device__ __forceinline__ Layout layout_of(int n, int k, int cols, bool own) {
-  constexpr int kCols = sizeof(T) == 4 ? 4 : 16;
   Layout l;
   l.page = 8u * n;                      // keys: 8 bytes a block from 0
   l.link = l.page + 4u * n;
@@ -109,7 +112,7 @@ __host__ __device__ __forceinline__ Layout layout_of(int n, int k, int cols, boo
   l.sel_n = l.sel_v + 8u * k;
   l.extra = (l.sel_n + 4u * k + 15) & ~15u;
   // fp32: the queries, and each wave's probabilities
-  l.bytes = l.extra + (sizeof(T) == 4 ? 4u * kCols * D + 4u * kWaves * kCols * 64 : 0u);
+  l.bytes = l.extra + (sizeof(T) == 4 ? 4u * kCols<T> * D + 4u * kWaves * kCols<T> * 64 : 0u);
   const uint32_t merge = 4u * kWaves * cols * (D + 2);
   if (l.bytes < merge) l.bytes = merge;
   if (own && l.bytes < own_scratch<T, D>() * kWaves) l.bytes = own_scratch<T, D>() * kWaves;
@@ -563,7 +566,6 @@ __device__ __forceinline__ void select_blocks(const uint64_t *key, int n, int ta
 template <typename T, int D>
 __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseLink *links,
                                             const SparseToken *tokens) {
-  constexpr int kCols = sizeof(T) == 4 ? 4 : 16;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, wave = uniform_wave();
   int x = blockIdx.x;
@@ -581,7 +583,7 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   int32_t *sel_n = (int32_t *)(lds + at.sel_n);
   const T *q = (const T *)p.q + ((int64_t)tok * p.n_q_heads + kvh * p.group) * D;
 
-  const int col0 = cb * kCols, cols = min(kCols, p.group - col0);
+  const int col0 = cb * kCols<T>, cols = min(kCols<T>, p.group - col0);
   // (the first blocks go to the first wave of every split, which has a SIMD to itself)
   const int w = wave * p.splits + split, W = p.splits * kWaves;
   Unit u;
@@ -600,7 +602,7 @@ __device__ __forceinline__ void link_sparse(const SparseParams &p, const SparseL
   Attention<T, D> att;
   att.start(q + col0 * D, cols, lane, lds + at.extra);
   if (sizeof(T) == 4) {
-    for (int i = threadIdx.x; i < kCols * D; i += kThreads)
+    for (int i = threadIdx.x; i < kCols<T> * D; i += kThreads)
       ((float *)(lds + at.extra))[i] = i < cols * D ? to_float(q[col0 * D + i]) : 0.f;
     __syncthreads();
   }
@@ -712,9 +714,8 @@ __global__ __launch_bounds__(kThreads, 1) void link_sparse_tabs_kernel(SparsePar
 
 template <typename T, int D>
 hipError_t launch_sparse_t(SparseParams p, const SparseTabs *tabs, hipStream_t st) {
-  constexpr int kCols = sizeof(T) == 4 ? 4 : 16;
-  p.col_blocks = (p.group + kCols - 1) / kCols;
-  p.cols = std::min(kCols, p.group);
+  p.col_blocks = col_blocks<T>(p.group);
+  p.cols = std::min(kCols<T>, p.group);
   const size_t lds = layout_of<T, D>(p.most_blocks, p.n_blocks, p.cols, p.k_self != nullptr).bytes;
   const void *f = tabs ? (const void *)link_sparse_tabs_kernel<T, D> : (const void *)link_sparse_kernel<T, D>;
   hipError_t e = hipSuccess;
@@ -767,6 +768,8 @@ __global__ __launch_bounds__(256) void block_means_kernel(MeansParams p) {
 bool sparse_supported(int dtype, int mla, int d_k, int d_v) {
   return !mla && d_k == d_v && (d_k == 64 || d_k == 128) && (dtype == 0 || dtype == 1);
 }
+
+int sparse_columns(int dtype, int group) { return dtype == 0 ? col_blocks<float>(group) : col_blocks<uint16_t>(group); }
 
 hipError_t launch_link_sparse(const SparseParams &p, const SparseTabs *tabs, int dtype, int d, hipStream_t st) {
   if (dtype == 0)

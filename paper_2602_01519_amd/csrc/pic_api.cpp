@@ -1987,13 +1987,17 @@ pic_status shared_link_call(pic_store *s, const pic_link_req *req, const pic_lin
   return PIC_OK;
 }
 
-// Workgroups that share a unit (query token x kv head) of `taken` blocks: as many as the CUs
-// have room for, down to two blocks each and up to 32 partials to merge. Few CUs do not draw on
-// all of HBM, and one keeps some 50 GB/s of it in flight: one request of 24 blocks, 32/8
+// Workgroups that share a unit (query token x kv head x column block of its query heads) of `taken`
+// blocks: as many as the CUs have room for, down to two blocks each and up to 32 partials to merge. Few CUs
+// do not draw on all of HBM, and one keeps some 50 GB/s of it in flight: one request of 24 blocks, 32/8
 // heads x 128, in 3 / 6 / 12 / 24 workgroups a unit 22.9 / 20.9 / 19.1 / 18.9 us, of 96 in 12 / 32 27.8 /
 // 24.5, 4 requests of 96 in 1 / 8 108 / 52; one of 64, 16/2 heads, in 8 / 32 / 64 38.1 / 33.2 / 35.0, of 300,
 // 64-wide, in 38 / 75 / 128 32.3 / 33.4 / 35.4. More than the CUs hold at once lose (12 requests of
-// 64 in 2 / 3 66 / 95), as each scores and selects for itself.
+// 64 in 2 / 3 66 / 95), as each scores and selects for itself. So do column blocks that are not counted
+// (fp32, 64/8 heads x 64, 32 of 64 blocks, 4 / 16 requests 43.3 / 70.8, counted 28.7 / 55.0; bf16, 40/2
+// heads x 128, 8 / 64 requests 42.1 / 94.9, counted 27.6 / 70.8). Units above the CUs run in
+// whole rounds, one workgroup a CU: 31 / 32 / 33 / 48 / 64 / 65 requests of 32 blocks, 32/8 heads x 128,
+// 62 / 63 / 101 / 112 / 119 / 155 us.
 int32_t sparse_splits(int32_t cus, int64_t units, int32_t taken) {
   const int32_t most = std::min(32, (taken + 1) / 2);
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, cus / std::max<int64_t>(1, units)));
@@ -3265,7 +3269,8 @@ pic_status pic_link_sparse(pic_index *x, const pic_link_req *req, int32_t n_q_he
     if (!dg.ok) return fail(PIC_ERR_HIP, "cannot select the store's device");
     const hipStream_t st = (hipStream_t)stream;
     const bool by_arg = links.size() <= (size_t)kSparseTabLinks && tq <= kSparseTabTokens;
-    p.splits = sparse_splits(s->shape.cus, (int64_t)tq * d.n_kv_heads, std::min(n_blocks, p.most_blocks));
+    p.splits = sparse_splits(s->shape.cus, (int64_t)tq * d.n_kv_heads * sparse_columns(d.dtype, p.group),
+                             std::min(n_blocks, p.most_blocks));
     if (capturing(st)) {
       if (!by_arg)
         return fail(PIC_ERR_UNSUPPORTED, "in a graph capture a call has at most %d links and %d query tokens",

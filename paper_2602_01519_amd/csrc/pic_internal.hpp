@@ -648,6 +648,7 @@ struct SparseTabs {
 };
 static_assert(sizeof(SparseParams) + sizeof(SparseTabs) <= 4064, "kernel arguments");
 bool sparse_supported(int dtype, int mla, int d_k, int d_v);
+int sparse_columns(int dtype, int group);     // workgroups that share a kv head's query heads
 // tabs: used in place of the tables when not NULL
 hipError_t launch_link_sparse(const SparseParams &p, const SparseTabs *tabs, int dtype, int d, hipStream_t st);
 
