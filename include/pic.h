@@ -310,8 +310,10 @@ typedef struct pic_link_req {
  * over long documents), the library splits each request's keys and merges
  * the partial softmax states exactly, as pic_link_decode does; the result
  * is the same up to floating-point rounding order.
- * Values above 2^63 in magnitude may give infinities in bf16 GQA stores of
- * d 128 and bf16 MLA stores of 576 / 512.
+ * In bf16 GQA stores of d 128 and bf16 MLA stores of 576 / 512, values above
+ * 2^61 / T in magnitude may give infinities, T the 64-token tiles that a row
+ * sees (pic_link_decode, d 128: only with more than 16 query rows per kv head,
+ * or limits that differ within a request).
  * UNSUPPORTED: one request's query rows alone pass what one launch holds
  * (2^23 - 1 workgroups of its row blocks; no limit of the batch).
  * Errors: INVALID, NOT_FOUND, UNSUPPORTED, HIP. */
@@ -412,9 +414,10 @@ pic_status pic_link_plan_destroy(pic_link_plan *plan);
  *     the batch. A group may be empty or share nothing.
  * Tensors, scale and lse as for pic_link_attn. Workspace: fp32 partials of every query row,
  * about 2 Tq * H_q * (d_v + 2) * 4 bytes or more where keys are split.
- * The range of the values and the rounding of lse are those of the store's link calls; over bf16
- * GQA stores with d_k = d_v = 128, or 64 and more than 16 query rows per kv head, the sums are of
- * fp32 probabilities.
+ * The range of the values and the rounding of lse are those of pic_link_attn: over bf16 GQA stores
+ * of d 128 and bf16 MLA stores of 576 / 512 values up to 2^61 / T, for single tokens too, where
+ * pic_link_decode takes larger ones. Over bf16 GQA stores with d_k = d_v = 128, or 64 and more than 16
+ * query rows per kv head, the sums are of fp32 probabilities.
  * pic_link_shared_plan_create: the same, resolved once (req->layer must be 0), run and
  *   destroyed by pic_link_plan_run and pic_link_plan_destroy: a run enqueues kernels only, and may
  *   be captured.

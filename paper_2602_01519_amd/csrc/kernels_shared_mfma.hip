@@ -360,7 +360,7 @@ __device__ __forceinline__ void block_partial(const LinkParams &p, const WorkIte
 #pragma unroll 1
     for (;;) {
       walk();
-      if constexpr (D == 128) break;
+      if constexpr (D == 128) break;            // (values up to 2^61 / tiles: see pic.h)
       // Probabilities against a max that lags reach 2^64: the sums of large values may leave the
       // fp32 range, of 128 rows also only where the two halves of the keys are joined. Then once
       // more, against a max that keeps them below the largest value.

@@ -42,3 +42,42 @@ def test_halves_of_a_block_that_pass_the_range_only_together(q_len, n, sign):
     assert over <= 0
     off = float((lse.double() - ref_lse).abs().max())
     assert off <= 2.0 ** -11
+
+
+@pytest.mark.parametrize("q_len,n,docs", [(1, 3, 700), (1, 70, 700), (3, 4, 130), (6, 3, 700), (40, 3, 700), (1, 160, 25001)])
+def test_wide_heads_up_to_the_stated_range(q_len, n, docs):
+    """128-wide heads: values up to 2^61 / T, T the 64-token tiles that a row sees, over a first tile of logits 0
+    and others 40 above it (2^57.7, which no maximum follows: a lane's 32 probabilities stay below 2^64). A
+    probability is off by half a bf16 step, 2^-8 of it, exponents and fp32 sums of up to 25,200 keys of one
+    size by less than 2^-9, the output by half a step."""
+    rng = np.random.default_rng(q_len + n)
+    own = q_len + 30
+    most = 2.0 ** (61 - int(np.ceil(np.log2((docs + 63) // 64 + (own + 63) // 64))))
+    big = lambda *s: (L.draw(rng, pic.F32, *s).clamp(-2, 2) * (most / 2)).bfloat16()  # noqa: E731
+    k = torch.zeros(docs, 2, 128, dtype=torch.bfloat16, device="cuda")
+    k[64:, :, 0] = 40.0
+    v = big(docs, 2, 128)
+    v[64:, :, :64] = v[64:, :, :64].abs()          # (sums of one sign in half of the columns)
+    q = torch.zeros(n * q_len, 8, 128, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 8.0
+    ko = torch.zeros(n * own, 2, 128, dtype=torch.bfloat16, device="cuda")
+    ko[::3, :, 0] = 38.0
+    vo = big(n * own, 2, 128)
+    out, lse = torch.full_like(q, 7.0), torch.zeros(n * q_len, 8, dtype=torch.float32, device="cuda")
+    with pic.Store(pic.GQA, pic.BF16, 2, 128, 128, (docs + 63) // 64 * 64) as store:
+        store.put(1, docs, k, v, L.stream())
+        pic.link_shared(store, [0, n], [0, 1], [1], [0] * (n + 1), [], L.offsets([q_len] * n), L.offsets([own] * n), 8, q,
+                        ko, vo, 0.125, out, lse, stream=L.stream())
+        torch.cuda.synchronize()
+    finite = bool(torch.isfinite(out).all())
+    assert finite
+    over = off = -1.0
+    for r in range(n):
+        at, rows = slice(r * q_len, (r + 1) * q_len), slice(r * own, (r + 1) * own)
+        kk, vv, seen = torch.cat([k, ko[rows]]), torch.cat([v, vo[rows]]), L.causal(q_len, own, docs)
+        ref, z = L.attend(q[at], kk, vv, 0.125, seen)
+        size, _ = L.attend(q[at], kk, vv.abs(), 0.125, seen)
+        over = max(over, float(((out[at].double() - ref).abs() - size * (2.0 ** -8 + 2.0 ** -9) - ref.abs() * 2.0 ** -8).max() / most))
+        off = max(off, float((lse[at].double() - z).abs().max()))
+    assert over <= 0
+    assert off <= 2.0 ** -9
