@@ -194,18 +194,20 @@ pic_status pic_store_write_rows(pic_store *store, uint64_t chunk_id, int32_t lay
  *     positions  device int32 [n], any value (with a handle)
  *   Several chunks of a batch are one launch. Ordered on `stream`; link calls already
  *   enqueued on another stream may see either content of a chunk's last page. A captured
- *   call writes the same rows again when it is replayed. Errors: INVALID (not a growing
- *   chunk, one that a live plan links, bad arguments), NOT_FOUND, OOM (beyond max_tokens),
- *   HIP; on an error no chunk has grown.
+ *   call writes the same rows again when it is replayed, and zeros behind them to the end of a
+ *   64-token page that it began: rows appended there since are lost, and a block index is not told
+ *   of either. Errors: INVALID (not a growing chunk, one that a live plan links, bad arguments),
+ *   NOT_FOUND, OOM (beyond max_tokens), HIP; on an error no chunk has grown.
  * pic_store_truncate: chunk chunk_ids[i] keeps at most its first n_tokens[i] tokens in
  *   every layer (n_tokens[i] at most what some layer holds): tokens that were proposed
- *   and not accepted. The rows taken back are cleared on `stream`. Errors: INVALID, NOT_FOUND,
- *   HIP.
+ *   and not accepted. The rows taken back are cleared on `stream` as far as they share a page with
+ *   rows that stay, by a captured call at each replay. Errors: INVALID, NOT_FOUND, HIP.
  * A growing chunk is linked, gathered, removed and exported like any other (one without
  * tokens adds no rows; pic_store_lookup: the fewest tokens of any layer, which is also what
  * an export holds); a link plan takes it as it stands, with as many tokens in every layer,
- * and it neither grows nor shrinks while the plan lives. pic_store_derive refuses it
- * (INVALID). */
+ * and it neither grows nor shrinks while the plan lives: a decode loop whose own tokens are in
+ * growing chunks makes direct calls, and one that runs a plan hands them over as own KV.
+ * pic_store_derive refuses it (INVALID). */
 pic_status pic_store_open(pic_store *store, uint64_t chunk_id, int64_t max_tokens);
 typedef struct pic_rope pic_rope;
 typedef struct pic_append {
@@ -462,7 +464,9 @@ pic_status pic_link_shared_plan_create(pic_store *store, const pic_link_req *req
  *   NULL. blocks: device int32 [Tq][n_kv_heads][n_blocks] or NULL: receives the taken blocks,
  *   ascending, -1 behind them. n_blocks 1 .. 1024, a request's blocks at most 8192 (else
  *   UNSUPPORTED). One token a request is the ordinary use (a decode step); several are
- *   computed one by one. A graph capture takes calls of up to 88 links and 32 query tokens in
+ *   computed one by one. It is the faster call for long document sets, n_blocks a few tenths
+ *   of them at most: with 16 or 24 blocks of 32/8 heads x 128, from about 128 blocks a request on for one or
+ *   two requests, 64 for four and 32 for sixteen. A graph capture takes calls of up to 88 links and 32 query tokens in
  *   all (else UNSUPPORTED); a replay reads the rows that those links had, so their chunks have
  *   to stay. Errors: INVALID (also a linked chunk whose summaries in the layer are
  *   not those of its present content), NOT_FOUND, UNSUPPORTED, OOM, HIP. */
